@@ -357,6 +357,114 @@ int ecoserve_attn_decode_noalloc(int device, const ecoserve_layout* layout, cons
                                  void* stream);
 
 /*
+ * KV-cache append with the position rotation on the way (Section 2.1: a layer's attention works on query and key
+ * embeddings; models encode a token's position by turning pairs of their elements).  Pair i of a head vector, i <
+ * rotary_dim / 2, is turned by the angle  theta = position * inv_freq[i]:
+ *     (a, b)  ->  (a cos theta - b sin theta,  a sin theta + b cos theta),
+ * in fp32, rounded once to E; theta is formed and reduced in 64 bits, so positions may be as large as int32 goes.
+ * Elements from rotary_dim on are not turned.  The rotated K rows and the V rows join the cache as ecoserve_kv_append
+ * stores them, and the rotated Q rows go to q_out, in one launch.
+ */
+enum { ECOSERVE_ROPE_HALVES = 0,    /* pair i is elements (i, i + rotary_dim / 2) */
+       ECOSERVE_ROPE_ADJACENT = 1   /* pair i is elements (2 i, 2 i + 1) */ };
+enum { ECOSERVE_ROPE_MAX_AXES = 4 };
+typedef struct {
+  int32_t rotary_dim;  /* elements turned: in (0, head_dim], a multiple of 8 (BF16) or 4 (F32) */
+  int32_t pairing;     /* ECOSERVE_ROPE_* */
+  int32_t num_axes;    /* position coordinates per token, 1 .. ECOSERVE_ROPE_MAX_AXES (images, video: time, height, width) */
+  uint8_t axis[128];   /* axis[i] < num_axes: the coordinate that turns pair i; entries from rotary_dim / 2 on are not read */
+} ecoserve_rope;
+
+/*
+ *   rope         : host
+ *   inv_freq     : dev, double[rotary_dim / 2], radians per position, 8-byte aligned
+ *   positions    : dev, int32[num_axes][T], coordinate a of packed token t at [a][t]; or NULL with num_axes == 1:
+ *                  the token's place in its sequence, ctx_before[b] + i
+ *   q, q_out     : dev, E[T][Hq][D] with rows q_row_stride and q_out_row_stride elements apart (rules of the strided
+ *                  calls), 16-byte aligned; both NULL: only K and V.  They may be the same array with the same stride;
+ *                  arrays that overlap otherwise: undefined.  Rows of q_out that belong to no sequence are left alone.
+ *   everything else as in ecoserve_kv_append_strided (max_new_len <= 1 again selects the one-token launch).
+ */
+int ecoserve_kv_append_rope(ecoserve_ctx* ctx, const ecoserve_rope* rope, const double* inv_freq, const int32_t* positions,
+                            const void* q, int64_t q_row_stride, void* q_out, int64_t q_out_row_stride, void* k_cache,
+                            void* v_cache, const void* k_new, const void* v_new, int64_t new_row_stride,
+                            const int32_t* cu_q, const int32_t* ctx_before, const int32_t* block_table,
+                            int32_t bt_stride, int32_t B, int32_t T, int32_t max_new_len, void* stream);
+
+/*
+ * Attention over a few blocks of a long context.  Table 2 has decode attention bound by the bytes of the cached keys
+ * and values; these three calls have a query read the blocks that a cheap score picks instead of all of them:
+ *   1. ecoserve_kv_summary keeps, per full cache block and K/V head, the largest and the smallest key of every channel in
+ *      one byte each (1/16 of the bf16 block's keys, 1/32 of keys and values);
+ *   2. ecoserve_block_select lets every (token, K/V head) choose blocks by a bound on its scores q.k from the summaries;
+ *   3. ecoserve_attn_sparse attends to the keys of the chosen blocks.
+ * Summaries are whole numbers with an exponent per (block, head): with A the largest |key| of the block,
+ *     e = the smallest integer >= -126 with A <= 127 * 2^e,
+ *     top[d] = ceil(max_s k[s][d] / 2^e),   low[d] = floor(min_s k[s][d] / 2^e)        (so they bound the keys),
+ * and a block that holds a NaN or an infinity has e = 127 and zeros.  One layer's buffer, all int8:
+ *     codes     [num_blocks][Hkv][2][Dp]   top, then low; Dp = head_dim rounded up to 32, zeros from head_dim on
+ *     exponents [num_blocks][Hkv]
+ * of ecoserve_summary_bytes(layout) bytes.  A query head is coded the same way, q8[d] = rint(q[d] / 2^eq) (half to even; a
+ * head with a NaN or an infinity: zeros, eq = 0), and the score of block j for K/V head g of a token is
+ *     max over the heads h of g of  2^(eq[h] + e) * sum_d max(q8[h][d] * top[d], q8[h][d] * low[d]),
+ * +inf if e = 127.  The sums are integers below 2^22, so scores are exact in fp32 and which blocks are chosen does not
+ * depend on the order of any sum.
+ */
+size_t ecoserve_summary_bytes(const ecoserve_layout* layout); /* 0 if the layout is invalid */
+
+/*
+ * Summarises the blocks that the call's tokens have filled: those of which a new token took slot 15.  Call it behind every
+ * append, with the same arguments; blocks that are not full yet keep what their summary holds, and nothing reads it.
+ *   k_cache : dev, 16-byte aligned;  summary : dev, in/out, layout above, 16-byte aligned
+ *   cu_q, ctx_before, block_table, bt_stride, B, T, max_new_len, stream : as in ecoserve_kv_append
+ */
+int ecoserve_kv_summary(ecoserve_ctx* ctx, const void* k_cache, void* summary, const int32_t* cu_q,
+                        const int32_t* ctx_before, const int32_t* block_table, int32_t bt_stride, int32_t B, int32_t T,
+                        int32_t max_new_len, void* stream);
+
+/*
+ * Selection.  The token at position p sees n = p / 16 + 1 blocks of its sequence, the last one with its own key.  Chosen are
+ * the first keep_first, the last keep_last and, of the others, those of the highest score, the lower index first among equal
+ * scores; num_selected in all, or all n if there are no more.  Every full block but the last of any token's must have been
+ * summarised.
+ *
+ *   q            : dev, E[T][Hq][D], rows q_row_stride elements apart (rotated, as the keys in the cache are)
+ *   cu_q         : dev, int32[B+1], or NULL: one token per sequence, token b of sequence b (T == B)
+ *   ctx_before   : dev, int32[B]: token i of sequence b is at position ctx_before[b] + i; a negative position (a place of
+ *                  a padded batch) sees nothing
+ *   blocks       : dev, out, int32[T][Hkv][num_selected]: logical blocks (indices into the sequence's row of the block
+ *                  table), ascending, -1 behind the last.  Rows of tokens behind cu_q[B] are left alone.
+ *   num_selected : 1 .. 65536;  keep_first >= 0, keep_last >= 1, keep_first + keep_last <= num_selected
+ *   max_ctx_len  : upper bound on any token's position + 1, as in ecoserve_attn_decode
+ *   workspace    : dev, 16-byte aligned, at least ecoserve_select_workspace_bytes(layout, T, max_ctx_len) bytes; nothing in
+ *                  it is kept from call to call, calls that overlap need one each (recorded into graphs: each graph one, if
+ *                  they may run at the same time)
+ */
+size_t ecoserve_select_workspace_bytes(const ecoserve_layout* layout, int32_t T, int32_t max_ctx_len);
+int ecoserve_block_select(ecoserve_ctx* ctx, const void* q, int64_t q_row_stride, const void* summary, const int32_t* cu_q,
+                          const int32_t* ctx_before, const int32_t* block_table, int32_t bt_stride, int32_t* blocks,
+                          int32_t num_selected, int32_t keep_first, int32_t keep_last, int32_t B, int32_t T,
+                          int32_t max_ctx_len, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Eq. 2 over listed blocks: the token at position p attends, for the heads of K/V head g, to the keys at positions <= p of the
+ * blocks in its list.  Entries outside 0 .. p / 16 (-1 among them) hold no keys, in any place of the list; the order of a list
+ * matters to rounding alone; a block listed twice counts twice.  Lists from ecoserve_block_select or any other source.
+ * A token without keys: out 0, lse -inf.
+ *
+ *   blocks       : dev, int32[T][Hkv][num_selected], num_selected 1 .. 65536
+ *   out, lse     : as in ecoserve_attn_prefill (lse may be NULL); rows of tokens behind cu_q[B] are left alone
+ *   workspace    : dev, 16-byte aligned, at least ecoserve_sparse_workspace_bytes(ctx, T, num_selected) bytes (0 for many
+ *                  tokens; NULL is fine then); rules as above
+ *   everything else as in ecoserve_block_select.
+ */
+size_t ecoserve_sparse_workspace_bytes(const ecoserve_ctx* ctx, int32_t T, int32_t num_selected);
+int ecoserve_attn_sparse(ecoserve_ctx* ctx, const void* q, int64_t q_row_stride, const void* k_cache, const void* v_cache,
+                         const int32_t* cu_q, const int32_t* ctx_before, const int32_t* block_table, int32_t bt_stride,
+                         const int32_t* blocks, int32_t num_selected, void* out, float* lse, int32_t B, int32_t T,
+                         void* workspace, size_t workspace_bytes, void* stream);
+
+/*
  * Machine ceilings for the roofline reasoning of Section 2.1 (Table 2 prices
  * decode attention in bytes read, prefill attention in matrix FLOPs): what
  * `device` sustains on each resource, to be reported beside the published

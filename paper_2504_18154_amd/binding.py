@@ -31,13 +31,20 @@ EXPORTS = [
     "ecoserve_kv_append_strided", "ecoserve_attn_prefill_strided", "ecoserve_attn_decode_strided",
     "ecoserve_attn_decode_append", "ecoserve_attn_decode_noalloc", "ecoserve_probe_mfma_valu",
     "ecoserve_debug_prefill_queue_shares",
+    "ecoserve_kv_append_rope", "ecoserve_summary_bytes", "ecoserve_kv_summary", "ecoserve_select_workspace_bytes",
+    "ecoserve_block_select", "ecoserve_sparse_workspace_bytes", "ecoserve_attn_sparse",
 ]
+ROPE_HALVES, ROPE_ADJACENT = 0, 1
 
 
 class Layout(ctypes.Structure):
     _fields_ = [("num_q_heads", ctypes.c_int32), ("num_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
                 ("block_size", ctypes.c_int32), ("num_blocks", ctypes.c_int32), ("dtype", ctypes.c_int32),
                 ("softmax_scale", ctypes.c_float)]
+
+
+class RopeStruct(ctypes.Structure):
+    _fields_ = [("rotary_dim", ctypes.c_int32), ("pairing", ctypes.c_int32), ("num_axes", ctypes.c_int32), ("axis", ctypes.c_uint8 * 128)]
 
 
 class EcoserveError(RuntimeError):
@@ -74,6 +81,17 @@ def _load(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.ecoserve_attn_decode_append.argtypes = [vp, vp, i64, vp, vp, i64, vp, vp, i32p, i32, i32p, vp, vp, i32, i32, vp]
     lib.ecoserve_attn_decode_noalloc.argtypes = [ctypes.c_int, ctypes.POINTER(Layout), vp, vp, vp, i32p, i32, i32p, vp, vp,
                                                  i32, i32, vp]
+    sz = ctypes.c_size_t
+    lib.ecoserve_kv_append_rope.argtypes = [vp, ctypes.POINTER(RopeStruct), vp, i32p, vp, i64, vp, i64, vp, vp, vp, vp, i64, i32p, i32p, i32p, i32, i32, i32,
+                                            i32, vp]
+    lib.ecoserve_summary_bytes.argtypes = [ctypes.POINTER(Layout)]
+    lib.ecoserve_kv_summary.argtypes = [vp, vp, vp, i32p, i32p, i32p, i32, i32, i32, i32, vp]
+    lib.ecoserve_select_workspace_bytes.argtypes = [ctypes.POINTER(Layout), i32, i32]
+    lib.ecoserve_block_select.argtypes = [vp, vp, i64, vp, i32p, i32p, i32p, i32, i32p, i32, i32, i32, i32, i32, i32, vp, sz, vp]
+    lib.ecoserve_sparse_workspace_bytes.argtypes = [vp, i32, i32]
+    for f in (lib.ecoserve_summary_bytes, lib.ecoserve_select_workspace_bytes, lib.ecoserve_sparse_workspace_bytes):
+        f.restype = sz
+    lib.ecoserve_attn_sparse.argtypes = [vp, vp, i64, vp, vp, i32p, i32p, i32p, i32, i32p, i32, vp, vp, i32, i32, vp, sz, vp]
     lib.ecoserve_debug_validate.argtypes = [vp, i32p, i32p, i32p, i32, i32]
     lib.ecoserve_debug_prefill_queue_shares.argtypes = [vp, ctypes.POINTER(ctypes.c_float)]
     lib.ecoserve_profile_read.argtypes = [vp, i32, ctypes.POINTER(ctypes.c_double), ctypes.POINTER(ctypes.c_int64)]
@@ -112,6 +130,15 @@ def make_layout(Hq, Hkv, D, num_blocks, dtype, bs=16, softmax_scale=0.0) -> Layo
 
 def cache_bytes(layout: Layout) -> int:
     return int(_lib.ecoserve_cache_bytes(ctypes.byref(layout)))
+
+
+def summary_bytes(layout: Layout) -> int:
+    """Bytes of one layer's block summaries."""
+    return int(_lib.ecoserve_summary_bytes(ctypes.byref(layout)))
+
+
+def select_workspace_bytes(layout: Layout, T: int, max_ctx_len: int) -> int:
+    return int(_lib.ecoserve_select_workspace_bytes(ctypes.byref(layout), int(T), int(max_ctx_len)))
 
 
 def k_cache_index(layout: Layout, blk, g, slot, d) -> int:
@@ -187,6 +214,30 @@ def _stream_source(c=torch._C):
 
 
 _stream = _stream_source()
+
+
+class Rope:
+    """A position rotation: inv_freq float64 [rotary_dim / 2] on the GPU (radians per position), pairs of elements "halves"
+    (i, i + rotary_dim / 2) or "adjacent" (2 i, 2 i + 1); axis[i]: which of the position coordinates turns pair i (None: one
+    coordinate).  A program makes it once and keeps it."""
+
+    def __init__(self, inv_freq: torch.Tensor, pairing: str = "halves", axis=None):
+        if inv_freq.dtype != torch.float64 or inv_freq.dim() != 1 or not inv_freq.is_contiguous():
+            raise ValueError("inv_freq must be a contiguous float64 vector")
+        pairs = inv_freq.numel()
+        axis = [0] * pairs if axis is None else [int(a) for a in axis]
+        if pairs > 128 or len(axis) != pairs or any(a < 0 or a > 3 for a in axis):
+            raise ValueError("one axis of 0 .. 3 for each of at most 128 pairs")
+        self.inv_freq = inv_freq
+        self.struct = RopeStruct(2 * pairs, {"halves": ROPE_HALVES, "adjacent": ROPE_ADJACENT}[pairing], max(axis, default=0) + 1,
+                                 (ctypes.c_uint8 * 128)(*axis))
+
+
+def _typed(t, dtype, what: str, dim=None):
+    """A call that reads or writes through an address needs to know what is there."""
+    if t.dtype != dtype or not t.is_contiguous() or (dim is not None and t.dim() != dim):
+        raise ValueError(f"{what} must be a contiguous {dtype} tensor" + (f" of {dim} dimensions" if dim is not None else ""))
+    return t
 
 
 class Context:
@@ -347,6 +398,67 @@ class Context:
         _check(_lib.ecoserve_attn_decode(self._h, _ptr(q), _ptr(k_cache), _ptr(v_cache), _ptr(block_table),
                                          block_table.shape[1], _ptr(ctx_len), _ptr(out), _ptr(lse), B,
                                          max_ctx_len, _stream()), "ecoserve_attn_decode")
+
+    # ---- rotated append, block summaries, selection, attention over listed blocks ----------
+    def kv_append_rope(self, k_cache, v_cache, k_new, v_new, cu_q, ctx_before, block_table, rope: Rope, positions=None, q=None, q_out=None, max_new_len=None):
+        """kv_append_strided with K rotated on the way, and Q (if given) rotated into q_out; positions int32 [axes, T] or None: the tokens' places."""
+        T = k_new.shape[0]
+        new_stride = _row_stride(k_new)
+        if new_stride != _row_stride(v_new):
+            raise ValueError("k_new and v_new must have the same row stride")
+        if positions is not None and _typed(positions, torch.int32, "positions", 2).shape != (rope.struct.num_axes, T):
+            raise ValueError("positions must be [axes, tokens]")
+        if (q is None) != (q_out is None) or (q is not None and not q.shape == q_out.shape == (T, self.layout.num_q_heads, self.layout.head_dim)):
+            raise ValueError("q and q_out must both be [tokens, query heads, D], or both None")
+        _check(_lib.ecoserve_kv_append_rope(self._h, ctypes.byref(rope.struct), _ptr(rope.inv_freq), _ptr(positions), _ptr(q), _row_stride(q) if q is not None else 0,
+                                            _ptr(q_out), _row_stride(q_out) if q is not None else 0, _ptr(k_cache), _ptr(v_cache), _ptr(k_new), _ptr(v_new),
+                                            new_stride, _ptr(cu_q), _ptr(ctx_before), _ptr(block_table), block_table.shape[1], ctx_before.numel(), T,
+                                            T if max_new_len is None else int(max_new_len), _stream()), "ecoserve_kv_append_rope")
+
+    def new_summary(self) -> torch.Tensor:
+        """One layer's block summaries, zeros."""
+        return torch.zeros(summary_bytes(self.layout), dtype=torch.int8, device=self.device)
+
+    def kv_summary(self, k_cache, summary, cu_q, ctx_before, block_table, T: int, max_new_len=None):
+        """Summarises the blocks that the T tokens of an append have filled."""
+        if _typed(summary, torch.int8, "summary").numel() < summary_bytes(self.layout):
+            raise ValueError("summary is too small")
+        _check(_lib.ecoserve_kv_summary(self._h, _ptr(k_cache), _ptr(summary), _ptr(cu_q), _ptr(ctx_before), _ptr(block_table), block_table.shape[1],
+                                        ctx_before.numel(), int(T), int(T) if max_new_len is None else int(max_new_len), _stream()), "ecoserve_kv_summary")
+
+    def _lists(self, q, blocks):
+        if _typed(blocks, torch.int32, "blocks", 3).shape[:2] != (q.shape[0], self.layout.num_kv_heads):
+            raise ValueError("blocks must be [tokens, K/V heads, entries]")
+        return blocks.shape[2]
+
+    def _workspace(self, workspace, need: int):
+        """The caller's workspace, or one from torch's allocator (which gives it to nobody else before this call's kernels are through)."""
+        if workspace is None and need:
+            workspace = torch.empty(need, dtype=torch.uint8, device=self.device)
+        return workspace, workspace.numel() * workspace.element_size() if workspace is not None else 0
+
+    def block_select(self, q, summary, ctx_before, block_table, blocks, max_ctx_len, keep_first=1, keep_last=1, cu_q=None, workspace=None):
+        """Each token's blocks by score into blocks int32 [T, Hkv, entries]; cu_q None: one token per sequence."""
+        entries = self._lists(q, blocks)
+        if _typed(summary, torch.int8, "summary").numel() < summary_bytes(self.layout):
+            raise ValueError("summary is too small")
+        T = q.shape[0]
+        workspace, room = self._workspace(workspace, select_workspace_bytes(self.layout, T, max_ctx_len))
+        _check(_lib.ecoserve_block_select(self._h, _ptr(q), _row_stride(q), _ptr(summary), _ptr(cu_q), _ptr(ctx_before), _ptr(block_table), block_table.shape[1],
+                                          _ptr(blocks), entries, int(keep_first), int(keep_last), ctx_before.numel(), T, int(max_ctx_len), _ptr(workspace), room,
+                                          _stream()), "ecoserve_block_select")
+
+    def sparse_workspace_bytes(self, T: int, entries: int) -> int:
+        return int(_lib.ecoserve_sparse_workspace_bytes(self._h, int(T), int(entries)))
+
+    def attn_sparse(self, q, k_cache, v_cache, ctx_before, block_table, blocks, out, lse=None, cu_q=None, workspace=None):
+        """Attention over the listed blocks; cu_q None: one token per sequence."""
+        entries = self._lists(q, blocks)
+        T = q.shape[0]
+        workspace, room = self._workspace(workspace, self.sparse_workspace_bytes(T, entries))
+        _check(_lib.ecoserve_attn_sparse(self._h, _ptr(q), _row_stride(q), _ptr(k_cache), _ptr(v_cache), _ptr(cu_q), _ptr(ctx_before), _ptr(block_table),
+                                         block_table.shape[1], _ptr(blocks), entries, _ptr(out), _ptr(lse), ctx_before.numel(), T, _ptr(workspace), room,
+                                         _stream()), "ecoserve_attn_sparse")
 
     # ---- debugging / profiling -----------------------------------------------------------
     def debug_validate(self, cu_q, ctx_total, block_table):

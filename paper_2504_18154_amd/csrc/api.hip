@@ -12,6 +12,8 @@
 #include "decode_slices.h"
 #include "prefill_shares.h"
 #include "prefill_short.h"
+#include "sparse.h"
+#include "summary.h"
 
 using namespace eco;
 
@@ -397,6 +399,130 @@ int ecoserve_kv_append_strided(ecoserve_ctx* c, void* k_cache, void* v_cache, co
   const hipError_t e = launch_kv_append(c, k_cache, v_cache, k_new, v_new, (int32_t)new_row_stride, cu_q, ctx_before,
                                         block_table, bt_stride, B, T, max_new_len, 0, s);
   return e == hipSuccess ? ECOSERVE_OK : ECOSERVE_EHIP;
+}
+
+int ecoserve_kv_append_rope(ecoserve_ctx* c, const ecoserve_rope* rope, const double* inv_freq, const int32_t* positions, const void* q, int64_t q_row_stride,
+                            void* q_out, int64_t q_out_row_stride, void* k_cache, void* v_cache, const void* k_new, const void* v_new, int64_t new_row_stride,
+                            const int32_t* cu_q, const int32_t* ctx_before, const int32_t* block_table, int32_t bt_stride, int32_t B, int32_t T,
+                            int32_t max_new_len, void* stream) {
+  if (!c || !rope || B < 0 || T < 0 || max_new_len < 0) return ECOSERVE_EINVAL;
+  const ecoserve_layout& L = c->lay;
+  const int32_t unit = L.dtype == ECOSERVE_BF16 ? 8 : 4;
+  if (rope->rotary_dim <= 0 || rope->rotary_dim > L.head_dim || rope->rotary_dim % unit != 0) return ECOSERVE_EINVAL;
+  if (rope->pairing != ECOSERVE_ROPE_HALVES && rope->pairing != ECOSERVE_ROPE_ADJACENT) return ECOSERVE_EINVAL;
+  if (rope->num_axes < 1 || rope->num_axes > ECOSERVE_ROPE_MAX_AXES || (rope->num_axes > 1 && !positions && T > 0)) return ECOSERVE_EINVAL;
+  for (int i = 0; i < rope->rotary_dim / 2; ++i)
+    if (rope->axis[i] >= rope->num_axes) return ECOSERVE_EINVAL;
+  if (!stride_ok(c, new_row_stride, L.num_kv_heads)) return ECOSERVE_EINVAL;
+  if ((q == nullptr) != (q_out == nullptr)) return ECOSERVE_EINVAL;
+  if (q && (!stride_ok(c, q_row_stride, L.num_q_heads) || !stride_ok(c, q_out_row_stride, L.num_q_heads))) return ECOSERVE_EINVAL;
+  if (B == 0 || T == 0) return ECOSERVE_OK;
+  if (!inv_freq || !k_cache || !v_cache || !k_new || !v_new || !cu_q || !ctx_before || !block_table) return ECOSERVE_EINVAL;
+  if (B > c->max_batch || bt_stride <= 0 || max_new_len > T || max_new_len == 0) return ECOSERVE_EINVAL;
+  if (!aligned16(k_cache) || !aligned16(v_cache) || !aligned16(k_new) || !aligned16(v_new) || !aligned16(q) || !aligned16(q_out)) return ECOSERVE_EINVAL;
+  if ((reinterpret_cast<uintptr_t>(inv_freq) & 7u) || (reinterpret_cast<uintptr_t>(positions) & 3u)) return ECOSERVE_EINVAL;
+  DeviceGuard guard(c->device);
+  if (!guard.ok) return ECOSERVE_EHIP;
+  hipStream_t s = (hipStream_t)stream;
+  RopeAppend a;
+  a.q = q;
+  a.q_row_stride = (int32_t)q_row_stride;
+  a.q_out = q_out;
+  a.q_out_row_stride = (int32_t)q_out_row_stride;
+  a.k_cache = k_cache;
+  a.v_cache = v_cache;
+  a.k_new = k_new;
+  a.v_new = v_new;
+  a.new_row_stride = (int32_t)new_row_stride;
+  a.cu_q = cu_q;
+  a.ctx_before = ctx_before;
+  a.block_table = block_table;
+  a.bt_stride = bt_stride;
+  a.B = B;
+  a.T = T;
+  a.max_new_len = max_new_len;
+  a.Hq = L.num_q_heads;
+  a.Hkv = L.num_kv_heads;
+  a.D = L.head_dim;
+  a.dtype = L.dtype;
+  ProfileScope prof(c, ECOSERVE_KERNEL_APPEND, s);
+  return launch_kv_append_rope(a, *rope, inv_freq, positions, c->num_cu, s) == hipSuccess ? ECOSERVE_OK : ECOSERVE_EHIP;
+}
+
+size_t ecoserve_summary_bytes(const ecoserve_layout* L) {
+  int st;
+  if (!layout_ok(L, &st)) return 0;
+  return (summary_code_bytes(*L) + (size_t)L->num_blocks * L->num_kv_heads + 15) / 16 * 16;
+}
+
+int ecoserve_kv_summary(ecoserve_ctx* c, const void* k_cache, void* summary, const int32_t* cu_q, const int32_t* ctx_before, const int32_t* block_table,
+                        int32_t bt_stride, int32_t B, int32_t T, int32_t max_new_len, void* stream) {
+  if (!c || B < 0 || T < 0 || max_new_len < 0) return ECOSERVE_EINVAL;
+  if (B == 0 || T == 0) return ECOSERVE_OK;
+  if (!k_cache || !summary || !cu_q || !ctx_before || !block_table) return ECOSERVE_EINVAL;
+  if (B > c->max_batch || bt_stride <= 0 || max_new_len > T || max_new_len == 0) return ECOSERVE_EINVAL;
+  if (!aligned16(k_cache) || !aligned16(summary)) return ECOSERVE_EINVAL;
+  DeviceGuard guard(c->device);
+  if (!guard.ok) return ECOSERVE_EHIP;
+  const hipError_t e = launch_kv_summary(c->lay, k_cache, summary, cu_q, ctx_before, block_table, bt_stride, B, T, (hipStream_t)stream);
+  return e == hipSuccess ? ECOSERVE_OK : ECOSERVE_EHIP;
+}
+
+// What both calls on listed blocks ask of their tokens and lists.
+static bool lists_ok(const ecoserve_ctx* c, const int32_t* cu_q, const int32_t* ctx_before, const int32_t* block_table, int32_t bt_stride,
+                     const int32_t* blocks, int32_t num_selected, int32_t B, int32_t T) {
+  return ctx_before && block_table && blocks && bt_stride > 0 && B <= c->max_batch && (cu_q || T == B) && num_selected >= 1 && num_selected <= 65536 &&
+         (reinterpret_cast<uintptr_t>(blocks) & 3u) == 0;
+}
+
+size_t ecoserve_select_workspace_bytes(const ecoserve_layout* L, int32_t T, int32_t max_ctx_len) {
+  int st;
+  if (!layout_ok(L, &st) || T <= 0 || max_ctx_len <= 0) return 0;
+  return select_workspace_bytes(L->num_kv_heads, T, max_ctx_len);
+}
+
+int ecoserve_block_select(ecoserve_ctx* c, const void* q, int64_t q_row_stride, const void* summary, const int32_t* cu_q, const int32_t* ctx_before,
+                          const int32_t* block_table, int32_t bt_stride, int32_t* blocks, int32_t num_selected, int32_t keep_first, int32_t keep_last,
+                          int32_t B, int32_t T, int32_t max_ctx_len, void* workspace, size_t workspace_bytes, void* stream) {
+  if (!c || B < 0 || T < 0 || max_ctx_len < 0) return ECOSERVE_EINVAL;
+  const ecoserve_layout& L = c->lay;
+  if (!stride_ok(c, q_row_stride, L.num_q_heads)) return ECOSERVE_EINVAL;
+  if (keep_first < 0 || keep_last < 1 || (int64_t)keep_first + keep_last > num_selected) return ECOSERVE_EINVAL;
+  if (B == 0 || T == 0) return ECOSERVE_OK;
+  if (!q || !summary || !workspace || !lists_ok(c, cu_q, ctx_before, block_table, bt_stride, blocks, num_selected, B, T)) return ECOSERVE_EINVAL;
+  if (max_ctx_len < 1 || (int64_t)max_ctx_len > (int64_t)c->max_blocks_per_seq * kBlockSize || (int64_t)max_ctx_len > (int64_t)bt_stride * kBlockSize)
+    return ECOSERVE_EINVAL;
+  if (!aligned16(q) || !aligned16(summary) || !aligned16(workspace)) return ECOSERVE_EINVAL;
+  if (workspace_bytes < select_workspace_bytes(L.num_kv_heads, T, max_ctx_len)) return ECOSERVE_EINVAL;
+  DeviceGuard guard(c->device);
+  if (!guard.ok) return ECOSERVE_EHIP;
+  const SelectArgs a = {q, (int32_t)q_row_stride, cu_q, ctx_before, block_table, bt_stride, blocks, num_selected, keep_first, keep_last, B, T,
+                        L.num_q_heads, L.num_kv_heads, L.head_dim, c->num_cu, (uint32_t*)workspace};
+  return launch_block_select(L, a, summary, max_ctx_len, (hipStream_t)stream) == hipSuccess ? ECOSERVE_OK : ECOSERVE_EHIP;
+}
+
+size_t ecoserve_sparse_workspace_bytes(const ecoserve_ctx* c, int32_t T, int32_t num_selected) {
+  if (!c || T <= 0 || num_selected <= 0) return 0;
+  return sparse_workspace_bytes(c->lay.num_q_heads, c->lay.num_kv_heads, c->lay.head_dim, T, num_selected, c->num_cu);
+}
+
+int ecoserve_attn_sparse(ecoserve_ctx* c, const void* q, int64_t q_row_stride, const void* k_cache, const void* v_cache, const int32_t* cu_q,
+                         const int32_t* ctx_before, const int32_t* block_table, int32_t bt_stride, const int32_t* blocks, int32_t num_selected, void* out,
+                         float* lse, int32_t B, int32_t T, void* workspace, size_t workspace_bytes, void* stream) {
+  if (!c || B < 0 || T < 0) return ECOSERVE_EINVAL;
+  const ecoserve_layout& L = c->lay;
+  if (!stride_ok(c, q_row_stride, L.num_q_heads)) return ECOSERVE_EINVAL;
+  if (B == 0 || T == 0) return ECOSERVE_OK;
+  if (!q || !k_cache || !v_cache || !out || !lists_ok(c, cu_q, ctx_before, block_table, bt_stride, blocks, num_selected, B, T)) return ECOSERVE_EINVAL;
+  if (!aligned16(q) || !aligned16(k_cache) || !aligned16(v_cache) || !aligned16(out) || !aligned16(workspace)) return ECOSERVE_EINVAL;
+  if (lse && (reinterpret_cast<uintptr_t>(lse) & 3u)) return ECOSERVE_EINVAL;
+  const size_t needed = sparse_workspace_bytes(L.num_q_heads, L.num_kv_heads, L.head_dim, T, num_selected, c->num_cu);
+  if (needed > 0 && (!workspace || workspace_bytes < needed)) return ECOSERVE_EINVAL;
+  DeviceGuard guard(c->device);
+  if (!guard.ok) return ECOSERVE_EHIP;
+  const SparseArgs a = {q, (int32_t)q_row_stride, k_cache, v_cache, cu_q, ctx_before, block_table, bt_stride, blocks, num_selected, out, lse, B, T,
+                        L.num_q_heads, L.num_kv_heads, L.head_dim, c->num_cu, L.dtype, c->scale * kLog2e, (float*)workspace};
+  return launch_attn_sparse(a, (hipStream_t)stream) == hipSuccess ? ECOSERVE_OK : ECOSERVE_EHIP;
 }
 
 static AttnArgs make_args(const ecoserve_ctx* c, const void* q, int64_t q_row_stride, const void* k_cache, const void* v_cache,

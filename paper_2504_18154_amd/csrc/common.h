@@ -162,6 +162,30 @@ hipError_t launch_kv_append(const ecoserve_ctx* ctx, void* k_cache, void* v_cach
                             const int32_t* block_table, int32_t bt_stride, int32_t B, int32_t T,
                             int32_t max_new_len, int32_t pos_bias, hipStream_t s);
 
+// kv_rope.hip: the append with the position rotation on the way
+struct RopeAppend {
+  const void* q;  // NULL: K and V alone
+  int32_t q_row_stride;
+  void* q_out;
+  int32_t q_out_row_stride;
+  void *k_cache, *v_cache;
+  const void *k_new, *v_new;
+  int32_t new_row_stride;
+  const int32_t *cu_q, *ctx_before, *block_table;
+  int32_t bt_stride, B, T, max_new_len, Hq, Hkv, D, dtype;
+};
+hipError_t launch_kv_append_rope(const RopeAppend& a, const ecoserve_rope& rope, const double* inv_freq, const int32_t* positions, int num_cu, hipStream_t s);
+
+// kv_summary.hip
+hipError_t launch_kv_summary(const ecoserve_layout& L, const void* k_cache, void* summary, const int32_t* cu_q, const int32_t* ctx_before,
+                             const int32_t* block_table, int32_t bt_stride, int32_t B, int32_t T, hipStream_t s);
+
+// block_select.hip, attn_sparse.hip (sparse.h has their arguments and workspaces)
+struct SelectArgs;
+struct SparseArgs;
+hipError_t launch_block_select(const ecoserve_layout& L, const SelectArgs& a, const void* summary, int32_t max_ctx_len, hipStream_t s);
+hipError_t launch_attn_sparse(const SparseArgs& a, hipStream_t s);
+
 // attn_plain.hip: any head size / dtype, no matrix cores
 hipError_t launch_prefill_plain(const AttnArgs& a, const int32_t* cu_q, const int32_t* ctx_before, int32_t T,
                                 hipStream_t s);

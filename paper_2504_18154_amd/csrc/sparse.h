@@ -1,0 +1,61 @@
+// Workspaces and argument blocks of block selection and of attention over listed blocks.  The sizes are plain arithmetic, for the
+// launches, the entry points and a host program alike.
+#pragma once
+
+#include <stddef.h>
+#include <stdint.h>
+
+#include <algorithm>
+
+namespace eco {
+
+// Selection: one 32-bit number per (token, K/V head, block), rows of whole tiles of 16 blocks.
+inline int64_t select_row_words(int32_t max_ctx_len) { return ((int64_t)max_ctx_len + 255) / 256 * 16; }
+// Tokens whose scores are held at a time: as many as 192 MiB take, which stays in the last-level cache (256 MiB) between the two launches.
+inline int32_t select_tokens_at_a_time(int32_t Hkv, int32_t T, int32_t max_ctx_len) {
+  const int64_t row_bytes = 4 * select_row_words(max_ctx_len) * Hkv;
+  return (int32_t)std::max<int64_t>(1, std::min<int64_t>({(int64_t)T, ((int64_t)192 << 20) / row_bytes, 32768}));
+}
+inline size_t select_workspace_bytes(int32_t Hkv, int32_t T, int32_t max_ctx_len) {
+  return (size_t)select_tokens_at_a_time(Hkv, T, max_ctx_len) * Hkv * select_row_words(max_ctx_len) * 4;
+}
+
+struct SelectArgs {
+  const void* q;
+  int32_t q_row_stride;
+  const int32_t *cu_q, *ctx_before, *block_table;
+  int32_t bt_stride;
+  int32_t* blocks;
+  int32_t num_selected, keep_first, keep_last, B, T, Hq, Hkv, D, num_cu;
+  uint32_t* scores;
+};
+
+// Attention over listed blocks: a list is cut into parts, one workgroup each, where there are few (token, K/V head)s.  Two
+// workgroups per CU are wanted, and a part has at least eight blocks: two per wavefront.
+inline int32_t sparse_parts(int32_t Hkv, int32_t T, int32_t num_selected, int32_t num_cu) {
+  const int64_t rows = (int64_t)T * Hkv;
+  return (int32_t)std::max<int64_t>(1, std::min<int64_t>({2 * (int64_t)num_cu / rows, (num_selected + 7) / 8, 64}));
+}
+// Floats of a part's state of one query head: the unnormalised head vector, its maximum and its sum, and two that keep 16 bytes aligned.
+constexpr int32_t sparse_state_words(int32_t D) { return D + 4; }
+inline size_t sparse_workspace_bytes(int32_t Hq, int32_t Hkv, int32_t D, int32_t T, int32_t num_selected, int32_t num_cu) {
+  const int32_t parts = sparse_parts(Hkv, T, num_selected, num_cu);
+  return parts == 1 ? 0 : (size_t)parts * T * Hq * sparse_state_words(D) * 4;
+}
+
+struct SparseArgs {
+  const void* q;
+  int32_t q_row_stride;
+  const void *k_cache, *v_cache;
+  const int32_t *cu_q, *ctx_before, *block_table;
+  int32_t bt_stride;
+  const int32_t* blocks;
+  int32_t num_selected;
+  void* out;
+  float* lse;
+  int32_t B, T, Hq, Hkv, D, num_cu, dtype;
+  float scale_log2e;
+  float* states;
+};
+
+}  // namespace eco

@@ -114,6 +114,11 @@ _fast.bind(*(ctypes.cast(f, ctypes.c_void_p).value for f in (_lib.ecoserve_kv_ap
                                                              _lib.ecoserve_attn_decode_noalloc)))
 
 
+_fast.bind_sparse(*(ctypes.cast(f, ctypes.c_void_p).value for f in (_lib.ecoserve_kv_append_rope, _lib.ecoserve_kv_summary,
+                                                                    _lib.ecoserve_select_workspace_bytes, _lib.ecoserve_block_select,
+                                                                    _lib.ecoserve_sparse_workspace_bytes, _lib.ecoserve_attn_sparse)))
+
+
 def strerror(status: int) -> str:
     return _lib.ecoserve_strerror(int(status)).decode()
 
@@ -231,13 +236,7 @@ class Rope:
         self.inv_freq = inv_freq
         self.struct = RopeStruct(2 * pairs, {"halves": ROPE_HALVES, "adjacent": ROPE_ADJACENT}[pairing], max(axis, default=0) + 1,
                                  (ctypes.c_uint8 * 128)(*axis))
-
-
-def _typed(t, dtype, what: str, dim=None):
-    """A call that reads or writes through an address needs to know what is there."""
-    if t.dtype != dtype or not t.is_contiguous() or (dim is not None and t.dim() != dim):
-        raise ValueError(f"{what} must be a contiguous {dtype} tensor" + (f" of {dim} dimensions" if dim is not None else ""))
-    return t
+        self._address = ctypes.addressof(self.struct)
 
 
 class Context:
@@ -247,11 +246,12 @@ class Context:
                  softmax_scale=0.0):
         self.layout = make_layout(Hq, Hkv, D, num_blocks, dtype, bs, softmax_scale)
         self.torch_dtype = torch.bfloat16 if self.layout.dtype == BF16 else torch.float32
-        self.device = torch.device("cuda", device)
+        self.device, self._device_index = torch.device("cuda", device), int(device)
         self._h = ctypes.c_void_p()
         _check(_lib.ecoserve_create(ctypes.byref(self._h), int(device), ctypes.byref(self.layout), int(max_batch),
                                     int(max_blocks_per_seq)), "ecoserve_create")
         self._address = self._h.value
+        self._layout_address = ctypes.addressof(self.layout)
         self._q_row, self._kv_row = self.layout.num_q_heads * self.layout.head_dim, self.layout.num_kv_heads * self.layout.head_dim
 
     def close(self):
@@ -400,65 +400,118 @@ class Context:
                                          max_ctx_len, _stream()), "ecoserve_attn_decode")
 
     # ---- rotated append, block summaries, selection, attention over listed blocks ----------
+    # These look at what they are given: _bind takes tensors of the context's GPU and of the types and sizes that the call reads and
+    # writes; anything else comes to the lines behind it, which say what is wrong, or make plain integers of bounds that are none.
+    def _same(self, t, what, dtype, least=0):
+        if not (torch.is_tensor(t) and t.device == self.device and t.dtype == dtype and t.is_contiguous() and t.numel() >= least):
+            raise ValueError(f"{what} must be a contiguous {dtype} tensor on {self.device}, of {least} elements at least")
+        return t.data_ptr()
+
+    def _rows(self, t, what, T, heads):
+        if not (torch.is_tensor(t) and t.device == self.device and t.dtype == self.torch_dtype and tuple(t.shape) == (T, heads, self.layout.head_dim)):
+            raise ValueError(f"{what} must be a {self.torch_dtype} tensor [{T}, {heads}, {self.layout.head_dim}] on {self.device}")
+        return t.data_ptr(), _row_stride(t)
+
+    def _pool(self, t, what):
+        L = self.layout
+        return self._same(t, what, self.torch_dtype, L.num_blocks * L.num_kv_heads * L.block_size * L.head_dim)
+
+    def _batch(self, cu_q, ctx_before, block_table):
+        """(cu_q, ctx_before, block table, its width, sequences)"""
+        before = self._same(ctx_before, "ctx_before", torch.int32)
+        B = ctx_before.numel()
+        if not torch.is_tensor(block_table) or block_table.dim() != 2 or block_table.shape[0] < B:
+            raise ValueError("block_table must be [sequences, blocks]")
+        return (self._same(cu_q, "cu_q", torch.int32, B + 1) if cu_q is not None else None, before, self._same(block_table, "block_table", torch.int32),
+                block_table.shape[1], B)
+
+    def _lists(self, blocks, T):
+        if not torch.is_tensor(blocks) or blocks.dim() != 3 or tuple(blocks.shape[:2]) != (T, self.layout.num_kv_heads):
+            raise ValueError("blocks must be [tokens, K/V heads, entries]")
+        return self._same(blocks, "blocks", torch.int32), blocks.shape[2]
+
+    def _workspace(self, workspace, need: int):
+        """The caller's workspace, or one of torch's allocator (which gives it to nobody else on this stream before the call's kernels are through)."""
+        if workspace is None:
+            workspace = torch.empty(need, dtype=torch.uint8, device=self.device)
+        return self._same(workspace, "workspace", workspace.dtype), workspace.numel() * workspace.element_size(), workspace
+
+    def _stream_here(self):
+        return torch.cuda.current_stream(self.device).cuda_stream
+
     def kv_append_rope(self, k_cache, v_cache, k_new, v_new, cu_q, ctx_before, block_table, rope: Rope, positions=None, q=None, q_out=None, max_new_len=None):
         """kv_append_strided with K rotated on the way, and Q (if given) rotated into q_out; positions int32 [axes, T] or None: the tokens' places."""
-        T = k_new.shape[0]
-        new_stride = _row_stride(k_new)
-        if new_stride != _row_stride(v_new):
+        status = _fast.kv_append_rope(self._address, self._layout_address, self._device_index, rope._address, rope.inv_freq, k_cache, v_cache, k_new, v_new, cu_q,
+                                      ctx_before, block_table, positions, q, q_out, max_new_len)
+        if status >= 0:
+            return _check(status, "ecoserve_kv_append_rope")
+        T, L, r = k_new.shape[0], self.layout, rope.struct
+        kn, new_stride = self._rows(k_new, "k_new", T, L.num_kv_heads)
+        vn, v_stride = self._rows(v_new, "v_new", T, L.num_kv_heads)
+        if new_stride != v_stride:
             raise ValueError("k_new and v_new must have the same row stride")
-        if positions is not None and _typed(positions, torch.int32, "positions", 2).shape != (rope.struct.num_axes, T):
+        freq = self._same(rope.inv_freq, "inv_freq", torch.float64, r.rotary_dim // 2)
+        if positions is not None and not (torch.is_tensor(positions) and tuple(positions.shape) == (r.num_axes, T)):
             raise ValueError("positions must be [axes, tokens]")
-        if (q is None) != (q_out is None) or (q is not None and not q.shape == q_out.shape == (T, self.layout.num_q_heads, self.layout.head_dim)):
-            raise ValueError("q and q_out must both be [tokens, query heads, D], or both None")
-        _check(_lib.ecoserve_kv_append_rope(self._h, ctypes.byref(rope.struct), _ptr(rope.inv_freq), _ptr(positions), _ptr(q), _row_stride(q) if q is not None else 0,
-                                            _ptr(q_out), _row_stride(q_out) if q is not None else 0, _ptr(k_cache), _ptr(v_cache), _ptr(k_new), _ptr(v_new),
-                                            new_stride, _ptr(cu_q), _ptr(ctx_before), _ptr(block_table), block_table.shape[1], ctx_before.numel(), T,
-                                            T if max_new_len is None else int(max_new_len), _stream()), "ecoserve_kv_append_rope")
+        if (q is None) != (q_out is None):
+            raise ValueError("q and q_out go together")
+        q_at, q_stride = self._rows(q, "q", T, L.num_q_heads) if q is not None else (None, 0)
+        out_at, out_stride = self._rows(q_out, "q_out", T, L.num_q_heads) if q is not None else (None, 0)
+        cu, before, table, width, B = self._batch(cu_q, ctx_before, block_table)
+        _check(_lib.ecoserve_kv_append_rope(self._h, ctypes.byref(r), freq, self._same(positions, "positions", torch.int32) if positions is not None else None,
+                                            q_at, q_stride, out_at, out_stride, self._pool(k_cache, "k_cache"), self._pool(v_cache, "v_cache"), kn, vn,
+                                            new_stride, cu, before, table, width, B, T, T if max_new_len is None else int(max_new_len), self._stream_here()),
+               "ecoserve_kv_append_rope")
 
     def new_summary(self) -> torch.Tensor:
         """One layer's block summaries, zeros."""
         return torch.zeros(summary_bytes(self.layout), dtype=torch.int8, device=self.device)
 
+    def _summary(self, summary):
+        L = self.layout
+        return self._same(summary, "summary", torch.int8, L.num_blocks * L.num_kv_heads * (2 * ((L.head_dim + 31) // 32 * 32) + 1))
+
     def kv_summary(self, k_cache, summary, cu_q, ctx_before, block_table, T: int, max_new_len=None):
         """Summarises the blocks that the T tokens of an append have filled."""
-        if _typed(summary, torch.int8, "summary").numel() < summary_bytes(self.layout):
-            raise ValueError("summary is too small")
-        _check(_lib.ecoserve_kv_summary(self._h, _ptr(k_cache), _ptr(summary), _ptr(cu_q), _ptr(ctx_before), _ptr(block_table), block_table.shape[1],
-                                        ctx_before.numel(), int(T), int(T) if max_new_len is None else int(max_new_len), _stream()), "ecoserve_kv_summary")
-
-    def _lists(self, q, blocks):
-        if _typed(blocks, torch.int32, "blocks", 3).shape[:2] != (q.shape[0], self.layout.num_kv_heads):
-            raise ValueError("blocks must be [tokens, K/V heads, entries]")
-        return blocks.shape[2]
-
-    def _workspace(self, workspace, need: int):
-        """The caller's workspace, or one from torch's allocator (which gives it to nobody else before this call's kernels are through)."""
-        if workspace is None and need:
-            workspace = torch.empty(need, dtype=torch.uint8, device=self.device)
-        return workspace, workspace.numel() * workspace.element_size() if workspace is not None else 0
+        status = _fast.kv_summary(self._address, self._layout_address, self._device_index, k_cache, summary, cu_q, ctx_before, block_table, T, max_new_len)
+        if status >= 0:
+            return _check(status, "ecoserve_kv_summary")
+        cu, before, table, width, B = self._batch(cu_q, ctx_before, block_table)
+        _check(_lib.ecoserve_kv_summary(self._h, self._pool(k_cache, "k_cache"), self._summary(summary), cu, before, table, width, B, int(T),
+                                        int(T) if max_new_len is None else int(max_new_len), self._stream_here()), "ecoserve_kv_summary")
 
     def block_select(self, q, summary, ctx_before, block_table, blocks, max_ctx_len, keep_first=1, keep_last=1, cu_q=None, workspace=None):
         """Each token's blocks by score into blocks int32 [T, Hkv, entries]; cu_q None: one token per sequence."""
-        entries = self._lists(q, blocks)
-        if _typed(summary, torch.int8, "summary").numel() < summary_bytes(self.layout):
-            raise ValueError("summary is too small")
+        status = _fast.block_select(self._address, self._layout_address, self._device_index, q, summary, ctx_before, block_table, blocks, max_ctx_len, keep_first,
+                                    keep_last, cu_q, workspace)
+        if status >= 0:
+            return _check(status, "ecoserve_block_select")
         T = q.shape[0]
-        workspace, room = self._workspace(workspace, select_workspace_bytes(self.layout, T, max_ctx_len))
-        _check(_lib.ecoserve_block_select(self._h, _ptr(q), _row_stride(q), _ptr(summary), _ptr(cu_q), _ptr(ctx_before), _ptr(block_table), block_table.shape[1],
-                                          _ptr(blocks), entries, int(keep_first), int(keep_last), ctx_before.numel(), T, int(max_ctx_len), _ptr(workspace), room,
-                                          _stream()), "ecoserve_block_select")
+        q_at, q_stride = self._rows(q, "q", T, self.layout.num_q_heads)
+        cu, before, table, width, B = self._batch(cu_q, ctx_before, block_table)
+        lists, entries = self._lists(blocks, T)
+        at, room, _held = self._workspace(workspace, select_workspace_bytes(self.layout, T, max_ctx_len))
+        _check(_lib.ecoserve_block_select(self._h, q_at, q_stride, self._summary(summary), cu, before, table, width, lists, entries, int(keep_first), int(keep_last),
+                                          B, T, int(max_ctx_len), at, room, self._stream_here()), "ecoserve_block_select")
 
     def sparse_workspace_bytes(self, T: int, entries: int) -> int:
         return int(_lib.ecoserve_sparse_workspace_bytes(self._h, int(T), int(entries)))
 
     def attn_sparse(self, q, k_cache, v_cache, ctx_before, block_table, blocks, out, lse=None, cu_q=None, workspace=None):
         """Attention over the listed blocks; cu_q None: one token per sequence."""
-        entries = self._lists(q, blocks)
-        T = q.shape[0]
-        workspace, room = self._workspace(workspace, self.sparse_workspace_bytes(T, entries))
-        _check(_lib.ecoserve_attn_sparse(self._h, _ptr(q), _row_stride(q), _ptr(k_cache), _ptr(v_cache), _ptr(cu_q), _ptr(ctx_before), _ptr(block_table),
-                                         block_table.shape[1], _ptr(blocks), entries, _ptr(out), _ptr(lse), ctx_before.numel(), T, _ptr(workspace), room,
-                                         _stream()), "ecoserve_attn_sparse")
+        status = _fast.attn_sparse(self._address, self._layout_address, self._device_index, q, k_cache, v_cache, ctx_before, block_table, blocks, out, lse, cu_q,
+                                   workspace)
+        if status >= 0:
+            return _check(status, "ecoserve_attn_sparse")
+        T, L = q.shape[0], self.layout
+        q_at, q_stride = self._rows(q, "q", T, L.num_q_heads)
+        cu, before, table, width, B = self._batch(cu_q, ctx_before, block_table)
+        lists, entries = self._lists(blocks, T)
+        at, room, _held = self._workspace(workspace, self.sparse_workspace_bytes(T, entries))
+        _check(_lib.ecoserve_attn_sparse(self._h, q_at, q_stride, self._pool(k_cache, "k_cache"), self._pool(v_cache, "v_cache"), cu, before, table, width, lists,
+                                         entries, self._same(out, "out", self.torch_dtype, T * self._q_row),
+                                         self._same(lse, "lse", torch.float32, T * L.num_q_heads) if lse is not None else None, B, T, at, room, self._stream_here()),
+               "ecoserve_attn_sparse")
 
     # ---- debugging / profiling -----------------------------------------------------------
     def debug_validate(self, cu_q, ctx_total, block_table):

@@ -10,6 +10,7 @@
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 
+#include <ATen/ops/empty.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -28,6 +29,14 @@ struct Entries {
   decltype(&ecoserve_attn_decode_append) decode_append;
   decltype(&ecoserve_attn_decode_noalloc) noalloc;
 } entry;
+struct SparseEntries {
+  decltype(&ecoserve_kv_append_rope) rope;
+  decltype(&ecoserve_kv_summary) summary;
+  decltype(&ecoserve_select_workspace_bytes) select_bytes;
+  decltype(&ecoserve_block_select) select;
+  decltype(&ecoserve_sparse_workspace_bytes) sparse_bytes;
+  decltype(&ecoserve_attn_sparse) sparse;
+} more;
 
 // Reads the arguments of a call.  What is binding.py's business is noted, and not thrown: an exception takes 2.5 us, half of what the
 // other way takes for such a call.
@@ -173,6 +182,172 @@ PyObject* attn_decode_noalloc(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+// The calls below look at what they are given (binding.py raises for what is not taken): tensors of the context's GPU, of its types and
+// sizes.  `l`: the context's layout, `device` its GPU.
+struct LayerArguments : Arguments {
+  const ecoserve_layout* l;
+  int device;
+  const at::Tensor* here(int i, at::ScalarType type) {
+    const at::Tensor* const t = tensor(i);
+    if (t && t->is_cuda() && t->get_device() == device && t->scalar_type() == type) return t;
+    taken = false;
+    return nullptr;
+  }
+  at::ScalarType element() const { return l->dtype == ECOSERVE_BF16 ? at::kBFloat16 : at::kFloat; }
+  // [tokens, heads, D], heads contiguous: address, and the distance of the tokens
+  struct Rows {
+    void* at = nullptr;
+    int64_t stride = 0;
+  };
+  Rows rows(int i, int64_t tokens, int32_t heads) {
+    const at::Tensor* const t = here(i, element());
+    if (!t || t->dim() != 3 || t->size(0) != tokens || t->size(1) != heads || t->size(2) != l->head_dim) return taken = false, Rows();
+    return {t->data_ptr(), row_stride(i)};
+  }
+  // contiguous and at least so long
+  void* whole(int i, at::ScalarType type, int64_t least) {
+    const at::Tensor* const t = here(i, type);
+    if (!t || !t->is_contiguous() || t->numel() < least) return taken = false, nullptr;
+    return t->data_ptr();
+  }
+  const int32_t* ints(int i, int64_t least) { return static_cast<const int32_t*>(whole(i, at::kInt, least)); }
+  const int32_t* table(int i, int64_t sequences) {
+    const at::Tensor* const t = here(i, at::kInt);
+    if (!t || t->dim() != 2 || t->size(0) < sequences) taken = false;
+    return ints(i, 0);
+  }
+  int64_t side(int sides) const { return (int64_t)l->num_blocks * l->num_kv_heads * sides; }
+  void* pool(int i) { return whole(i, element(), side(16) * l->head_dim); }
+  void* summaries(int i) { return whole(i, at::kChar, side(2 * ((l->head_dim + 31) / 32 * 32) + 1)); }
+  // [tokens, K/V heads, entries]
+  int32_t* lists(int i, int64_t tokens, int32_t& entries) {
+    const at::Tensor* const t = here(i, at::kInt);
+    if (!t || t->dim() != 3 || t->size(0) != tokens || t->size(1) != l->num_kv_heads || !t->is_contiguous()) return taken = false, nullptr;
+    entries = narrow(t->size(2));
+    return static_cast<int32_t*>(t->data_ptr());
+  }
+  // the caller's workspace, or one of torch's allocator, which gives it to nobody else on this stream before the call's kernels are through
+  struct Space {
+    void* at;
+    size_t bytes;
+    at::Tensor held;
+  };
+  Space space(int i, size_t need) {
+    if (a[i] == Py_None) {
+      if (!need || !taken) return {nullptr, 0, {}};
+      at::Tensor t = at::empty({(int64_t)need}, at::TensorOptions().dtype(at::kByte).device(at::kCUDA, device));
+      return {t.data_ptr(), need, t};
+    }
+    const at::Tensor* const t = tensor(i);
+    if (!t || !t->is_cuda() || t->get_device() != device || !t->is_contiguous()) return taken = false, Space{nullptr, 0, {}};
+    return {t->data_ptr(), (size_t)t->nbytes(), {}};
+  }
+  template <typename F>
+  int call(F f) {
+    if (!taken) return -1;
+    void* const s = c10::hip::getCurrentHIPStream((c10::DeviceIndex)device).stream();
+    struct Unlocked {
+      PyThreadState* const state = PyEval_SaveThread();
+      ~Unlocked() { PyEval_RestoreThread(state); }
+    } scope;
+    return f(s);
+  }
+};
+template <typename F>
+PyObject* guarded_layer(PyObject* const* a, Py_ssize_t n, Py_ssize_t want, F f) {
+  return guarded(a, n, want, [&](Arguments& plain) {
+    LayerArguments in{plain};
+    auto* const c = static_cast<ecoserve_ctx*>(in.handle(0));
+    in.l = static_cast<const ecoserve_layout*>(in.handle(1));
+    in.device = in.narrow_integer(2);
+    return in.taken && in.l ? f(in, c) : -1;
+  });
+}
+
+// (handle, address of the layout, device, address of the rope, inv_freq, k_cache, v_cache, k_new, v_new, cu_q, ctx_before, block_table, positions, q, q_out, max_new_len)
+PyObject* kv_append_rope(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded_layer(a, n, 16, [](LayerArguments& in, ecoserve_ctx* c) {
+    const auto* const rope = static_cast<const ecoserve_rope*>(in.handle(3));
+    if (!in.taken || !rope) return -1;
+    const int32_t T = in.size(7, 0), B = in.numel(10), width = in.size(11, 1), most = in.or_all(15, T);
+    const auto* const freq = static_cast<const double*>(in.whole(4, at::kDouble, rope->rotary_dim / 2));
+    void *const kc = in.pool(5), *const vc = in.pool(6);
+    const auto kn = in.rows(7, T, in.l->num_kv_heads), vn = in.rows(8, T, in.l->num_kv_heads);
+    if (kn.stride != vn.stride) in.taken = false;
+    const int32_t *const cu = in.ints(9, (int64_t)B + 1), *const before = in.ints(10, B), *const table = in.table(11, B);
+    const int32_t* positions = nullptr;
+    if (in.a[12] != Py_None) {
+      positions = in.ints(12, (int64_t)rope->num_axes * T);
+      if (in.size(12, 0) != rope->num_axes || in.size(12, 1) != T) in.taken = false;
+    }
+    LayerArguments::Rows q, qo;
+    if ((in.a[13] == Py_None) != (in.a[14] == Py_None)) in.taken = false;
+    if (in.taken && in.a[13] != Py_None) q = in.rows(13, T, in.l->num_q_heads), qo = in.rows(14, T, in.l->num_q_heads);
+    return in.call([&](void* s) { return more.rope(c, rope, freq, positions, q.at, q.stride, qo.at, qo.stride, kc, vc, kn.at, vn.at, kn.stride, cu, before, table, width, B, T, most, s); });
+  });
+}
+
+// (handle, address of the layout, device, k_cache, summary, cu_q, ctx_before, block_table, T, max_new_len)
+PyObject* kv_summary(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded_layer(a, n, 10, [](LayerArguments& in, ecoserve_ctx* c) {
+    void *const kc = in.pool(3), *const summary = in.summaries(4);
+    const int32_t B = in.numel(6), width = in.size(7, 1), T = in.narrow_integer(8), most = in.or_all(9, T);
+    const int32_t *const cu = in.ints(5, (int64_t)B + 1), *const before = in.ints(6, B), *const table = in.table(7, B);
+    return in.call([&](void* s) { return more.summary(c, kc, summary, cu, before, table, width, B, T, most, s); });
+  });
+}
+
+// (handle, address of the layout, device, q, summary, ctx_before, block_table, blocks, max_ctx_len, keep_first, keep_last, cu_q, workspace)
+PyObject* block_select(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded_layer(a, n, 13, [](LayerArguments& in, ecoserve_ctx* c) {
+    const int32_t T = in.size(3, 0), B = in.numel(5), width = in.size(6, 1), most = in.narrow_integer(8), first = in.narrow_integer(9), last = in.narrow_integer(10);
+    const auto q = in.rows(3, T, in.l->num_q_heads);
+    const void* const summary = in.summaries(4);
+    const int32_t *const before = in.ints(5, B), *const table = in.table(6, B), *const cu = in.a[11] == Py_None ? nullptr : in.ints(11, (int64_t)B + 1);
+    int32_t entries = 0;
+    int32_t* const lists = in.lists(7, T, entries);
+    const auto ws = in.space(12, in.taken ? more.select_bytes(in.l, T, most) : 0);
+    return in.call([&](void* s) { return more.select(c, q.at, q.stride, summary, cu, before, table, width, lists, entries, first, last, B, T, most, ws.at, ws.bytes, s); });
+  });
+}
+
+// (handle, address of the layout, device, q, k_cache, v_cache, ctx_before, block_table, blocks, out, lse, cu_q, workspace)
+PyObject* attn_sparse(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded_layer(a, n, 13, [](LayerArguments& in, ecoserve_ctx* c) {
+    const int32_t T = in.size(3, 0), B = in.numel(6), width = in.size(7, 1);
+    const auto q = in.rows(3, T, in.l->num_q_heads);
+    void *const kc = in.pool(4), *const vc = in.pool(5);
+    const int32_t *const before = in.ints(6, B), *const table = in.table(7, B), *const cu = in.a[11] == Py_None ? nullptr : in.ints(11, (int64_t)B + 1);
+    int32_t entries = 0;
+    const int32_t* const lists = in.lists(8, T, entries);
+    const int64_t heads = (int64_t)T * in.l->num_q_heads;
+    void* const out = in.whole(9, in.element(), heads * in.l->head_dim);
+    float* const lse = in.a[10] == Py_None ? nullptr : static_cast<float*>(in.whole(10, at::kFloat, heads));
+    const auto ws = in.space(12, in.taken ? more.sparse_bytes(c, T, entries) : 0);
+    return in.call([&](void* s) { return more.sparse(c, q.at, q.stride, kc, vc, cu, before, table, width, lists, entries, out, lse, B, T, ws.at, ws.bytes, s); });
+  });
+}
+
+// (addresses of the entry points, in the order of SparseEntries)
+PyObject* bind_sparse(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  void* at[6];
+  if (n != 6) {
+    PyErr_SetString(PyExc_TypeError, "bind_sparse() takes six addresses");
+    return nullptr;
+  }
+  for (int i = 0; i < 6; ++i) {
+    at[i] = PyLong_AsVoidPtr(a[i]);
+    if (!at[i] && PyErr_Occurred()) return nullptr;
+  }
+  more.rope = reinterpret_cast<decltype(more.rope)>(at[0]);
+  more.summary = reinterpret_cast<decltype(more.summary)>(at[1]);
+  more.select_bytes = reinterpret_cast<decltype(more.select_bytes)>(at[2]);
+  more.select = reinterpret_cast<decltype(more.select)>(at[3]);
+  more.sparse_bytes = reinterpret_cast<decltype(more.sparse_bytes)>(at[4]);
+  more.sparse = reinterpret_cast<decltype(more.sparse)>(at[5]);
+  Py_RETURN_NONE;
+}
+
 // (addresses of the entry points, in the order of Entries)
 PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
   void* at[5];
@@ -194,7 +369,8 @@ PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
 
 #define ECO_FAST(f) {#f, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {ECO_FAST(bind), ECO_FAST(kv_append), ECO_FAST(attn_prefill), ECO_FAST(attn_decode), ECO_FAST(attn_decode_append),
-                         ECO_FAST(attn_decode_noalloc), {nullptr, nullptr, 0, nullptr}};
+                         ECO_FAST(attn_decode_noalloc),
+                         ECO_FAST(bind_sparse), ECO_FAST(kv_append_rope), ECO_FAST(kv_summary), ECO_FAST(block_select), ECO_FAST(attn_sparse), {nullptr, nullptr, 0, nullptr}};
 // (ECO_BIND_FITS: the interpreter and the torch that this is compiled for; build.py looks for it in the built file)
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_bind", "Marshalling of the hot calls' arguments, " ECO_BIND_FITS, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -510,3 +510,43 @@ def test_recorded_into_a_graph_on_another_stream():
             assert torch.equal(a.view(torch.uint8), b.view(torch.uint8)), i
         before += 1
     ctx.close()
+
+
+def test_what_the_binding_takes_and_what_it_refuses():
+    """Bounds of any integer type go the longer way with the same result; tensors of another type, size, device or layout are refused by name."""
+    b = Batch("bf16", 64, 4, 2, [300, 77], [1, 1], seed=4)
+    summary, _, _ = _all_summarised(b)
+    q, lists, K = b.q.cuda(), torch.zeros(2, 2, 4, dtype=torch.int32, device="cuda"), 4
+    d, out, lse = b.dev, torch.zeros(2, 4, 64, dtype=b.dt, device="cuda"), torch.zeros(2, 4, device="cuda")
+    sel = dict(q=q, summary=summary, ctx_before=d["ctx_before"], block_table=d["block_table"], blocks=lists, max_ctx_len=301, cu_q=None, workspace=None)
+    b.ctx.block_select(**sel)
+    want = lists.clone()
+    for bound in (np.int32(301), np.int64(301), torch.tensor(301)):
+        lists.zero_()
+        b.ctx.block_select(**{**sel, "max_ctx_len": bound, "keep_first": np.int64(1)})
+        assert torch.equal(lists, want)
+    att = dict(q=q, k_cache=b.kc, v_cache=b.vc, ctx_before=d["ctx_before"], block_table=d["block_table"], blocks=lists, out=out, lse=lse, cu_q=None, workspace=None)
+    b.ctx.attn_sparse(**att)
+    summ = dict(k_cache=b.kc, summary=summary, cu_q=d["cu_q"], ctx_before=d["ctx_before"], block_table=d["block_table"], T=2)
+    before = summary.clone()
+    b.ctx.kv_summary(**{**summ, "T": np.int32(2), "max_new_len": np.int64(1)})
+    assert torch.equal(summary, before)
+    small = torch.zeros(8, dtype=torch.uint8, device="cuda")
+    wrong = [(b.ctx.block_select, sel, {"q": [q.float(), q.cpu(), q[:, :2], q[..., :32], q[:1]], "summary": [summary[:-99], summary.to(torch.uint8), summary.cpu()],
+                                        "ctx_before": [d["ctx_before"].long(), d["ctx_before"].cpu(), torch.stack([d["ctx_before"]] * 2, 1)[:, 0]],
+                                        "block_table": [d["block_table"][0], d["block_table"][:1], d["block_table"].long(), d["block_table"][:, 1:]],
+                                        "blocks": [lists[:1], lists[:, :1], lists.long(), lists[..., ::2]], "cu_q": [d["cu_q"][:2], d["cu_q"].long()], "workspace": [small.cpu()]}),
+             (b.ctx.attn_sparse, att, {"q": [q.float()], "k_cache": [b.kc[:-1], b.kc.float(), b.kc.cpu()], "v_cache": [b.vc[:-1]], "blocks": [lists[0], lists.cpu()],
+                                       "out": [out[:1], out.float(), out.transpose(0, 1)], "lse": [lse[:1], lse.double(), lse.cpu()], "cu_q": [d["cu_q"].cpu()]}),
+             (b.ctx.kv_summary, summ, {"k_cache": [b.kc[:-1], b.kc.float()], "summary": [summary[:-99]], "cu_q": [d["cu_q"][:2]], "block_table": [d["block_table"].cpu()]})]
+    for call, good, changes in wrong:
+        for name, values in changes.items():
+            for value in values:
+                with pytest.raises(ValueError):
+                    call(**{**good, name: value})
+    from paper_2504_18154_amd import binding
+    for call, change in ((b.ctx.block_select, {**sel, "workspace": small}), (b.ctx.block_select, {**sel, "keep_last": 0}), (b.ctx.block_select, {**sel, "max_ctx_len": 0}),
+                         (b.ctx.block_select, {**sel, "max_ctx_len": 1 << 20})):
+        with pytest.raises(binding.EcoserveError):
+            call(**change)
+    b.ctx.close()

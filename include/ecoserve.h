@@ -405,7 +405,7 @@ int ecoserve_kv_append_rope(ecoserve_ctx* ctx, const ecoserve_rope* rope, const 
  *     codes     [num_blocks][Hkv][2][Dp]   top, then low; Dp = head_dim rounded up to 32, zeros from head_dim on
  *     exponents [num_blocks][Hkv]
  * of ecoserve_summary_bytes(layout) bytes.  A query head is coded the same way, q8[d] = rint(q[d] / 2^eq) (half to even; a
- * head with a NaN or an infinity: zeros, eq = 0), and the score of block j for K/V head g of a token is
+ * head with a NaN, an infinity or an element beyond 127 * 2^100: zeros), and the score of block j for K/V head g of a token is
  *     max over the heads h of g of  2^(eq[h] + e) * sum_d max(q8[h][d] * top[d], q8[h][d] * low[d]),
  * +inf if e = 127.  The sums are integers below 2^22, so scores are exact in fp32 and which blocks are chosen does not
  * depend on the order of any sum.

@@ -41,7 +41,7 @@ def summarise(keys: np.ndarray):
 
 def query_codes(q: np.ndarray):
     """q [D] -> (codes int [D], exponent); Python's round is to even."""
-    if not np.isfinite(q).all():
+    if not (np.abs(q.astype(np.float64)) <= 127.0 * 2.0 ** 100).all():
         return np.zeros(len(q), dtype=np.int64), 0
     e = code_exponent(float(np.abs(q.astype(np.float64)).max()))
     return np.array([round(float(x) / 2.0 ** e) for x in q], dtype=np.int64), e

@@ -5,14 +5,15 @@
 // column it is v_mfma_i32_16x16x64_i8, exact in 32 bits; scaled by a power of two it is exact in fp32 too.  Hence no
 // order of sums, number of tokens or split of the blocks changes which blocks are chosen.
 //
-// Two launches, with the scores between them in the workspace, as unsigned numbers that are ordered as the scores are:
-//   score_kernel   a wavefront has the rows (token, head of the group) of up to NA tiles of 16 as operands in registers and walks tiles of 16 blocks:
-//                  16 bytes a lane and step, straight into operand layout.  The rows of a token are padded to a power of two with
-//                  copies of its last head, so that the maximum over the heads is within a lane's four results and over
-//                  at most two exchanges.  One token: bound by reading the records; prompts: by the products.
-//   choose_kernel  a workgroup per (token, K/V head): a histogram of 2048 bins between the smallest and the largest
-//                  number finds the bin that holds the last one to be chosen, then the same within that bin, until it is a
-//                  single number or all of it is chosen; one prefix sum then writes the indices in their order.
+// The rows of a product are (token, head of the group), a token's padded to a power of two with copies of its last head, so that the
+// maximum over the heads is within a lane's four results and over at most two exchanges; its columns are 16 blocks, 16 bytes a lane and step, straight into
+// operand layout.
+//   score_step_kernel    few tokens per sequence: a workgroup codes up to 16 rows into LDS and walks a run of block tiles.  Bound by reading the records.
+//   code_kernel, score_prompt_kernel   prompts: the rows are coded once, into the workspace; a wavefront has four tiles of them in registers.  Bound by the
+//                        products and what is done with their results.
+//   choose               a wavefront or more per (token, K/V head), the scores in registers.  For steps over short contexts the workgroup that is
+//                        done last with a row's scores does it in the same launch, otherwise choose_kernel.
+// The scores go through the workspace.
 #include <algorithm>
 #include <type_traits>
 
@@ -25,6 +26,7 @@ namespace eco {
 namespace {
 
 constexpr int kScoreThreads = 256, kScoreWaves = 4;
+constexpr float kLargestQuery = 127.f * 0x1p100f;  // query heads beyond it are coded as zeros: a sum of products times 2^eq then stays in range
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 
 // The tokens of a call: which sequence a token belongs to and where it stands.
@@ -33,34 +35,314 @@ struct Tokens {
   int B, T;
 };
 
-// 16 elements of a query row from d on, as floats; zeros from D on.
-template <typename E>
-__device__ __forceinline__ void load16(const E* __restrict__ row, int d, int D, float (&x)[16]) {
-  constexpr int X = Elem<E>::X;
-#pragma unroll
-  for (int u = 0; u < 16 / X; ++u) {
-    u32x4 raw = {0u, 0u, 0u, 0u};
-    if (d + u * X < D) raw = *reinterpret_cast<const u32x4*>(row + d + u * X);
-#pragma unroll
-    for (int e = 0; e < X; ++e)
-      x[u * X + e] = sizeof(E) == 2 ? __uint_as_float(e & 1 ? raw[e / 2] & 0xffff0000u : raw[e / 2] << 16) : __uint_as_float(raw[e % 4]);
-  }
+// What a row is chosen into.
+struct Chosen {
+  int32_t* blocks;
+  int K, keep_first, keep_last;
+};
+
+// The maximum over lanes 16 (32) apart.
+__device__ __forceinline__ float max_of_rows16(float v) {
+  const auto x = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(x[0]), __uint_as_float(x[1]));
+}
+__device__ __forceinline__ float max_of_rows32(float v) {
+  const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(x[0]), __uint_as_float(x[1]));
+}
+// The maximum over the 16 lanes of a row of lanes.
+__device__ __forceinline__ float max_in_row(float v) {
+  auto with = [&](auto ctrl) {
+    v = fmaxf(v, __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), decltype(ctrl)::value, 0xf, 0xf, false)));
+  };
+  with(std::integral_constant<int, 0xB1>());   // quad_perm 1 0 3 2
+  with(std::integral_constant<int, 0x4E>());   // quad_perm 2 3 0 1
+  with(std::integral_constant<int, 0x141>());  // row_half_mirror
+  with(std::integral_constant<int, 0x140>());  // row_mirror
+  return v;
 }
 
-// Unsigned numbers in the order of the floats (no NaN; -0 counts as 0).  0 and 0xffffffff are no float's.
+// A query head as whole numbers, by the 16 lanes of a row of lanes: `ask` has its 16-byte units on the way, `code` writes [max(q8, 0) | min(q8, 0)] to
+// `to` and returns 2^eq.
+template <typename E, int NF>
+struct CodedRow {
+  static constexpr int X = Elem<E>::X, kUnits = (NF * 32 / X + 15) / 16;
+  u32x4 raw[kUnits];
+  __device__ __forceinline__ void ask(const E* __restrict__ row, int D, int col) {
+#pragma unroll
+    for (int k = 0; k < kUnits; ++k) {
+      const int d = (col + 16 * k) * X;
+      raw[k] = d < D ? *reinterpret_cast<const u32x4*>(row + d) : u32x4{0u, 0u, 0u, 0u};
+    }
+  }
+  __device__ __forceinline__ float code(int8_t* to, int col) const {
+    constexpr int Dp = NF * 32;
+    float x[kUnits][X], size = 0.f;
+    bool fine = true;
+#pragma unroll
+    for (int k = 0; k < kUnits; ++k)
+#pragma unroll
+      for (int i = 0; i < X; ++i) {
+        x[k][i] = sizeof(E) == 2 ? __uint_as_float(i & 1 ? raw[k][i / 2] & 0xffff0000u : raw[k][i / 2] << 16) : __uint_as_float(raw[k][i % 4]);
+        size = fmaxf(size, fabsf(x[k][i]));
+        fine = fine && x[k][i] == x[k][i];
+      }
+    size = max_in_row(fine ? size : INFINITY);
+    fine = size <= kLargestQuery;
+    const int e = code_exponent(size);
+#pragma unroll
+    for (int k = 0; k < kUnits; ++k) {
+      uint32_t top[X / 4], low[X / 4];
+#pragma unroll
+      for (int w = 0; w < X / 4; ++w) {
+        top[w] = low[w] = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int c = fine ? (int)rintf(ldexpf(x[k][w * 4 + i], -e)) : 0;
+          top[w] |= ((uint32_t)max(c, 0) & 0xffu) << (8 * i);
+          low[w] |= ((uint32_t)min(c, 0) & 0xffu) << (8 * i);
+        }
+      }
+      const int d = (col + 16 * k) * X;
+      if (d >= Dp) continue;
+      if constexpr (X == 8) {
+        *reinterpret_cast<u32x2*>(to + d) = u32x2{top[0], top[1]};
+        *reinterpret_cast<u32x2*>(to + Dp + d) = u32x2{low[0], low[1]};
+      } else {
+        *reinterpret_cast<uint32_t*>(to + d) = top[0];
+        *reinterpret_cast<uint32_t*>(to + Dp + d) = low[0];
+      }
+    }
+    return fine ? ldexpf(1.f, e) : 1.f;
+  }
+};
+
+// The numbers of a row in order: the larger the score the larger the number.  (No NaN; -0 counts as 0; 0 is no score's number.)
 __device__ __forceinline__ uint32_t ordered(float x) {
   const uint32_t u = __float_as_uint(x + 0.f);
   return u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
 }
 
-// NF: steps of 64 (record bytes / 64); NA: row tiles of a wavefront.  Grid: K/V heads, runs of tiles_per_wave * 4 block tiles, token groups from `unit0` on;
-// a group is up to `group` tokens of one sequence, numbered from cu_q[b] / group + b.  Tokens outside [t0, t1) are another launch's.
-template <typename E, int NF, int NA>
-__global__ __launch_bounds__(kScoreThreads) void score_kernel(const E* __restrict__ q, int q_row_stride, const int8_t* __restrict__ codes,
-                                                               const int8_t* __restrict__ exponents, Tokens tk, const int32_t* __restrict__ block_table,
-                                                               int bt_stride, uint32_t* __restrict__ scores, int64_t row_words, int G, int log_rows, int Hkv, int D,
-                                                               int group, int unit0, int t0, int t1, int tiles_per_wave) {
-  const int g = blockIdx.x, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, quad = lane >> 4;
+// Choosing the largest of a row's numbers: histograms, two that are used in turn, with a bin per lane for what is not counted, and what the wavefronts tell one
+// another.
+template <int WAVES, int BINS>
+struct ChooseShared {
+  alignas(16) int hist[2][BINS + 64];
+  uint32_t low[WAVES], high[WAVES], left[64];
+  int sures[WAVES], sames[WAVES], n_left;
+};
+template <int WAVES>
+__device__ __forceinline__ void together() {
+  if constexpr (WAVES > 1) {
+    __syncthreads();
+  } else {  // (a wavefront by itself: its LDS accesses take effect in their order)
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+  }
+}
+
+// K of the n blocks of a row, ascending, to `out`: all outside [c0, c1), and of those inside, whose scores are ask(j), the best; lower indices first
+// among equal ones.  n > K.  Each wavefront has a run of indices, a lane every 64th: PER of them, in registers, or, PER 0, as many as it takes, asked for
+// again each time.  A histogram between the smallest and the largest number finds the bin in which the last one to be chosen is.  Up to 64 numbers of
+// that bin are then compared with one another, a lane each, bit by bit; of more, another histogram is made.  Every wavefront does all of that but the counting
+// by itself: a barrier or two a round.  What bounds it is instructions, their fetching where a row is alone: hence no branch per number.
+// (895 tokens, 8 K/V heads, about 1500 blocks, a wavefront a row, us: loads and counts under branches 36.1, loads at once 27.0, so 16.0.)
+template <int WAVES, int PER, int BINS, typename Ask>
+__device__ __forceinline__ void choose(Ask ask, int wave, int n, int c0, int c1, int K, int32_t* __restrict__ out, ChooseShared<WAVES, BINS>& s) {
+  constexpr int THREADS = WAVES * 64, kMine = BINS / 64, kLog = BINS == 1024 ? 10 : 9, kAll = 2 * (BINS + 64);
+  static_assert(BINS == 1 << kLog, "bins");
+  const int lane = threadIdx.x & 63, tid = wave * 64 + lane;
+  const int run = PER > 0 ? PER * 64 : (n + THREADS - 1) / THREADS * 64, j0 = wave * run + lane;
+  // 0: no block; the largest: chosen whatever its score
+  auto number = [&](float x, int j) { return j >= n ? 0u : j < c0 || j >= c1 ? ~0u : ordered(x); };
+  uint32_t key[PER > 0 ? PER : 1];
+  if constexpr (PER > 0) {
+    float x[PER];  // (all asked for at once, the last one in place of those behind it)
+#pragma unroll
+    for (int i = 0; i < PER; ++i) x[i] = ask(min(j0 + i * 64, c1 - 1));
+#pragma unroll
+    for (int i = 0; i < PER; ++i) key[i] = number(x[i], j0 + i * 64);
+  }
+  auto each = [&](auto f) {
+    if constexpr (PER > 0) {
+#pragma unroll
+      for (int i = 0; i < PER; ++i) {
+        if (i % 8 == 0 && wave * run + i * 64 >= n) break;
+        f(key[i], j0 + i * 64);
+      }
+    } else {
+      for (int j = j0; j - lane < min(n, (wave + 1) * run); j += 64) f(number(ask(min(j, c1 - 1)), j), j);
+    }
+  };
+  int need = K - (n - (c1 - c0));
+  uint32_t at = ~0u - 1u;  // all numbers above it are chosen, and `need` of those equal to it
+  if (need > 0) {
+    uint32_t low = ~0u, high = 0u;
+    each([&](uint32_t k, int) {  // (0 becomes the largest for one, the largest 0 for the other)
+      low = min(low, k - 1u);
+      high = max(high, k + 1u);
+    });
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) low = min(low, (uint32_t)__shfl_xor((int)low, o)), high = max(high, (uint32_t)__shfl_xor((int)high, o));
+    for (int i = tid * 4; i < kAll; i += THREADS * 4) *reinterpret_cast<u32x4*>(&s.hist[0][0] + i) = u32x4{0u, 0u, 0u, 0u};
+    if (tid == 0) s.n_left = 0;
+    if (WAVES > 1 && lane == 0) s.low[wave] = low, s.high[wave] = high;
+    together<WAVES>();
+    if (WAVES > 1)
+#pragma unroll
+      for (int w = 0; w < WAVES; ++w) low = min(low, s.low[w]), high = max(high, s.high[w]);
+    ++low;
+    uint32_t span = high - 1u - low;  // numbers low .. low + span
+    for (int turn = 0;; turn ^= 1) {
+      const int shift = max(0, 32 - kLog - __clz((int)(span | 1u)));
+      each([&](uint32_t k, int) {
+        const uint32_t d = k - low;
+        atomicAdd(&s.hist[turn][d <= span ? d >> shift : BINS + lane], 1);
+      });
+      together<WAVES>();
+      // from the last bin down, a lane kMine of them: the bin in which the count reaches `need`
+      int mine = 0;
+#pragma unroll
+      for (int i = 0; i < kMine; i += 4) {
+        const u32x4 x = *reinterpret_cast<const u32x4*>(&s.hist[turn][BINS - 4 - lane * kMine - i]);
+        mine += (int)(x[0] + x[1]) + (int)(x[2] + x[3]);
+      }
+      const int upto = lanes_prefix_sum(mine);
+      const int l = __builtin_ctzll(__ballot(upto >= need) | 1ull << 63);  // the lane that has it
+      need -= __builtin_amdgcn_readlane(upto - mine, l);
+      // (its bins, a lane each)
+      const int one = lane < kMine ? s.hist[turn][BINS - 1 - l * kMine - min(lane, kMine - 1)] : 0, to = lanes_prefix_sum(one);
+      const int b = __builtin_ctzll(__ballot(to >= need) | 1ull << 63), in_bin = __builtin_amdgcn_readlane(one, b);
+      need -= __builtin_amdgcn_readlane(to - one, b);
+      low += (uint32_t)(BINS - 1 - l * kMine - b) << shift;
+      if (need == in_bin) {  // all of the bin
+        at = low - 1;
+        need = 0;
+        break;
+      }
+      if (shift == 0) {
+        at = low;
+        break;
+      }
+      span = (1u << shift) - 1u;
+      if (in_bin <= 64) {
+        each([&](uint32_t k, int) {
+          const bool in = k - low <= span;
+          if (__any(in)) {
+            if (in) s.left[atomicAdd(&s.n_left, 1) & 63] = k - low;
+          }
+        });
+        together<WAVES>();
+        const uint32_t d = lane < in_bin ? s.left[lane] : 0u;
+        uint32_t found = 0;  // the largest number that at least `need` of them reach
+        for (uint32_t bit = 1u << (shift - 1); bit; bit >>= 1)
+          if (__popcll(__ballot(lane < in_bin && d >= (found | bit))) >= need) found |= bit;
+        need -= __popcll(__ballot(lane < in_bin && d > found));
+        at = low + found;
+        if (need == __popcll(__ballot(lane < in_bin && d == found))) --at, need = 0;  // (all of them)
+        break;
+      }
+      // the histogram of the round after the next
+      together<WAVES>();
+      for (int i = tid * 4; i < BINS; i += THREADS * 4) *reinterpret_cast<u32x4*>(&s.hist[turn][i]) = u32x4{0u, 0u, 0u, 0u};
+    }
+  }
+  // how many each wavefront has, then where they go
+  auto before = [&](unsigned long long m) { return (int)__builtin_amdgcn_mbcnt_hi((unsigned)(m >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)m, 0u)); };
+  int sures = 0, sames = 0;
+  if (WAVES > 1) {
+    each([&](uint32_t k, int) {
+      sures += __popcll(__ballot(k > at));
+      sames += __popcll(__ballot(k == at));
+    });
+    if (lane == 0) s.sures[wave] = sures, s.sames[wave] = sames;
+    together<WAVES>();
+    sures = sames = 0;
+    for (int w = 0; w < wave; ++w) sures += s.sures[w], sames += s.sames[w];
+  }
+  if (need == 0) {
+    each([&](uint32_t k, int j) {
+      const unsigned long long m = __ballot(k > at);
+      if (k > at) out[min(sures + before(m), K - 1)] = j;
+      sures += __popcll(m);
+    });
+  } else {
+    each([&](uint32_t k, int j) {
+      const unsigned long long m0 = __ballot(k > at), m1 = __ballot(k == at);
+      const int nth_same = sames + before(m1);
+      if (k > at || (k == at && nth_same < need)) out[min(sures + before(m0) + min(nth_same, need), K - 1)] = j;
+      sures += __popcll(m0);
+      sames += __popcll(m1);
+    });
+  }
+}
+
+// Scores of a row, from one workgroup to another within a launch and possibly between XCDs: past the caches that XCDs do not share.
+constexpr int kRsrc = 0x00020000, kAgent = 16;
+// Scores of n tokens for one K/V head, from the first one's row on (below 2 GiB: more than one token at a time have 192 MiB).
+constexpr int kNowhere = 0x7fff0000;
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t score_rows(float* out, int n, int Hkv, int64_t row_words) {
+  return __builtin_amdgcn_make_buffer_rsrc(out, 0, (int)(((int64_t)(n - 1) * Hkv + 1) * row_words * 4), kRsrc);
+}
+// (no branch around a store: it would have everything waited for that is under way)
+template <int AUX>
+__device__ __forceinline__ void put_score(__amdgpu_buffer_rsrc_t to, int where, int tile, float v, int e) {
+  const float score = e == kNotFinite ? INFINITY : ldexpf(v, e);
+  __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(score), to, where, tile * 64, AUX);
+}
+
+// A tile of 16 records, from memory to LDS to operands.  A lane's operand is 16 bytes of "its" block, so loads straight into operand layout would have
+// neighbouring lanes ask different lines, 64 requests an instruction (and they bound both kernels: 62 us of 895 tokens, 64 us of 32 long contexts);
+// so lanes ask for 64 bytes in a row per four, and LDS turns them over.  Unit s (16 bytes) of block c lies at unit s ^ mix(c) of its
+// row, which has the 16 blocks' units of any step at different banks.
+template <int NF>
+struct Records {
+  static constexpr int kUnits = 4 * NF, kBytes = 16 * kUnits * 16, kBits = NF % 4 == 0 ? 4 : NF % 2 == 0 ? 3 : 2;
+  u32x4 raw[NF];
+  int e;
+  static __device__ __forceinline__ int mix(int c) { return c >> (4 - kBits); }
+  // id: the block of lanes c, c + 16, ..
+  __device__ __forceinline__ void ask(const int8_t* __restrict__ codes, const int8_t* __restrict__ exponents, int id, int g, int Hkv, int lane) {
+#pragma unroll
+    for (int i = 0; i < NF; ++i) {
+      const int u = i * 64 + lane, c = u / kUnits, s = (u - c * kUnits) ^ mix(c);
+      raw[i] = *reinterpret_cast<const u32x4*>(codes + ((size_t)__shfl(id, c) * Hkv + g) * (kUnits * 16) + s * 16);
+    }
+    e = exponents[(size_t)id * Hkv + g];
+  }
+  __device__ __forceinline__ void put(char* tile, int lane) const {
+#pragma unroll
+    for (int i = 0; i < NF; ++i) *reinterpret_cast<u32x4*>(tile + (i * 64 + lane) * 16) = raw[i];
+  }
+  static __device__ __forceinline__ void get(i32x4 (&bf)[NF], const char* tile, int col, int quad) {
+#pragma unroll
+    for (int f = 0; f < NF; ++f) bf[f] = *reinterpret_cast<const i32x4*>(tile + (col * kUnits + ((4 * f + quad) ^ mix(col))) * 16);
+  }
+};
+
+// NF: steps of 64 (record bytes / 64).  Grid: K/V heads, runs of tiles_per_wave * 4 block tiles, token groups from `unit0` on; a group is up to `group` tokens of one
+// sequence, numbered from cu_q[b] / group + b.  Tokens outside [t0, t1) are another launch's.  PER > 0 (one token per sequence, rows of at most 256 PER blocks):
+// the workgroup that is done last with a row chooses its blocks; counters [T][Hkv] are zero and stay so.
+template <typename E, int NF, int PER>
+__global__ __launch_bounds__(kScoreThreads) void score_step_kernel(const E* __restrict__ q, int q_row_stride, const int8_t* __restrict__ codes,
+                                                                    const int8_t* __restrict__ exponents, Tokens tk, const int32_t* __restrict__ block_table,
+                                                                    int bt_stride, float* __restrict__ scores, int64_t row_words, int G, int log_rows, int Hkv, int D,
+                                                                    int group, int unit0, int t0, int t1, int tiles_per_wave, Chosen to,
+                                                                    uint32_t* __restrict__ counters) {
+  constexpr int Dp = NF * 32, kRow = 2 * Dp + 16;  // bytes of a coded row in LDS, 16 more than it has: rows begin at different banks
+  constexpr bool kChoose = PER > 0;
+  struct Coded {
+    float scale[16];
+    alignas(16) int8_t row[16 * kRow];
+  };
+  __shared__ Coded coded;
+  __shared__ __attribute__((aligned(16))) char s_tiles[kScoreWaves][Records<NF>::kBytes];
+  __shared__ ChooseShared<kScoreWaves, kChoose ? 1024 : 512> s_choose;
+  __shared__ int s_order;
+  // (the records of a block's K/V heads are neighbours of 256 bytes, say: an XCD that had one head alone, as it would by the first index, would ask the
+  // same few channels of its cache for all of them)
+  const int g = (int)((blockIdx.x + blockIdx.y + blockIdx.z) % (unsigned)Hkv);
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 15, quad = lane >> 4;
   // the group's tokens: first .. first + n - 1 of sequence b, the first at position p0
   int b, first, n, p0;
   if (tk.cu_q) {
@@ -72,138 +354,244 @@ __global__ __launch_bounds__(kScoreThreads) void score_kernel(const E* __restric
     first = max(seq.tok0 + i0, t0);
     n = min(min(seq.tok0 + i0 + group, seq.tok0 + seq.S), t1) - first;
     p0 = seq.cb + first - seq.tok0;
+    if (n <= 0 || p0 + n - 1 < 0) return;
   } else {
     b = first = unit0 + blockIdx.z;
-    n = first < t1 ? 1 : 0;
-    p0 = n ? tk.ctx_before[b] : -1;
+    n = 1;
+    p0 = tk.ctx_before[b];
   }
-  if (n <= 0 || p0 + n - 1 < 0) return;
-  // the blocks that the group's last token scores: all in front of its own, which are full
-  const int scored = (int)min((int64_t)((p0 + n - 1) >> 4), row_words);
-  const int tile0 = (blockIdx.y * kScoreWaves + wave) * tiles_per_wave;
-  if (tile0 * 16 >= scored) return;
+  // a row to each 16 lanes, asked for before anything is known of the lengths
+  const int r = wave * 4 + quad, r_tok = min(r / G, n - 1), r_head = r - r / G * G;
+  CodedRow<E, NF> mine;
+  mine.ask(q + (size_t)(first + r_tok) * q_row_stride + (size_t)(g * G + r_head) * D, D, col);
 
-  // operands of the rows: row r of tile a is head min(r % rows, G - 1) of token a * (16 / rows) + r / rows
-  const int rows = 1 << log_rows, per_tile = 16 >> log_rows, Dp = NF * 32;
+  // the blocks that the group's last token scores: all in front of its own, which are full
+  const int scored = p0 + n - 1 < 0 ? 0 : (int)min((int64_t)((p0 + n - 1) >> 4), row_words);
+  const int per_wg = kScoreWaves * tiles_per_wave, tile0 = blockIdx.y * per_wg, tiles = (scored + 15) >> 4;
+  if constexpr (kChoose) {
+    const int seen = p0 < 0 ? 0 : scored + 1;
+    if (seen <= to.K) {  // all of them
+      int32_t* const out = to.blocks + ((int64_t)first * Hkv + g) * to.K;
+      if (blockIdx.y == 0)
+        for (int i = tid; i < to.K; i += kScoreThreads) out[i] = i < seen ? i : -1;
+      return;
+    }
+  }
+  if (tile0 >= tiles) return;
+
+  // records of the wavefront's first tile and block ids of the second, on their way while the rows are coded
+  const int32_t* const table = block_table + (size_t)b * bt_stride;
+  const int tile_first = tile0 + wave, tile1 = min(tile0 + per_wg, tiles);
+  auto block_at = [&](int tile) { return table[min(tile * 16 + col, scored - 1)]; };
+  // (records two tiles ahead, block ids three)
+  Records<NF> ahead[2];
+  const int id0 = block_at(tile_first), id1 = block_at(tile_first + kScoreWaves);
+  int id2 = block_at(tile_first + 2 * kScoreWaves);
+  ahead[0].ask(codes, exponents, id0, g, Hkv, lane);
+  ahead[1].ask(codes, exponents, id1, g, Hkv, lane);
+
+  const float scale_here = mine.code(&coded.row[r * kRow], col);
+  if (col == 0) coded.scale[r] = scale_here;
+  __syncthreads();
+  // operands of the rows: row r is head min(r % rows, G - 1) of token r / rows
+  const int rows = 1 << log_rows;
+  auto row_of = [&](int x) { return min(x >> log_rows, n - 1) * G + min(x & (rows - 1), G - 1); };
+  i32x4 af[NF];
+  float scale[4];
+#pragma unroll
+  for (int f = 0; f < NF; ++f) af[f] = *reinterpret_cast<const i32x4*>(&coded.row[row_of(col) * kRow + quad * 16 + f * 64]);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) scale[i] = coded.scale[row_of(quad * 4 + i)];
+
+  // scores of the group's first token from `out` on; lanes that hold none store behind the end, which the hardware leaves out
+  float* const out = scores + ((int64_t)(first - t0) * Hkv + g) * row_words;
+  const __amdgpu_buffer_rsrc_t to_scores = score_rows(out, n, Hkv, row_words);
+  const int step = log_rows < 2 ? rows : 4;  // results 0, step, .. of a lane are tokens of their own
+  int where[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int row = quad * 4 + i, tok = row >> log_rows;
+    where[i] = (row & (rows - 1)) == 0 && tok < n ? (int)(tok * Hkv * row_words) * 4 + col * 4 : kNowhere;
+  }
+  char* const tile_lds = s_tiles[wave];
+  auto walk = [&](Records<NF>& r, int tile) {
+    r.put(tile_lds, lane);
+    const int e = r.e;
+    r.ask(codes, exponents, id2, g, Hkv, lane);  // (behind the last tile: its last block)
+    id2 = block_at(tile + 3 * kScoreWaves);
+    i32x4 bf[NF], c = {0, 0, 0, 0};
+    Records<NF>::get(bf, tile_lds, col, quad);
+#pragma unroll
+    for (int f = 0; f < NF; ++f) c = __builtin_amdgcn_mfma_i32_16x16x64_i8(af[f], bf[f], c, 0, 0, 0);
+    float v[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = (float)c[i] * scale[i];
+    // the maximum over a token's rows; it is then in v[0] (and, for one or two rows a token, v[2] or all four)
+    if (log_rows >= 1) v[0] = fmaxf(v[0], v[1]), v[2] = fmaxf(v[2], v[3]);
+    if (log_rows >= 2) v[0] = fmaxf(v[0], v[2]);
+    if (log_rows >= 3) v[0] = max_of_rows16(v[0]);
+    if (log_rows >= 4) v[0] = max_of_rows32(v[0]);
+#pragma unroll
+    for (int i = 0; i < (kChoose ? 1 : 4); ++i) {
+      if (i & (step - 1)) continue;
+      put_score<kChoose ? kAgent : 0>(to_scores, where[i], tile, v[i], e);
+    }
+  };
+  for (int tile = tile_first; tile < tile1; tile += 2 * kScoreWaves) {
+    walk(ahead[0], tile);
+    if (tile + kScoreWaves >= tile1) break;
+    walk(ahead[1], tile + kScoreWaves);
+  }
+  if constexpr (kChoose) {
+    const int wgs = (tiles + per_wg - 1) / per_wg;    // that score blocks of this row
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // (this wavefront's scores are where every XCD finds them)
+    __syncthreads();
+    if (wgs > 1) {
+      if (tid == 0) {
+        uint32_t* const counter = counters + (int64_t)first * Hkv + g;
+        s_order = (int)__hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        if (s_order == wgs - 1) __hip_atomic_store(counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      }
+      __syncthreads();
+      if (__builtin_amdgcn_readfirstlane(s_order) != wgs - 1) return;
+    }
+    const __amdgpu_buffer_rsrc_t from = __builtin_amdgcn_make_buffer_rsrc(out, 0, (int)row_words * 4, kRsrc);
+    const int seen = scored + 1;
+    choose<kScoreWaves, PER>([&](int j) { return __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(from, j * 4, 0, kAgent)); }, wave, seen, to.keep_first,
+                             seen - to.keep_last, to.K, to.blocks + ((int64_t)first * Hkv + g) * to.K, s_choose);
+  }
+}
+
+// Rows (token, K/V head, head of the group padded to 1 << log_rows) of tokens from t0 on, as whole numbers; a row to each 16 lanes.
+template <typename E, int NF>
+__global__ __launch_bounds__(256) void code_kernel(const E* __restrict__ q, int q_row_stride, int8_t* __restrict__ coded, float* __restrict__ scale, int64_t rows,
+                                                   int G, int log_rows, int Hkv, int D, int t0) {
+  const int64_t r = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4), at = min(r, rows - 1), pair = at >> log_rows, t = pair / Hkv;
+  const int col = threadIdx.x & 15, h = min((int)(at & ((1 << log_rows) - 1)), G - 1), g = (int)(pair - t * Hkv);
+  CodedRow<E, NF> mine;
+  mine.ask(q + (size_t)(t0 + t) * q_row_stride + (size_t)(g * G + h) * D, D, col);
+  const float s = mine.code(coded + at * (NF * 64), col);  // (the last row, possibly several times: the same bytes)
+  if (col == 0) scale[at] = s;
+}
+
+constexpr int kPromptTiles = 4;  // row tiles of a wavefront
+// Tokens of a wavefront of score_prompt_kernel; a workgroup has four times as many.
+constexpr int prompt_tokens(int log_rows) { return kPromptTiles * (16 >> log_rows); }
+
+// Grid: K/V heads, runs of `run` times four block tiles, token groups from unit0 on as in score_step_kernel.  The wavefronts of a workgroup have different tokens of the
+// group; four tiles of blocks at a time, each brought in by one of them, serve all.
+template <int NF, int LOG>
+__global__ __launch_bounds__(kScoreThreads) void score_prompt_kernel(const int8_t* __restrict__ coded, const float* __restrict__ scales,
+                                                                      const int8_t* __restrict__ codes, const int8_t* __restrict__ exponents, Tokens tk,
+                                                                      const int32_t* __restrict__ block_table, int bt_stride, float* __restrict__ scores,
+                                                                      int64_t row_words, int Hkv, int unit0, int t0, int t1, int run) {
+  constexpr int Dp = NF * 32, NA = kPromptTiles, kTokens = prompt_tokens(LOG), kGroup = kTokens * kScoreWaves, kPerTile = 16 >> LOG;
+  __shared__ __attribute__((aligned(16))) char s_tiles[2][kScoreWaves][Records<NF>::kBytes];
+  __shared__ int s_e[2][kScoreWaves][16];
+  const int g = blockIdx.x, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, quad = lane >> 4;
+  const int unit = unit0 + blockIdx.z;
+  auto first_unit = [&](int cu, int s) { return (long long)(cu / kGroup) + s; };
+  const SeqOf seq = find_sequence(tk.cu_q, tk.ctx_before, tk.B, unit, first_unit);
+  const int i0 = (int)(unit - first_unit(seq.tok0, seq.b)) * kGroup;
+  const int group0 = max(seq.tok0 + i0, t0), in_group = min(min(seq.tok0 + i0 + kGroup, seq.tok0 + seq.S), t1) - group0;
+  const int p_last = seq.cb + group0 - seq.tok0 + in_group - 1;
+  if (in_group <= 0 || p_last < 0) return;
+  // the blocks that the group's last token scores, the workgroup's share of them, and this wavefront's tokens (maybe none)
+  const int scored = (int)min((int64_t)(p_last >> 4), row_words), tiles = (scored + 15) >> 4;
+  const int super0 = blockIdx.y * run, super1 = min(super0 + run, (tiles + 3) >> 2);
+  if (super0 >= super1) return;
+  const int first = group0 + wave * kTokens, n = min(kTokens, in_group - wave * kTokens);
+
   i32x4 af[NA][NF];
-  int eq[NA][4];
+  float scale[NA][4];
 #pragma unroll
   for (int a = 0; a < NA; ++a) {
-    const int tok = min(a * per_tile + (col >> log_rows), n - 1);
-    const E* const row = q + (size_t)(first + tok) * q_row_stride + (size_t)(g * G + min(col & (rows - 1), G - 1)) * D;
-    float size = 0.f, odd = 0.f;
+    auto row_of = [&](int x) { return (((int64_t)((n > 0 ? first : group0) - t0 + max(0, min(a * kPerTile + (x >> LOG), n - 1))) * Hkv + g) << LOG) + (x & ((1 << LOG) - 1)); };
+    const int8_t* const row = coded + row_of(col) * (2 * Dp) + quad * 16;
 #pragma unroll
-    for (int f = 0; f < NF; ++f) {
-      const int k = f * 64 + quad * 16;
-      float x[16];
-      load16(row, k < Dp ? k : k - Dp, D, x);
+    for (int f = 0; f < NF; ++f) af[a][f] = *reinterpret_cast<const i32x4*>(row + f * 64);
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        size = fmaxf(size, fabsf(x[i]));
-        odd = __builtin_fmaf(x[i], 0.f, odd);
-      }
-    }
-    size = fmaxf(size, __shfl_xor(size, 16));
-    size = fmaxf(size, __shfl_xor(size, 32));
-    odd += __shfl_xor(odd, 16);
-    odd += __shfl_xor(odd, 32);
-    const bool fine = odd == odd;
-    const int e = fine ? code_exponent(size) : 0;
+    for (int i = 0; i < 4; ++i) scale[a][i] = scales[row_of(quad * 4 + i)];
+  }
+  const int32_t* const table = block_table + (size_t)seq.b * bt_stride;
+  auto block_at = [&](int super) { return table[min((super * 4 + wave) * 16 + col, scored - 1)]; };
+  Records<NF> ahead;
+  ahead.ask(codes, exponents, block_at(super0), g, Hkv, lane);
+  int id = block_at(super0 + 1);
+  const __amdgpu_buffer_rsrc_t to_scores = score_rows(scores + ((int64_t)(first - t0) * Hkv + g) * row_words, max(n, 1), Hkv, row_words);
+  // tokens whose results a lane stores: of each row tile all four, two or one, or, where the rows of lanes hold copies, of one tile in two or four
+  constexpr int kPerRowTile = LOG == 0 ? 4 : LOG == 1 ? 2 : 1, kStores = LOG <= 2 ? NA * kPerRowTile : LOG == 3 ? NA / 2 : NA / 4;
+  int where[kStores];
 #pragma unroll
-    for (int f = 0; f < NF; ++f) {
-      const int k = f * 64 + quad * 16;
-      float x[16];
-      load16(row, k < Dp ? k : k - Dp, D, x);
+  for (int i = 0; i < kStores; ++i) {
+    const int tok = LOG == 0   ? i / 4 * 16 + quad * 4 + i % 4
+                    : LOG == 1 ? i / 2 * 8 + quad * 2 + i % 2
+                    : LOG == 2 ? i * 4 + quad
+                    : LOG == 3 ? (i * 2 + (quad & 1)) * 2 + (quad >> 1)
+                               : i * 4 + quad;
+    where[i] = tok < n ? (int)(tok * Hkv * row_words) * 4 + col * 4 : kNowhere;
+  }
+  auto put = [&](int i, float v, int e, int tile) { put_score<0>(to_scores, where[i], tile, v, e); };
+  for (int super = super0; super < super1; ++super) {
+    const int at = super & 1;
+    ahead.put(s_tiles[at][wave], lane);
+    if (lane < 16) s_e[at][wave][lane] = ahead.e;
+    ahead.ask(codes, exponents, id, g, Hkv, lane);  // (behind the last one: its last block)
+    id = block_at(super + 2);
+    __syncthreads();  // (who has passed it has read the tiles before the last ones: one barrier a turn)
+    if (n <= 0) continue;
+#pragma unroll 1
+    for (int k = 0; k < kScoreWaves; ++k) {
+      const int tile = super * 4 + k, e = s_e[at][k][col];
+      if (tile >= tiles) break;
+      i32x4 bf[NF];
+      Records<NF>::get(bf, s_tiles[at][k], col, quad);
+      float m[NA];
 #pragma unroll
-      for (int w = 0; w < 4; ++w) {
-        uint32_t packed = 0;
+      for (int a = 0; a < NA; ++a) {
+        i32x4 c = {0, 0, 0, 0};
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int c = fine ? (int)rintf(ldexpf(x[w * 4 + i], -e)) : 0;
-          packed |= ((uint32_t)(k < Dp ? max(c, 0) : min(c, 0)) & 0xffu) << (8 * i);
+        for (int f = 0; f < NF; ++f) c = __builtin_amdgcn_mfma_i32_16x16x64_i8(af[a][f], bf[f], c, 0, 0, 0);
+        float v[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = (float)c[i] * scale[a][i];
+        if constexpr (LOG == 0) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) put(a * 4 + i, v[i], e, tile);
+        } else if constexpr (LOG == 1) {
+          put(a * 2, fmaxf(v[0], v[1]), e, tile);
+          put(a * 2 + 1, fmaxf(v[2], v[3]), e, tile);
+        } else {
+          m[a] = fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3]));
+          if constexpr (LOG == 2) put(a, m[a], e, tile);
+          if constexpr (LOG >= 3) m[a] = max_of_rows16(m[a]);
+          if constexpr (LOG == 4) m[a] = max_of_rows32(m[a]);
         }
-        af[a][f][w] = (int)packed;
+      }
+      // (the rows of lanes hold copies: each stores another tile's)
+      if constexpr (LOG == 3)
+#pragma unroll
+        for (int a = 0; a < NA; a += 2) {
+          const float even = m[a], odd = m[a + 1];
+          put(a / 2, quad & 1 ? odd : even, e, tile);
+        }
+      if constexpr (LOG == 4) {
+        const float m0 = m[0], m1 = m[1], m2 = m[2], m3 = m[3], even = quad & 2 ? m2 : m0, odd = quad & 2 ? m3 : m1;
+        put(0, quad & 1 ? odd : even, e, tile);
       }
     }
-#pragma unroll
-    for (int i = 0; i < 4; ++i) eq[a][i] = __shfl(e, quad * 4 + i);
-  }
-
-  const int32_t* const table = block_table + (size_t)b * bt_stride;
-  const int tile1 = min(tile0 + tiles_per_wave, (scored + 15) >> 4);
-  auto block_at = [&](int tile) { return (int64_t)table[min(tile * 16 + col, scored - 1)]; };
-  uint32_t* const out = scores + ((int64_t)(first - t0) * Hkv + g) * row_words;
-  auto load = [&](i32x4 (&bf)[NF], int& e, int64_t blk) {
-    const int8_t* const rec = codes + ((size_t)blk * Hkv + g) * (2 * Dp) + quad * 16;
-#pragma unroll
-    for (int f = 0; f < NF; ++f) bf[f] = *reinterpret_cast<const i32x4*>(rec + f * 64);
-    e = exponents[(size_t)blk * Hkv + g];
-  };
-  i32x4 bf[NF], next[NF];
-  int e, e_next = 0;
-  load(bf, e, block_at(tile0));
-  int64_t blk = block_at(min(tile0 + 1, tile1 - 1));
-  for (int tile = tile0; tile < tile1; ++tile) {
-    load(next, e_next, blk);
-    blk = block_at(min(tile + 2, tile1 - 1));
-#pragma unroll
-    for (int a = 0; a < NA; ++a) {
-      if (a * per_tile >= n) break;
-      i32x4 c = {0, 0, 0, 0};
-#pragma unroll
-      for (int f = 0; f < NF; ++f) c = __builtin_amdgcn_mfma_i32_16x16x64_i8(af[a][f], bf[f], c, 0, 0, 0);
-      float v[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) v[i] = ldexpf((float)c[i], eq[a][i] + e);
-      // the maximum over a token's rows; it is then in v[0] (and, for one or two rows a token, v[2] or all four)
-      if (log_rows >= 1) v[0] = fmaxf(v[0], v[1]), v[2] = fmaxf(v[2], v[3]);
-      if (log_rows >= 2) v[0] = fmaxf(v[0], v[2]);
-      if (log_rows >= 3) v[0] = fmaxf(v[0], __shfl_xor(v[0], 16));
-      if (log_rows >= 4) v[0] = fmaxf(v[0], __shfl_xor(v[0], 32));
-      const int step = log_rows < 2 ? rows : 4;  // v[0], v[step], .. are tokens of their own
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        if (i & (step - 1)) continue;
-        const int row = quad * 4 + i, tok = a * per_tile + (row >> log_rows);
-        if ((row & (rows - 1)) == 0 && tok < n) out[(int64_t)tok * Hkv * row_words + tile * 16 + col] = ordered(e == kNotFinite ? INFINITY : v[i]);
-      }
-    }
-#pragma unroll
-    for (int f = 0; f < NF; ++f) bf[f] = next[f];
-    e = e_next;
   }
 }
 
-constexpr int kBins = 2048, kPer = 8;  // bins of a histogram; numbers of a thread at a time
-
-// Inclusive sums over the workgroup of two counts; `all`: their totals.
-template <int THREADS>
-__device__ __forceinline__ int2 sum_over_threads(int2 x, int2* s_wave, int2& all) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  x.x = lanes_prefix_sum(x.x);
-  x.y = lanes_prefix_sum(x.y);
-  __syncthreads();
-  if (lane == 63) s_wave[wave] = x;
-  __syncthreads();
-  all = int2{0, 0};
-#pragma unroll
-  for (int w = 0; w < THREADS / 64; ++w) {
-    const int2 y = s_wave[w];
-    if (w < wave) x.x += y.x, x.y += y.y;
-    all.x += y.x, all.y += y.y;
-  }
-  return x;
-}
-
-// Grid: K/V heads, tokens t0 .. t1 - 1.
-template <int THREADS>
-__global__ __launch_bounds__(THREADS) void choose_kernel(const uint32_t* __restrict__ scores, int64_t row_words, Tokens tk, int32_t* __restrict__ blocks, int K,
-                                                         int keep_first, int keep_last, int Hkv, int t0) {
-  __shared__ int s_hist[kBins];
-  __shared__ int2 s_wave[THREADS / 64];
-  __shared__ uint32_t s_low[THREADS / 64], s_high[THREADS / 64];
-  __shared__ int s_bin, s_above;
-  const int g = blockIdx.x, t = t0 + blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+// A row to every WAVES wavefronts, rows (token, K/V head) from token t0 on.
+template <int WAVES, int PER, int BINS>
+__global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void choose_kernel(const float* __restrict__ scores, int64_t row_words, Tokens tk, Chosen to, int Hkv,
+                                                                               int t0, int rows) {
+  constexpr int kAtOnce = WAVES == 1 ? 4 : 1;  // rows of a workgroup
+  __shared__ ChooseShared<WAVES, BINS> s[kAtOnce];
+  const int of = WAVES == 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : 0, wave = WAVES == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int r = blockIdx.x * kAtOnce + of, t = t0 + r / Hkv, tid = threadIdx.x - of * 64;
+  if (r >= rows) return;
   int p;
   if (tk.cu_q) {
     const SeqOf seq = find_sequence(tk.cu_q, tk.ctx_before, tk.B, t, [](int cu, int) { return (long long)cu; });
@@ -212,139 +600,74 @@ __global__ __launch_bounds__(THREADS) void choose_kernel(const uint32_t* __restr
   } else {
     p = tk.ctx_before[t];
   }
-  const int n = p < 0 ? 0 : (int)min((int64_t)(p >> 4) + 1, row_words);
-  int32_t* const out = blocks + ((int64_t)t * Hkv + g) * K;
-  if (n <= K) {
-    for (int i = tid; i < K; i += THREADS) out[i] = i < n ? i : -1;
+  const int n = p < 0 ? 0 : (int)min((int64_t)(p >> 4), row_words) + 1;
+  int32_t* const out = to.blocks + ((int64_t)t0 * Hkv + r) * to.K;
+  if (n <= to.K) {
+    for (int i = tid; i < to.K; i += WAVES * 64) out[i] = i < n ? i : -1;
     return;
   }
-  const uint32_t* const row = scores + ((int64_t)(t - t0) * Hkv + g) * row_words;
-  constexpr int kSpan = THREADS * kPer;
-  const int c0 = keep_first, c1 = n - keep_last;  // the blocks that compete
-  int need = K - keep_first - keep_last;
-  uint32_t key[kPer];
-  // numbers base + 8 tid .. + 7: 0 behind the last block, the largest for what is kept anyway
-  auto load = [&](int base) {
-    const int j0 = base + tid * kPer;
-#pragma unroll
-    for (int w = 0; w < kPer / 4; ++w) {
-      u32x4 x = {0u, 0u, 0u, 0u};
-      if (j0 + 4 * w < c1) x = *reinterpret_cast<const u32x4*>(row + j0 + 4 * w);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int j = j0 + 4 * w + i;
-        key[4 * w + i] = j >= n ? 0u : j < c0 || j >= c1 ? ~0u : x[i];
-      }
-    }
-  };
-  const bool once = n <= kSpan;  // all of them in registers
-  load(0);
-  // the smallest number that is chosen and how many equal to it are: `at` and `need`
-  uint32_t at = ~0u;
-  bool whole = true;  // all numbers from `at` on are chosen
-  if (need > 0) {
-    uint32_t low = ~0u, high = 0u;
-    for (int base = 0; base < n; base += kSpan) {
-      if (!once) load(base);
-#pragma unroll
-      for (int i = 0; i < kPer; ++i)
-        if (key[i] != 0u && key[i] != ~0u) low = min(low, key[i]), high = max(high, key[i]);
-    }
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) low = min(low, (uint32_t)__shfl_xor((int)low, o)), high = max(high, (uint32_t)__shfl_xor((int)high, o));
-    if (lane == 0) s_low[wave] = low, s_high[wave] = high;
-    __syncthreads();
-#pragma unroll
-    for (int w = 0; w < THREADS / 64; ++w) low = min(low, s_low[w]), high = max(high, s_high[w]);
-    uint32_t span = high - low;  // numbers low .. low + span
-    for (;;) {
-      const int shift = max(0, 32 - __clz((int)(span | 1u)) - 11);
-      __syncthreads();
-      for (int i = tid; i < kBins; i += THREADS) s_hist[i] = 0;
-      __syncthreads();
-      for (int base = 0; base < n; base += kSpan) {
-        if (!once) load(base);
-#pragma unroll
-        for (int i = 0; i < kPer; ++i)
-          if (key[i] != 0u && key[i] != ~0u && key[i] >= low && key[i] - low <= span) atomicAdd(&s_hist[(key[i] - low) >> shift], 1);
-      }
-      __syncthreads();
-      // from the last bin down: the one in which the count reaches `need`
-      constexpr int kBinsPer = kBins / THREADS;
-      int mine = 0, bins[kBinsPer];
-#pragma unroll
-      for (int i = 0; i < kBinsPer; ++i) {
-        bins[i] = s_hist[kBins - 1 - (tid * kBinsPer + i)];
-        mine += bins[i];
-      }
-      int2 all;
-      int above = sum_over_threads<THREADS>(int2{mine, 0}, s_wave, all).x - mine;
-#pragma unroll
-      for (int i = 0; i < kBinsPer; ++i) {
-        if (above < need && above + bins[i] >= need) s_bin = kBins - 1 - (tid * kBinsPer + i), s_above = above;
-        above += bins[i];
-      }
-      __syncthreads();
-      const int bin = s_bin;
-      need -= s_above;
-      at = low + ((uint32_t)bin << shift);
-      whole = need == s_hist[bin];
-      if (whole || shift == 0) break;
-      low = at;
-      span = (1u << shift) - 1u;
-    }
-  }
-  // indices in their order: all numbers above `at`, and of those equal to it the first `need`
-  int done = 0, equal = 0;
-  for (int base = 0; base < n; base += kSpan) {
-    if (!once) load(base);
-    int2 mine = {0, 0};
-#pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-      const bool sure = key[i] != 0u && (whole ? key[i] >= at : key[i] > at);
-      mine.x += sure ? 1 : 0;
-      mine.y += !whole && key[i] == at ? 1 : 0;
-    }
-    int2 all;
-    const int2 upto = sum_over_threads<THREADS>(mine, s_wave, all);
-    int sure_before = done + upto.x - mine.x, equal_before = equal + upto.y - mine.y;
-#pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-      const bool sure = key[i] != 0u && (whole ? key[i] >= at : key[i] > at), same = !whole && key[i] == at;
-      if (sure || (same && equal_before < need)) out[sure_before + min(equal_before, need)] = base + tid * kPer + i;
-      sure_before += sure ? 1 : 0;
-      equal_before += same ? 1 : 0;
-    }
-    done += all.x;
-    equal += all.y;
-  }
+  const float* const row = scores + (int64_t)r * row_words;
+  choose<WAVES, PER>([&](int j) { return row[j]; }, wave, n, to.keep_first, n - to.keep_last, to.K, out, s[of]);
 }
 
-template <typename E, int NF, int NA>
-void launch_scores(const SelectArgs& a, const Tokens& tk, const int8_t* codes, const int8_t* exponents, int64_t row_words, int log_rows, int group, int t0, int t1,
-                   hipStream_t s) {
-  const int G = a.Hq / a.Hkv, tiles = (int)(row_words / 16);
+// Tokens [t0, t1) of a call, and what of it the launches need.
+struct Slab {
+  const SelectArgs& a;
+  const Tokens tk;
+  const int8_t *codes, *exponents;
+  int64_t row_words;
+  int log_rows, t0, t1;
+  hipStream_t s;
   // tokens t of sequence b are in unit t / group + b or the one in front of it
-  const int unit0 = a.cu_q ? std::max(0, t0 / group - 1) : t0, units = a.cu_q ? t1 / group + a.B + 1 - unit0 : t1 - t0;
+  int unit0(int group) const { return a.cu_q ? std::max(0, t0 / group - 1) : t0; }
+  int units(int group) const { return a.cu_q ? t1 / group + a.B + 1 - unit0(group) : t1 - t0; }
+};
+
+template <typename E, int NF, int PER>
+void launch_step(const Slab& x) {
+  const SelectArgs& a = x.a;
+  const int group = a.cu_q ? 16 >> x.log_rows : 1, units = x.units(group), tiles = (int)(x.row_words / 16);
   // as many wavefronts as the device takes at once, then more tiles to one
-  const int64_t waves = (int64_t)units * a.Hkv * tiles, room = (int64_t)a.num_cu * 16;
+  const int64_t waves = (int64_t)units * a.Hkv * tiles, room = (int64_t)a.num_cu * 32;
   const int per_wave = (int)std::min<int64_t>(std::max<int64_t>(1, waves / room), 16), runs = (tiles + kScoreWaves * per_wave - 1) / (kScoreWaves * per_wave);
-  hipLaunchKernelGGL((score_kernel<E, NF, NA>), dim3((unsigned)a.Hkv, (unsigned)runs, (unsigned)units), dim3(kScoreThreads), 0, s, (const E*)a.q, a.q_row_stride,
-                     codes, exponents, tk, a.block_table, a.bt_stride, a.scores, row_words, G, log_rows, a.Hkv, a.D, group, unit0, t0, t1, per_wave);
+  hipLaunchKernelGGL((score_step_kernel<E, NF, PER>), dim3((unsigned)a.Hkv, (unsigned)runs, (unsigned)units), dim3(kScoreThreads), 0, x.s, (const E*)a.q,
+                     a.q_row_stride, x.codes, x.exponents, x.tk, a.block_table, a.bt_stride, a.scores, x.row_words, a.Hq / a.Hkv, x.log_rows, a.Hkv, a.D, group,
+                     x.unit0(group), x.t0, x.t1, per_wave, Chosen{a.blocks, a.num_selected, a.keep_first, a.keep_last}, a.counters);
+}
+
+template <typename E, int NF>
+void launch_prompts(const Slab& x) {
+  const SelectArgs& a = x.a;
+  const int64_t rows = ((int64_t)(x.t1 - x.t0) * a.Hkv) << x.log_rows;
+  hipLaunchKernelGGL((code_kernel<E, NF>), dim3((unsigned)((rows + 15) / 16)), dim3(256), 0, x.s, (const E*)a.q, a.q_row_stride, a.coded, a.scales, rows, a.Hq / a.Hkv,
+                     x.log_rows, a.Hkv, a.D, x.t0);
+  auto go = [&](auto log) {
+    constexpr int LOG = decltype(log)::value, group = prompt_tokens(LOG) * kScoreWaves;
+    const int units = x.units(group), tiles = (int)(x.row_words / 16);
+    // four workgroups per CU; a workgroup walks eight tiles at least
+    const int64_t wgs = ((int64_t)(x.t1 - x.t0) / group + 1) * a.Hkv;
+    const int runs = (int)std::max<int64_t>(1, std::min<int64_t>((4 * a.num_cu + wgs - 1) / wgs, tiles / 8)), run = ((tiles + 3) / 4 + runs - 1) / runs;
+    hipLaunchKernelGGL((score_prompt_kernel<NF, LOG>), dim3((unsigned)a.Hkv, (unsigned)(((tiles + 3) / 4 + run - 1) / run), (unsigned)units), dim3(kScoreThreads), 0, x.s, a.coded,
+                       a.scales, x.codes, x.exponents, x.tk, a.block_table, a.bt_stride, a.scores, x.row_words, a.Hkv, x.unit0(group), x.t0, x.t1, run);
+  };
+  switch (x.log_rows) {
+    case 0: return go(std::integral_constant<int, 0>());
+    case 1: return go(std::integral_constant<int, 1>());
+    case 2: return go(std::integral_constant<int, 2>());
+    case 3: return go(std::integral_constant<int, 3>());
+    default: return go(std::integral_constant<int, 4>());
+  }
 }
 
 template <typename E>
-void launch_typed(const SelectArgs& a, const Tokens& tk, const int8_t* codes, const int8_t* exponents, int64_t row_words, int t0, int t1, hipStream_t s) {
-  const int G = a.Hq / a.Hkv;
-  int log_rows = 0;
-  while ((1 << log_rows) < G) ++log_rows;
-  const bool prompts = a.cu_q && a.T > 2 * a.B;
+void launch_scores(const Slab& x, bool choose_too) {
   auto steps = [&](auto nf) {
-    constexpr int NF = decltype(nf)::value, NA = NF <= 4 ? 4 : 2;
-    if (prompts) launch_scores<E, NF, NA>(a, tk, codes, exponents, row_words, log_rows, NA * (16 >> log_rows), t0, t1, s);
-    else launch_scores<E, NF, 1>(a, tk, codes, exponents, row_words, log_rows, a.cu_q ? 16 >> log_rows : 1, t0, t1, s);
+    constexpr int NF = decltype(nf)::value;
+    if (x.a.cu_q && x.a.T > 2 * x.a.B) launch_prompts<E, NF>(x);
+    else if (choose_too) launch_step<E, NF, kFusedBlocks / kScoreThreads>(x);
+    else launch_step<E, NF, 0>(x);
   };
-  switch (summary_channels(a.D) / 32) {
+  switch (summary_channels(x.a.D) / 32) {
     case 1: return steps(std::integral_constant<int, 1>());
     case 2: return steps(std::integral_constant<int, 2>());
     case 3: return steps(std::integral_constant<int, 3>());
@@ -360,22 +683,27 @@ void launch_typed(const SelectArgs& a, const Tokens& tk, const int8_t* codes, co
 
 hipError_t launch_block_select(const ecoserve_layout& L, const SelectArgs& a, const void* summary, int32_t max_ctx_len, hipStream_t s) {
   const int8_t* const codes = (const int8_t*)summary;
-  const int8_t* const exponents = codes + summary_code_bytes(L);
-  const Tokens tk = {a.cu_q, a.ctx_before, a.B, a.T};
+  const Chosen to = {a.blocks, a.num_selected, a.keep_first, a.keep_last};
   const int64_t row_words = select_row_words(max_ctx_len);
-  const int at_a_time = select_tokens_at_a_time(L.num_kv_heads, a.T, max_ctx_len);
+  const int at_a_time = select_tokens_at_a_time(L, a.T, max_ctx_len);
+  // (rows of no more blocks than are asked for, whatever the lengths: nothing is scored)
+  const bool scored = row_words > a.num_selected, fused = scored && !a.cu_q && row_words <= kFusedBlocks;
   for (int t0 = 0; t0 < a.T; t0 += at_a_time) {
     const int t1 = std::min(a.T, t0 + at_a_time);
-    // (no more blocks than are asked for, whatever the lengths: nothing is scored)
-    if (row_words > a.num_selected) {
-      if (L.dtype == ECOSERVE_BF16) launch_typed<uint16_t>(a, tk, codes, exponents, row_words, t0, t1, s);
-      else launch_typed<float>(a, tk, codes, exponents, row_words, t0, t1, s);
+    const Slab x = {a, {a.cu_q, a.ctx_before, a.B, a.T}, codes, codes + summary_code_bytes(L), row_words, select_log_rows(L), t0, t1, s};
+    if (scored) {
+      if (L.dtype == ECOSERVE_BF16) launch_scores<uint16_t>(x, fused);
+      else launch_scores<float>(x, fused);
     }
-    const dim3 grid((unsigned)a.Hkv, (unsigned)(t1 - t0));
-    if (row_words <= 256 * kPer)
-      hipLaunchKernelGGL((choose_kernel<256>), grid, dim3(256), 0, s, a.scores, row_words, tk, a.blocks, a.num_selected, a.keep_first, a.keep_last, a.Hkv, t0);
-    else
-      hipLaunchKernelGGL((choose_kernel<1024>), grid, dim3(1024), 0, s, a.scores, row_words, tk, a.blocks, a.num_selected, a.keep_first, a.keep_last, a.Hkv, t0);
+    if (fused) continue;
+    const int rows = (t1 - t0) * a.Hkv;
+    auto go = [&](auto kernel, int threads, int at_once) {
+      hipLaunchKernelGGL(kernel, dim3((unsigned)((rows + at_once - 1) / at_once)), dim3(threads), 0, s, a.scores, row_words, x.tk, to, a.Hkv, t0, rows);
+    };
+    if (row_words <= 2048) go(&choose_kernel<1, 32, 512>, 256, 4);
+    else if (row_words <= 8192) go(&choose_kernel<16, 8, 1024>, 1024, 1);
+    else if (row_words <= 32768) go(&choose_kernel<16, 32, 1024>, 1024, 1);
+    else go(&choose_kernel<16, 0, 1024>, 1024, 1);
   }
   return hipGetLastError();
 }

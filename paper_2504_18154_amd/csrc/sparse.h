@@ -7,17 +7,30 @@
 
 #include <algorithm>
 
+#include "summary.h"
+
 namespace eco {
 
-// Selection: one 32-bit number per (token, K/V head, block), rows of whole tiles of 16 blocks.
+// Selection: one fp32 score per (token, K/V head, block), rows of whole tiles of 16 blocks.
 inline int64_t select_row_words(int32_t max_ctx_len) { return ((int64_t)max_ctx_len + 255) / 256 * 16; }
-// Tokens whose scores are held at a time: as many as 192 MiB take, which stays in the last-level cache (256 MiB) between the two launches.
-inline int32_t select_tokens_at_a_time(int32_t Hkv, int32_t T, int32_t max_ctx_len) {
-  const int64_t row_bytes = 4 * select_row_words(max_ctx_len) * Hkv;
-  return (int32_t)std::max<int64_t>(1, std::min<int64_t>({(int64_t)T, ((int64_t)192 << 20) / row_bytes, 32768}));
+constexpr int32_t kFusedBlocks = 2048;  // rows of a step up to which the launch that scores them also chooses
+// Rows of the products that a token takes per K/V head: 1 << this, its heads padded to a power of two.
+inline int32_t select_log_rows(const ecoserve_layout& L) {
+  int32_t log = 0;
+  while (L.num_kv_heads << log < L.num_q_heads) ++log;
+  return log;
 }
-inline size_t select_workspace_bytes(int32_t Hkv, int32_t T, int32_t max_ctx_len) {
-  return (size_t)select_tokens_at_a_time(Hkv, T, max_ctx_len) * Hkv * select_row_words(max_ctx_len) * 4;
+// Bytes of a token: its scores, and its query heads as whole numbers with a scale each.
+inline int64_t select_score_bytes(const ecoserve_layout& L, int32_t max_ctx_len) { return 4 * select_row_words(max_ctx_len) * L.num_kv_heads; }
+inline int64_t select_coded_bytes(const ecoserve_layout& L) { return ((int64_t)L.num_kv_heads << select_log_rows(L)) * (2 * summary_channels(L.head_dim)); }
+inline int64_t select_scale_bytes(const ecoserve_layout& L) { return ((int64_t)L.num_kv_heads << select_log_rows(L)) * 4; }
+// Tokens whose scores are held at a time: as many as 192 MiB take, which stay in the last-level cache (256 MiB) between the launches.
+inline int32_t select_tokens_at_a_time(const ecoserve_layout& L, int32_t T, int32_t max_ctx_len) {
+  return (int32_t)std::max<int64_t>(1, std::min<int64_t>({(int64_t)T, ((int64_t)192 << 20) / select_score_bytes(L, max_ctx_len), 32768}));
+}
+inline size_t select_workspace_bytes(const ecoserve_layout& L, int32_t T, int32_t max_ctx_len) {
+  const int64_t bytes = select_score_bytes(L, max_ctx_len) + select_coded_bytes(L) + select_scale_bytes(L);
+  return ((size_t)select_tokens_at_a_time(L, T, max_ctx_len) * bytes + 15) / 16 * 16;
 }
 
 struct SelectArgs {
@@ -27,7 +40,11 @@ struct SelectArgs {
   int32_t bt_stride;
   int32_t* blocks;
   int32_t num_selected, keep_first, keep_last, B, T, Hq, Hkv, D, num_cu;
-  uint32_t* scores;
+  // the workspace: scores, rows of whole numbers (16-byte aligned: scores are whole tiles), their scales
+  float* scores;
+  int8_t* coded;
+  float* scales;
+  uint32_t* counters;  // one per (token, K/V head) where there is one token per sequence, zero between launches
 };
 
 // Attention over listed blocks: a list is cut into parts, one workgroup each, where there are few (token, K/V head)s.  Two

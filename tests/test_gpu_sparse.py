@@ -202,7 +202,7 @@ def test_equal_scores_and_blocks_that_are_not_finite():
     b.ctx.close()
 
 
-@pytest.mark.parametrize("blocks", [2047, 2048, 2050, 8190, 8193, 20011])
+@pytest.mark.parametrize("blocks", [2047, 2048, 2050, 8190, 8193, 20011, 33333])
 def test_long_contexts(blocks):
     """Around the numbers of blocks that the ways through the histogram change at; scores in narrow and wide ranges, many of them equal."""
     from paper_2504_18154_amd import binding
@@ -225,6 +225,9 @@ def test_long_contexts(blocks):
             lists = torch.full((2, Hkv, K), -7, dtype=torch.int32, device="cuda")
             ctx.block_select(q.cuda(), summary, dev_i32(before), dev_i32(table), lists, blocks * 16, keep_first=first, keep_last=last)
             got = lists.cpu().numpy()
+            lists.fill_(-7)                                   # (the same as a batch of prompts of one token)
+            ctx.block_select(q.cuda(), summary, dev_i32(before), dev_i32(table), lists, blocks * 16, keep_first=first, keep_last=last, cu_q=dev_i32([0, 1, 2]))
+            assert np.array_equal(lists.cpu().numpy(), got)
             for t in range(2):
                 n = before[t] // 16 + 1
                 ids = table[t, :n - 1]
@@ -242,8 +245,7 @@ def test_tokens_in_several_passes(monkeypatch):
     blocks, T = 30000, 130
     rng = np.random.default_rng(3)
     ctx = binding.Context(16, 16, 32, 500, "bf16", 3, blocks)
-    per = binding.select_workspace_bytes(ctx.layout, 1 << 20, blocks * 16) // (16 * 4 * blocks)
-    assert per < T                                            # 192 MiB of 1.9 MB each
+    assert binding.select_workspace_bytes(ctx.layout, 1 << 20, blocks * 16) < binding.select_workspace_bytes(ctx.layout, 1, blocks * 16) * T   # (192 MiB of scores, 1.9 MB each)
     summary = torch.randint(-100, 100, ctx.new_summary().shape, dtype=torch.int8, device="cuda")
     table = rng.integers(0, 500, size=(3, blocks)).astype(np.int32)
     new = np.array([60, 0, 70])

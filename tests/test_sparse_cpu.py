@@ -74,10 +74,11 @@ def test_sizes():
     assert b.summary_bytes(b.make_layout(4, 2, 72, 10, "bf16")) == (10 * 2 * (2 * 96 + 1) + 15) // 16 * 16
     assert b.summary_bytes(b.make_layout(5, 2, 64, 16, "f32")) == 0
     lay = b.make_layout(40, 8, 128, 1000, "bf16")
-    assert b.select_workspace_bytes(lay, 1, 20000) == 8 * 1264 * 4      # 1250 blocks, in whole tiles of 16
+    coded = 8 * 8 * (256 + 4)            # per token: its heads, eight places per K/V head, as whole numbers with a scale
+    assert b.select_workspace_bytes(lay, 1, 20000) == 8 * 1264 * 4 + coded      # 1250 blocks, in whole tiles of 16
     assert b.select_workspace_bytes(lay, 0, 20000) == 0
-    assert b.select_workspace_bytes(lay, 100000, 131072) <= 192 << 20
-    assert b.select_workspace_bytes(lay, 3, (1 << 31) - 1) == 8 * (1 << 27) * 4   # (one token at a time, however long)
+    assert b.select_workspace_bytes(lay, 100000, 131072) == 768 * (262144 + coded)     # 192 MiB of scores
+    assert b.select_workspace_bytes(lay, 3, (1 << 31) - 1) == 8 * (1 << 27) * 4 + coded   # (one token at a time, however long)
 
 
 def test_rotations_that_cannot_be():

@@ -524,7 +524,7 @@ int ecoserve_attn_sparse(ecoserve_ctx* c, const void* q, int64_t q_row_stride, c
   DeviceGuard guard(c->device);
   if (!guard.ok) return ECOSERVE_EHIP;
   const SparseArgs a = {q, (int32_t)q_row_stride, k_cache, v_cache, cu_q, ctx_before, block_table, bt_stride, blocks, num_selected, out, lse, B, T,
-                        L.num_q_heads, L.num_kv_heads, L.head_dim, c->num_cu, L.dtype, c->scale * kLog2e, (float*)workspace};
+                        L.num_q_heads, L.num_kv_heads, L.head_dim, c->num_cu, L.dtype, c->scale * kLog2e, (float*)workspace, c->ws_count};
   return launch_attn_sparse(a, (hipStream_t)stream) == hipSuccess ? ECOSERVE_OK : ECOSERVE_EHIP;
 }
 

@@ -73,6 +73,7 @@ struct SparseArgs {
   int32_t B, T, Hq, Hkv, D, num_cu, dtype;
   float scale_log2e;
   float* states;
+  uint32_t* counters;  // one per (token, K/V head) of lists in parts (at most one per CU), zero between launches
 };
 
 }  // namespace eco

@@ -274,14 +274,15 @@ def _attend(b: Batch, lists, ragged=True, with_lse=True, q=None, pad=0, **kw):
     return out, lse
 
 
-def _compare(b: Batch, lists, out, lse, q=None, name="", parts_of_weights=True):
+def _compare(b: Batch, lists, out, lse, q=None, name="", tokens=None, rounded_weights=False):
     """Errors that the kernel makes.  A score: the fp32 sum of D products (bounded by D + 2 roundings of the sum of |q k|) and its scaling.
     A weight: twice that, the exponential (2^-21 in all), for bf16 its two parts (2^-15).  The sums over n keys: n + 8 roundings.
-    A relative error d of all weights moves the result by at most 2 d sum w |v|.  Then one rounding to the type."""
+    A relative error d of all weights moves the result by at most 2 d sum w |v|.  Then one rounding to the type.
+    rounded_weights: the weights of the values (not those of the sum) were rounded to bf16, 2^-8 each."""
     q = (b.q if q is None else q).float().cpu().numpy()
     o = out.float().cpu().numpy().astype(np.float64)
     worst = 0.0
-    for t in range(b.T):
+    for t in range(b.T) if tokens is None else tokens:
         s, p = b.seq[t], b.pos[t]
         for g in range(b.Hkv):
             keys, vals = b.sequence(s, b.keys, g, p + 1), b.sequence(s, b.vals, g, p + 1)
@@ -291,7 +292,7 @@ def _compare(b: Batch, lists, out, lse, q=None, name="", parts_of_weights=True):
             es = (b.D + 4) * 2.0 ** -24 * product
             d = 2 * es + 2.0 ** -21 + (2.0 ** -15 if b.dtype == "bf16" else 0) + (len(at) + 8) * 2.0 ** -24
             half = torch.finfo(b.dt).eps / 2
-            bound = half * np.abs(ref) + (1 + half) * 2 * d[:, None] * size
+            bound = half * np.abs(ref) + (1 + half) * (2 * d[:, None] + (2.0 ** -8 if rounded_weights else 0)) * size
             err = np.abs(o[t, rows] - ref)
             assert (err <= bound).all(), (name, t, g, float(err.max()), float((err / np.maximum(bound, 1e-300)).max()))
             worst = max(worst, float((err / np.maximum(bound, 1e-300)).max()))
@@ -346,6 +347,76 @@ def test_lists_of_many_lengths_and_parts(B, K):
     out, lse = _attend(b, lists, ragged=False)
     _compare(b, lists, out, lse, name="decode")
     assert torch.equal(out, _attend(b, lists, ragged=False)[0])
+    b.ctx.close()
+
+
+def _of_prompts(b: Batch):
+    """Tokens at the edges of sequences and groups, and every 37th."""
+    ends = np.cumsum(b.new)
+    edges = {t for e in ends for t in (e - 1, e, e + 1, e - 31, e + 16, e + 31, e + 32)} | set(range(0, b.T, 37)) | {0, 1, 15, 16, 31, 32, 33}
+    return sorted(t for t in edges if 0 <= t < b.T)
+
+
+GROUPS = [(128, 16, 2, [100, 0, 2600]), (128, 5, 1, [2100, 2050]), (128, 3, 3, [1400]), (128, 16, 1, [4200]), (128, 12, 4, [1030]), (72, 14, 2, [3700]), (64, 8, 8, [40, 1200]),
+          (96, 6, 2, [2800]), (160, 9, 1, [3400]), (216, 4, 2, [1300]), (256, 8, 1, [2100])]
+
+
+@pytest.mark.parametrize("D,Hq,Hkv,new", GROUPS, ids=[f"d{a[0]}-{a[1]}x{a[2]}" for a in GROUPS])
+def test_many_tokens_of_prompts(D, Hq, Hkv, new):
+    """The kernel that shares the blocks of neighbouring tokens (524288 channels of K/V rows on 256 CUs): lists in any order with entries that hold no keys; lists that agree, as
+    those of real prompts do; tails that nobody has written."""
+    rng = np.random.default_rng(D)
+    say(f"D {D}, heads {Hq}/{Hkv}: {new} tokens")
+    b = Batch("bf16", D, Hq, Hkv, [17 + 100 * i for i in range(len(new))], new, seed=D)
+    assert b.T * Hkv * D >= 2048 * 256
+    some = _of_prompts(b)
+    lists = _random_lists(b, 7, rng)
+    out, lse = _attend(b, lists)
+    _compare(b, lists, out, lse, name="lists in any order", tokens=some, rounded_weights=True)
+    assert torch.equal(out, _attend(b, lists)[0])
+    lists[:] = -1
+    for t in range(b.T):                                                    # the first block, the last two, and four that 64 tokens agree on but for one
+        n = b.pos[t] // 16 + 1
+        for g in range(Hkv):
+            r = np.random.default_rng((t // 64, g))
+            mine = sorted({0, n - 1, max(n - 2, 0)} | set(r.choice(max(n, 4), 3).tolist()) | {int(rng.integers(n))})
+            lists[t, g, :len(mine)] = mine
+    out, lse = _attend(b, lists)
+    _compare(b, lists, out, lse, name="lists that agree", tokens=some, rounded_weights=True)
+    b.ctx.close()
+
+
+def test_many_tokens_of_prompts_and_values_that_are_not_finite():
+    """In the blocks that tokens side by side do not share: an infinite value and an undefined key reach the rows that list them alone; blocks that are listed twice; rows behind the
+    last sequence; queries as slices of wider rows; a scale of its own."""
+    rng = np.random.default_rng(1)
+    b = Batch("bf16", 128, 16, 2, [64, 640], [900, 1200], seed=5, scale=0.2)
+    lists = _random_lists(b, 5, rng, order=False)
+    lists[1000, 0] = [3, 5, 3, 0, -1]                                       # (twice: its group goes the long way)
+    some = sorted(set(_of_prompts(b)) | set(range(990, 1030)))
+    wide = torch.full((b.T + 5, 24, 128), float("nan"), dtype=b.dt, device="cuda")
+    wide[:b.T, 4:20] = b.q.cuda()
+    padded = np.concatenate([lists, np.zeros((5, 2, 5), np.int32)])
+    out, lse = _attend(b, padded, q=wide[:, 4:20], pad=5)
+    _compare(b, lists, out, lse, name="a block twice", tokens=some, rounded_weights=True)
+    assert out[b.T:].isnan().all() and lse[b.T:].isnan().all()
+    again, _ = _attend(b, padded, q=wide[:, 4:20], pad=5, with_lse=False)
+    assert torch.equal(again[:b.T], out[:b.T])
+    lists[1000, 0, 2] = 9
+    inf_block, nan_block = int(b.table[1, 4]), int(b.table[1, 11])
+    b.vals[inf_block, 0, 3, 7] = float("inf")
+    b.keys[nan_block, 1, 5, 2] = float("nan")
+    b.upload()
+    got, got_lse = _attend(b, lists)
+    second = b.seq == 1
+    has_inf, has_nan = (lists[:, 0] == 4).any(1) & second, (lists[:, 1] == 11).any(1) & second
+    assert has_inf.any() and (~has_inf & second).any() and has_nan.any()
+    o = got.float().cpu().numpy()
+    assert np.isposinf(o[has_inf][:, :8, 7]).all() and np.isfinite(np.delete(o[has_inf][:, :8], 7, 2)).all()
+    assert np.isnan(o[has_nan][:, 8:]).all()
+    assert np.isfinite(o[~has_inf][:, :8]).all() and np.isfinite(o[~has_nan][:, 8:]).all()
+    clean = [t for t in some if not has_inf[t] and not has_nan[t]]
+    _compare(b, lists, got, got_lse, name="beside values that are not finite", tokens=clean, rounded_weights=True)
     b.ctx.close()
 
 

@@ -8,7 +8,9 @@
 // The rows of a product are (token, head of the group), a token's padded to a power of two with copies of its last head, so that the
 // maximum over the heads is within a lane's four results and over at most two exchanges; its columns are 16 blocks, 16 bytes a lane and step, straight into
 // operand layout.
-//   score_step_kernel    few tokens per sequence: a workgroup codes up to 16 rows into LDS and walks a run of block tiles.  Bound by reading the records.
+//   score_step_kernel    few tokens per sequence: a workgroup codes up to 16 rows into LDS and walks a run of block tiles.  Bound by reading the
+//                        records, 256 bytes of each of a table's scattered blocks (32 sequences of 16384 to 131000 tokens, 8 heads of 128, 0.3 GB: 64 us,
+//                        4.7 TB/s; blocks in order: 51).
 //   code_kernel, score_prompt_kernel   prompts: the rows are coded once, into the workspace; a wavefront has four tiles of them in registers.  Bound by the
 //                        products and what is done with their results.
 //   choose               a wavefront or more per (token, K/V head), the scores in registers.  For steps over short contexts the workgroup that is
@@ -146,7 +148,7 @@ __device__ __forceinline__ void together() {
 // again each time.  A histogram between the smallest and the largest number finds the bin in which the last one to be chosen is.  Up to 64 numbers of
 // that bin are then compared with one another, a lane each, bit by bit; of more, another histogram is made.  Every wavefront does all of that but the counting
 // by itself: a barrier or two a round.  What bounds it is instructions, their fetching where a row is alone: hence no branch per number.
-// (895 tokens, 8 K/V heads, about 1500 blocks, a wavefront a row, us: loads and counts under branches 36.1, loads at once 27.0, so 16.0.)
+// (895 tokens, 8 K/V heads, about 1500 blocks, a wavefront a row, us: loads and counts under branches 36.1, loads at once 27.0, so 20.2.)
 template <int WAVES, int PER, int BINS, typename Ask>
 __device__ __forceinline__ void choose(Ask ask, int wave, int n, int c0, int c1, int K, int32_t* __restrict__ out, ChooseShared<WAVES, BINS>& s) {
   constexpr int THREADS = WAVES * 64, kMine = BINS / 64, kLog = BINS == 1024 ? 10 : 9, kAll = 2 * (BINS + 64);
@@ -292,8 +294,8 @@ __device__ __forceinline__ void put_score(__amdgpu_buffer_rsrc_t to, int where, 
 }
 
 // A tile of 16 records, from memory to LDS to operands.  A lane's operand is 16 bytes of "its" block, so loads straight into operand layout would have
-// neighbouring lanes ask different lines, 64 requests an instruction (and they bound both kernels: 62 us of 895 tokens, 64 us of 32 long contexts);
-// so lanes ask for 64 bytes in a row per four, and LDS turns them over.  Unit s (16 bytes) of block c lies at unit s ^ mix(c) of its
+// neighbouring lanes ask different lines, 64 requests an instruction (895 tokens: 62 us; steps over 32 long contexts: 64);
+// so lanes ask for 64 bytes in a row per four, and LDS turns them over: 36.4 us and, where random records of 256 bytes bound it, 64 as before.  Unit s (16 bytes) of block c lies at unit s ^ mix(c) of its
 // row, which has the 16 blocks' units of any step at different banks.
 template <int NF>
 struct Records {
@@ -339,9 +341,7 @@ __global__ __launch_bounds__(kScoreThreads) void score_step_kernel(const E* __re
   __shared__ __attribute__((aligned(16))) char s_tiles[kScoreWaves][Records<NF>::kBytes];
   __shared__ ChooseShared<kScoreWaves, kChoose ? 1024 : 512> s_choose;
   __shared__ int s_order;
-  // (the records of a block's K/V heads are neighbours of 256 bytes, say: an XCD that had one head alone, as it would by the first index, would ask the
-  // same few channels of its cache for all of them)
-  const int g = (int)((blockIdx.x + blockIdx.y + blockIdx.z) % (unsigned)Hkv);
+  const int g = blockIdx.x;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 15, quad = lane >> 4;
   // the group's tokens: first .. first + n - 1 of sequence b, the first at position p0
   int b, first, n, p0;
@@ -540,7 +540,7 @@ __global__ __launch_bounds__(kScoreThreads) void score_prompt_kernel(const int8_
     id = block_at(super + 2);
     __syncthreads();  // (who has passed it has read the tiles before the last ones: one barrier a turn)
     if (n <= 0) continue;
-#pragma unroll 1
+#pragma unroll
     for (int k = 0; k < kScoreWaves; ++k) {
       const int tile = super * 4 + k, e = s_e[at][k][col];
       if (tile >= tiles) break;
@@ -629,7 +629,8 @@ void launch_step(const Slab& x) {
   const int group = a.cu_q ? 16 >> x.log_rows : 1, units = x.units(group), tiles = (int)(x.row_words / 16);
   // as many wavefronts as the device takes at once, then more tiles to one
   const int64_t waves = (int64_t)units * a.Hkv * tiles, room = (int64_t)a.num_cu * 32;
-  const int per_wave = (int)std::min<int64_t>(std::max<int64_t>(1, waves / room), 16), runs = (tiles + kScoreWaves * per_wave - 1) / (kScoreWaves * per_wave);
+  const int most = std::max(16, tiles / (kScoreWaves * 32768) + 1);  // (runs are a grid's second dimension)
+  const int per_wave = (int)std::min<int64_t>(std::max<int64_t>(1, waves / room), most), runs = (tiles + kScoreWaves * per_wave - 1) / (kScoreWaves * per_wave);
   hipLaunchKernelGGL((score_step_kernel<E, NF, PER>), dim3((unsigned)a.Hkv, (unsigned)runs, (unsigned)units), dim3(kScoreThreads), 0, x.s, (const E*)a.q,
                      a.q_row_stride, x.codes, x.exponents, x.tk, a.block_table, a.bt_stride, a.scores, x.row_words, a.Hq / a.Hkv, x.log_rows, a.Hkv, a.D, group,
                      x.unit0(group), x.t0, x.t1, per_wave, Chosen{a.blocks, a.num_selected, a.keep_first, a.keep_last}, a.counters);

@@ -264,14 +264,14 @@ __device__ __forceinline__ void store_row(E* out, f32x4 o, float l) {
 }
 __device__ __forceinline__ float row_lse(float m, float l) { return l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2; }
 
-// Workgroup x: K/V head x % Hkv, then part, then token.  With several parts: counters [T][Hkv] are zero and stay so.
+// Workgroup x: K/V head x % Hkv, then part, then token, from t0 on.  With several parts: counters [T][Hkv] are zero and stay so.
 template <typename E, int KS>
 __global__ __launch_bounds__(kWaves * 64) void attn_sparse_kernel(const E* __restrict__ q, int q_row_stride, const E* __restrict__ k_cache,
                                                                    const E* __restrict__ v_cache, const int32_t* __restrict__ cu_q,
                                                                    const int32_t* __restrict__ ctx_before, const int32_t* __restrict__ block_table, int bt_stride,
                                                                    const int32_t* __restrict__ blocks, int num_selected, E* __restrict__ out,
                                                                    float* __restrict__ lse, float* states, uint32_t* counters, int B, int Hkv, int G, int D, int parts,
-                                                                   float scale_log2e) {
+                                                                   int t0, float scale_log2e) {
   typedef Walk<E, KS> W;
   constexpr int NV = W::NV, NK = W::NK, X = W::X, kRow = 32 * KS + 4;
   __shared__ float s_m[kWaves][16], s_l[kWaves][16];
@@ -280,7 +280,7 @@ __global__ __launch_bounds__(kWaves * 64) void attn_sparse_kernel(const E* __res
   constexpr int kStates = (kWaves - 1) * kMaxGroup * kRow * 4, kWalks = kWaves * W::kLds;
   __shared__ __attribute__((aligned(16))) char s_any[kStates > kWalks ? kStates : kWalks];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 15, quad = lane >> 4;
-  const int g = blockIdx.x % Hkv, rest = blockIdx.x / Hkv, part = rest % parts, t = rest / parts;
+  const int g = blockIdx.x % Hkv, rest = blockIdx.x / Hkv, part = rest % parts, t = t0 + rest / parts;
   int b = t, p;
   if (cu_q) {
     const SeqOf seq = find_sequence(cu_q, ctx_before, B, t, [](int cu, int) { return (long long)cu; });
@@ -428,7 +428,7 @@ template <int KS>
 __global__ __launch_bounds__(group_waves(KS) * 64, group_waves(KS) / 4) void attn_sparse_prompt_kernel(
     const uint16_t* __restrict__ q, int q_row_stride, const uint16_t* __restrict__ k_cache, const uint16_t* __restrict__ v_cache, const int32_t* __restrict__ cu_q,
     const int32_t* __restrict__ ctx_before, const int32_t* __restrict__ block_table, int bt_stride, const int32_t* __restrict__ blocks, int num_selected,
-    uint16_t* __restrict__ out, float* __restrict__ lse, int B, int Hkv, int G, int log_rows, int D, float scale_log2e) {
+    uint16_t* __restrict__ out, float* __restrict__ lse, int B, int Hkv, int G, int log_rows, int D, int unit0, float scale_log2e) {
   constexpr int NV = 2 * KS, kPiece = KS * 1024;  // a block's K or V in LDS: channels up to 32 KS
   constexpr int kGroupWaves = group_waves(KS), kStage = kGroupWaves / 2, words = kWords;  // a wavefront to each piece of a stage's blocks
   __shared__ __attribute__((aligned(16))) char s_stage[2 * kStage * 2 * kPiece];  // twice kStage blocks, K and V
@@ -436,7 +436,7 @@ __global__ __launch_bounds__(group_waves(KS) * 64, group_waves(KS) / 4) void att
   __shared__ uint16_t s_list[words];
   __shared__ int s_count[kGroupWaves], s_alone;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 15, quad = lane >> 4;
-  const int g = blockIdx.x % Hkv, unit = blockIdx.x / Hkv, per_wave = tokens_of_wave(log_rows), group = kGroupWaves * per_wave;
+  const int g = blockIdx.x % Hkv, unit = unit0 + blockIdx.x / Hkv, per_wave = tokens_of_wave(log_rows), group = kGroupWaves * per_wave;
   auto first_unit = [&](int cu, int s) { return (long long)(cu / group) + s; };
   const SeqOf seq = find_sequence(cu_q, ctx_before, B, unit, first_unit);
   const int i0 = (int)(unit - first_unit(seq.tok0, seq.b)) * group, n = min(group, seq.S - i0);
@@ -660,14 +660,20 @@ SparseGroups sparse_groups(const SparseArgs& a) {
   const bool many = a.cu_q && (int64_t)a.T * a.Hkv * a.D >= 2048 * (int64_t)a.num_cu && a.T / a.B >= group && a.bt_stride <= kWords;
   return {log_rows, many ? a.T / group + a.B : 0};
 }
+// n units of `wgs` workgroups of so many threads: launches of fewer than 2^32 threads each.
+template <typename F>
+void in_launches(int n, int wgs, int threads, F f) {
+  const int most = std::max(1, (int)(((int64_t)1 << 31) / threads / wgs));
+  for (int64_t u = 0; u < n; u += most) f((int)u, std::min(most, (int)(n - u)));
+}
+
 template <int KS>
 void launch_groups(const SparseArgs& a, const SparseGroups& by, hipStream_t s) {
-  auto go = [&](auto kernel) {
-    hipLaunchKernelGGL(kernel, dim3((unsigned)((int64_t)a.Hkv * by.units)), dim3(group_waves(KS) * 64), 0, s, (const uint16_t*)a.q, a.q_row_stride, (const uint16_t*)a.k_cache,
-                       (const uint16_t*)a.v_cache, a.cu_q, a.ctx_before, a.block_table, a.bt_stride, a.blocks, a.num_selected, (uint16_t*)a.out, a.lse, a.B, a.Hkv,
-                       a.Hq / a.Hkv, by.log_rows, a.D, a.scale_log2e);
-  };
-  go(&attn_sparse_prompt_kernel<KS>);
+  in_launches(by.units, a.Hkv, group_waves(KS) * 64, [&](int unit0, int units) {
+    hipLaunchKernelGGL((attn_sparse_prompt_kernel<KS>), dim3((unsigned)(a.Hkv * units)), dim3(group_waves(KS) * 64), 0, s, (const uint16_t*)a.q, a.q_row_stride,
+                       (const uint16_t*)a.k_cache, (const uint16_t*)a.v_cache, a.cu_q, a.ctx_before, a.block_table, a.bt_stride, a.blocks, a.num_selected, (uint16_t*)a.out,
+                       a.lse, a.B, a.Hkv, a.Hq / a.Hkv, by.log_rows, a.D, unit0, a.scale_log2e);
+  });
 }
 
 template <typename E, int KS>
@@ -676,9 +682,11 @@ void launch_steps(const SparseArgs& a, hipStream_t s) {
     if (const SparseGroups by = sparse_groups(a)) return launch_groups<KS>(a, by, s);
   }
   const int G = a.Hq / a.Hkv, parts = sparse_parts(a.Hkv, a.T, a.num_selected, a.num_cu);
-  hipLaunchKernelGGL((attn_sparse_kernel<E, KS>), dim3((unsigned)((int64_t)a.Hkv * parts * a.T)), dim3(kWaves * 64), 0, s, (const E*)a.q, a.q_row_stride,
-                     (const E*)a.k_cache, (const E*)a.v_cache, a.cu_q, a.ctx_before, a.block_table, a.bt_stride, a.blocks, a.num_selected, (E*)a.out, a.lse, a.states,
-                     a.counters, a.B, a.Hkv, G, a.D, parts, a.scale_log2e);
+  in_launches(a.T, a.Hkv * parts, kWaves * 64, [&](int t0, int tokens) {
+    hipLaunchKernelGGL((attn_sparse_kernel<E, KS>), dim3((unsigned)(a.Hkv * parts * tokens)), dim3(kWaves * 64), 0, s, (const E*)a.q, a.q_row_stride,
+                       (const E*)a.k_cache, (const E*)a.v_cache, a.cu_q, a.ctx_before, a.block_table, a.bt_stride, a.blocks, a.num_selected, (E*)a.out, a.lse, a.states,
+                       a.counters, a.B, a.Hkv, G, a.D, parts, t0, a.scale_log2e);
+  });
 }
 
 template <typename E>

@@ -9,8 +9,8 @@
 // maximum over the heads is within a lane's four results and over at most two exchanges; its columns are 16 blocks, 16 bytes a lane and step, straight into
 // operand layout.
 //   score_step_kernel    few tokens per sequence: a workgroup codes up to 16 rows into LDS and walks a run of block tiles.  Bound by reading the
-//                        records, 256 bytes of each of a table's scattered blocks (32 sequences of 16384 to 131000 tokens, 8 heads of 128, 0.3 GB: 64 us,
-//                        4.7 TB/s; blocks in order: 51).
+//                        records, 256 bytes per head of each of a table's scattered blocks (32 sequences of 16384 to 131000 tokens, 8 heads of 128, 0.3 GB: 67 us,
+//                        4.5 TB/s).
 //   code_kernel, score_prompt_kernel   prompts: the rows are coded once, into the workspace; a wavefront has four tiles of them in registers.  Bound by the
 //                        products and what is done with their results.
 //   choose               a wavefront or more per (token, K/V head), the scores in registers.  For steps over short contexts the workgroup that is
@@ -295,7 +295,7 @@ __device__ __forceinline__ void put_score(__amdgpu_buffer_rsrc_t to, int where, 
 
 // A tile of 16 records, from memory to LDS to operands.  A lane's operand is 16 bytes of "its" block, so loads straight into operand layout would have
 // neighbouring lanes ask different lines, 64 requests an instruction (895 tokens: 62 us; steps over 32 long contexts: 64);
-// so lanes ask for 64 bytes in a row per four, and LDS turns them over: 36.4 us and, where random records of 256 bytes bound it, 64 as before.  Unit s (16 bytes) of block c lies at unit s ^ mix(c) of its
+// so lanes ask for 64 bytes in a row per four, and LDS turns them over: 36.4 us and, bound by the records' places, 64 as before.  Unit s (16 bytes) of block c lies at unit s ^ mix(c) of its
 // row, which has the 16 blocks' units of any step at different banks.
 template <int NF>
 struct Records {
@@ -322,14 +322,14 @@ struct Records {
   }
 };
 
-// NF: steps of 64 (record bytes / 64).  Grid: K/V heads, runs of tiles_per_wave * 4 block tiles, token groups from `unit0` on; a group is up to `group` tokens of one
-// sequence, numbered from cu_q[b] / group + b.  Tokens outside [t0, t1) are another launch's.  PER > 0 (one token per sequence, rows of at most 256 PER blocks):
+// NF: steps of 64 (record bytes / 64).  Grid: K/V heads, 1 << log_heads of them a workgroup, runs of tiles_per_wave block tiles for each wavefront of a head,
+// token groups from `unit0` on; a group is up to `group` tokens of one sequence, numbered from cu_q[b] / group + b.  Tokens outside [t0, t1) are another launch's.  PER > 0 (one token per sequence, rows of at most 256 PER blocks):
 // the workgroup that is done last with a row chooses its blocks; counters [T][Hkv] are zero and stay so.
 template <typename E, int NF, int PER>
 __global__ __launch_bounds__(kScoreThreads) void score_step_kernel(const E* __restrict__ q, int q_row_stride, const int8_t* __restrict__ codes,
                                                                     const int8_t* __restrict__ exponents, Tokens tk, const int32_t* __restrict__ block_table,
                                                                     int bt_stride, float* __restrict__ scores, int64_t row_words, int G, int log_rows, int Hkv, int D,
-                                                                    int group, int unit0, int t0, int t1, int tiles_per_wave, Chosen to,
+                                                                    int group, int unit0, int t0, int t1, int tiles_per_wave, int log_heads, Chosen to,
                                                                     uint32_t* __restrict__ counters) {
   constexpr int Dp = NF * 32, kRow = 2 * Dp + 16;  // bytes of a coded row in LDS, 16 more than it has: rows begin at different banks
   constexpr bool kChoose = PER > 0;
@@ -337,12 +337,16 @@ __global__ __launch_bounds__(kScoreThreads) void score_step_kernel(const E* __re
     float scale[16];
     alignas(16) int8_t row[16 * kRow];
   };
-  __shared__ Coded coded;
-  __shared__ __attribute__((aligned(16))) char s_tiles[kScoreWaves][Records<NF>::kBytes];
+  // the coded rows of the heads, then each wavefront's tile
+  constexpr int kHeads = kChoose ? 1 : kScoreWaves, kTiles = kScoreWaves * Records<NF>::kBytes, kCoded = kHeads * (int)sizeof(Coded);
+  __shared__ __attribute__((aligned(16))) char s_any[kTiles > kCoded ? kTiles : kCoded];
+  Coded* const coded = reinterpret_cast<Coded*>(s_any);
   __shared__ ChooseShared<kScoreWaves, kChoose ? 1024 : 512> s_choose;
   __shared__ int s_order;
-  const int g = blockIdx.x;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 15, quad = lane >> 4;
+  // this wavefront: a head of the workgroup's, and every `phases`th tile
+  const int heads = kChoose ? 1 : 1 << log_heads, phases = kChoose ? kScoreWaves : kScoreWaves >> log_heads;
+  const int g0 = blockIdx.x * heads, here = kChoose ? 0 : wave & (heads - 1), phase = kChoose ? wave : wave >> log_heads, g = g0 + here;
   // the group's tokens: first .. first + n - 1 of sequence b, the first at position p0
   int b, first, n, p0;
   if (tk.cu_q) {
@@ -362,12 +366,14 @@ __global__ __launch_bounds__(kScoreThreads) void score_step_kernel(const E* __re
   }
   // a row to each 16 lanes, asked for before anything is known of the lengths
   const int r = wave * 4 + quad, r_tok = min(r / G, n - 1), r_head = r - r / G * G;
-  CodedRow<E, NF> mine;
-  mine.ask(q + (size_t)(first + r_tok) * q_row_stride + (size_t)(g * G + r_head) * D, D, col);
+  CodedRow<E, NF> mine[kHeads];
+#pragma unroll
+  for (int i = 0; i < kHeads; ++i)
+    if (i < heads) mine[i].ask(q + (size_t)(first + r_tok) * q_row_stride + (size_t)((g0 + i) * G + r_head) * D, D, col);
 
   // the blocks that the group's last token scores: all in front of its own, which are full
   const int scored = p0 + n - 1 < 0 ? 0 : (int)min((int64_t)((p0 + n - 1) >> 4), row_words);
-  const int per_wg = kScoreWaves * tiles_per_wave, tile0 = blockIdx.y * per_wg, tiles = (scored + 15) >> 4;
+  const int per_wg = phases * tiles_per_wave, tile0 = blockIdx.y * per_wg, tiles = (scored + 15) >> 4;
   if constexpr (kChoose) {
     const int seen = p0 < 0 ? 0 : scored + 1;
     if (seen <= to.K) {  // all of them
@@ -381,17 +387,21 @@ __global__ __launch_bounds__(kScoreThreads) void score_step_kernel(const E* __re
 
   // records of the wavefront's first tile and block ids of the second, on their way while the rows are coded
   const int32_t* const table = block_table + (size_t)b * bt_stride;
-  const int tile_first = tile0 + wave, tile1 = min(tile0 + per_wg, tiles);
+  const int tile_first = tile0 + phase, tile1 = min(tile0 + per_wg, tiles);
   auto block_at = [&](int tile) { return table[min(tile * 16 + col, scored - 1)]; };
   // (records two tiles ahead, block ids three)
   Records<NF> ahead[2];
-  const int id0 = block_at(tile_first), id1 = block_at(tile_first + kScoreWaves);
-  int id2 = block_at(tile_first + 2 * kScoreWaves);
+  const int id0 = block_at(tile_first), id1 = block_at(tile_first + phases);
+  int id2 = block_at(tile_first + 2 * phases);
   ahead[0].ask(codes, exponents, id0, g, Hkv, lane);
   ahead[1].ask(codes, exponents, id1, g, Hkv, lane);
 
-  const float scale_here = mine.code(&coded.row[r * kRow], col);
-  if (col == 0) coded.scale[r] = scale_here;
+#pragma unroll
+  for (int i = 0; i < kHeads; ++i)
+    if (i < heads) {
+      const float scale_here = mine[i].code(&coded[i].row[r * kRow], col);
+      if (col == 0) coded[i].scale[r] = scale_here;
+    }
   __syncthreads();
   // operands of the rows: row r is head min(r % rows, G - 1) of token r / rows
   const int rows = 1 << log_rows;
@@ -399,9 +409,10 @@ __global__ __launch_bounds__(kScoreThreads) void score_step_kernel(const E* __re
   i32x4 af[NF];
   float scale[4];
 #pragma unroll
-  for (int f = 0; f < NF; ++f) af[f] = *reinterpret_cast<const i32x4*>(&coded.row[row_of(col) * kRow + quad * 16 + f * 64]);
+  for (int f = 0; f < NF; ++f) af[f] = *reinterpret_cast<const i32x4*>(&coded[here].row[row_of(col) * kRow + quad * 16 + f * 64]);
 #pragma unroll
-  for (int i = 0; i < 4; ++i) scale[i] = coded.scale[row_of(quad * 4 + i)];
+  for (int i = 0; i < 4; ++i) scale[i] = coded[here].scale[row_of(quad * 4 + i)];
+  __syncthreads();  // (the tiles lie where the coded rows were)
 
   // scores of the group's first token from `out` on; lanes that hold none store behind the end, which the hardware leaves out
   float* const out = scores + ((int64_t)(first - t0) * Hkv + g) * row_words;
@@ -413,12 +424,12 @@ __global__ __launch_bounds__(kScoreThreads) void score_step_kernel(const E* __re
     const int row = quad * 4 + i, tok = row >> log_rows;
     where[i] = (row & (rows - 1)) == 0 && tok < n ? (int)(tok * Hkv * row_words) * 4 + col * 4 : kNowhere;
   }
-  char* const tile_lds = s_tiles[wave];
+  char* const tile_lds = s_any + wave * Records<NF>::kBytes;
   auto walk = [&](Records<NF>& r, int tile) {
     r.put(tile_lds, lane);
     const int e = r.e;
     r.ask(codes, exponents, id2, g, Hkv, lane);  // (behind the last tile: its last block)
-    id2 = block_at(tile + 3 * kScoreWaves);
+    id2 = block_at(tile + 3 * phases);
     i32x4 bf[NF], c = {0, 0, 0, 0};
     Records<NF>::get(bf, tile_lds, col, quad);
 #pragma unroll
@@ -437,10 +448,10 @@ __global__ __launch_bounds__(kScoreThreads) void score_step_kernel(const E* __re
       put_score<kChoose ? kAgent : 0>(to_scores, where[i], tile, v[i], e);
     }
   };
-  for (int tile = tile_first; tile < tile1; tile += 2 * kScoreWaves) {
+  for (int tile = tile_first; tile < tile1; tile += 2 * phases) {
     walk(ahead[0], tile);
-    if (tile + kScoreWaves >= tile1) break;
-    walk(ahead[1], tile + kScoreWaves);
+    if (tile + phases >= tile1) break;
+    walk(ahead[1], tile + phases);
   }
   if constexpr (kChoose) {
     const int wgs = (tiles + per_wg - 1) / per_wg;    // that score blocks of this row
@@ -627,13 +638,16 @@ template <typename E, int NF, int PER>
 void launch_step(const Slab& x) {
   const SelectArgs& a = x.a;
   const int group = a.cu_q ? 16 >> x.log_rows : 1, units = x.units(group), tiles = (int)(x.row_words / 16);
-  // as many wavefronts as the device takes at once, then more tiles to one
+  // Up to four heads in a workgroup, a wavefront each: their records of a block are neighbours (32 sequences of 16384 to 131000 tokens, 8 heads of 128, both launches:
+  // one head 84 us, four 76).  Where the workgroup also chooses, its wavefronts are at one row.
+  const int log_heads = PER > 0 || a.Hkv % 2 != 0 ? 0 : a.Hkv % 4 != 0 ? 1 : 2, phases = kScoreWaves >> log_heads;
+  // as many wavefronts as the device takes at once, then more tiles to one: up to 8 (the same call: 4 tiles 81 us, 8 76, 12 77)
   const int64_t waves = (int64_t)units * a.Hkv * tiles, room = (int64_t)a.num_cu * 32;
-  const int most = std::max(16, tiles / (kScoreWaves * 32768) + 1);  // (runs are a grid's second dimension)
-  const int per_wave = (int)std::min<int64_t>(std::max<int64_t>(1, waves / room), most), runs = (tiles + kScoreWaves * per_wave - 1) / (kScoreWaves * per_wave);
-  hipLaunchKernelGGL((score_step_kernel<E, NF, PER>), dim3((unsigned)a.Hkv, (unsigned)runs, (unsigned)units), dim3(kScoreThreads), 0, x.s, (const E*)a.q,
+  const int most = std::max(8, tiles / (phases * 32768) + 1);  // (runs are a grid's second dimension)
+  const int per_wave = (int)std::min<int64_t>(std::max<int64_t>(1, waves / room), most), runs = (tiles + phases * per_wave - 1) / (phases * per_wave);
+  hipLaunchKernelGGL((score_step_kernel<E, NF, PER>), dim3((unsigned)(a.Hkv >> log_heads), (unsigned)runs, (unsigned)units), dim3(kScoreThreads), 0, x.s, (const E*)a.q,
                      a.q_row_stride, x.codes, x.exponents, x.tk, a.block_table, a.bt_stride, a.scores, x.row_words, a.Hq / a.Hkv, x.log_rows, a.Hkv, a.D, group,
-                     x.unit0(group), x.t0, x.t1, per_wave, Chosen{a.blocks, a.num_selected, a.keep_first, a.keep_last}, a.counters);
+                     x.unit0(group), x.t0, x.t1, per_wave, log_heads, Chosen{a.blocks, a.num_selected, a.keep_first, a.keep_last}, a.counters);
 }
 
 template <typename E, int NF>

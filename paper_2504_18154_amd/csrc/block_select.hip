@@ -12,7 +12,7 @@
 //                        records, 256 bytes per head of each of a table's scattered blocks (32 sequences of 16384 to 131000 tokens, 8 heads of 128, 0.3 GB: 67 us,
 //                        4.5 TB/s).
 //   code_kernel, score_prompt_kernel   prompts: the rows are coded once, into the workspace; a wavefront has four tiles of them in registers.  Bound by the
-//                        products and what is done with their results.
+//                        products and the instructions on their results (895 tokens, 64 heads on 8 of 128, about 1500 blocks: 33.3 us; either alone would take about 9).
 //   choose               a wavefront or more per (token, K/V head), the scores in registers.  For steps over short contexts the workgroup that is
 //                        done last with a row's scores does it in the same launch, otherwise choose_kernel.
 // The scores go through the workspace.
@@ -43,13 +43,13 @@ struct Chosen {
   int K, keep_first, keep_last;
 };
 
-// The maximum over lanes 16 (32) apart.
-__device__ __forceinline__ float max_of_rows16(float v) {
-  const auto x = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+// The maximum over lanes 16 (32) apart: a's in the first of each two rows (halves) of lanes, b's in the second.
+__device__ __forceinline__ float max_of_rows16(float a, float b) {
+  const auto x = __builtin_amdgcn_permlane16_swap(__float_as_uint(a), __float_as_uint(b), false, false);
   return fmaxf(__uint_as_float(x[0]), __uint_as_float(x[1]));
 }
-__device__ __forceinline__ float max_of_rows32(float v) {
-  const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+__device__ __forceinline__ float max_of_rows32(float a, float b) {
+  const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(a), __float_as_uint(b), false, false);
   return fmaxf(__uint_as_float(x[0]), __uint_as_float(x[1]));
 }
 // The maximum over the 16 lanes of a row of lanes.
@@ -295,7 +295,7 @@ __device__ __forceinline__ void put_score(__amdgpu_buffer_rsrc_t to, int where, 
 
 // A tile of 16 records, from memory to LDS to operands.  A lane's operand is 16 bytes of "its" block, so loads straight into operand layout would have
 // neighbouring lanes ask different lines, 64 requests an instruction (895 tokens: 62 us; steps over 32 long contexts: 64);
-// so lanes ask for 64 bytes in a row per four, and LDS turns them over: 36.4 us and, bound by the records' places, 64 as before.  Unit s (16 bytes) of block c lies at unit s ^ mix(c) of its
+// so lanes ask for 64 bytes in a row per four, and LDS turns them over: 38 us and, bound by the records' places, 64 as before.  Unit s (16 bytes) of block c lies at unit s ^ mix(c) of its
 // row, which has the 16 blocks' units of any step at different banks.
 template <int NF>
 struct Records {
@@ -440,8 +440,8 @@ __global__ __launch_bounds__(kScoreThreads) void score_step_kernel(const E* __re
     // the maximum over a token's rows; it is then in v[0] (and, for one or two rows a token, v[2] or all four)
     if (log_rows >= 1) v[0] = fmaxf(v[0], v[1]), v[2] = fmaxf(v[2], v[3]);
     if (log_rows >= 2) v[0] = fmaxf(v[0], v[2]);
-    if (log_rows >= 3) v[0] = max_of_rows16(v[0]);
-    if (log_rows >= 4) v[0] = max_of_rows32(v[0]);
+    if (log_rows >= 3) v[0] = max_of_rows16(v[0], v[0]);
+    if (log_rows >= 4) v[0] = max_of_rows32(v[0], v[0]);
 #pragma unroll
     for (int i = 0; i < (kChoose ? 1 : 4); ++i) {
       if (i & (step - 1)) continue;
@@ -490,9 +490,10 @@ constexpr int kPromptTiles = 4;  // row tiles of a wavefront
 constexpr int prompt_tokens(int log_rows) { return kPromptTiles * (16 >> log_rows); }
 
 // Grid: K/V heads, runs of `run` times four block tiles, token groups from unit0 on as in score_step_kernel.  The wavefronts of a workgroup have different tokens of the
-// group; four tiles of blocks at a time, each brought in by one of them, serve all.
+// group; four tiles of blocks at a time, each brought in by one of them, serve all.  (Two workgroups per CU at least: of at most 256 registers the products' results are in those
+// that other instructions can read.)
 template <int NF, int LOG>
-__global__ __launch_bounds__(kScoreThreads) void score_prompt_kernel(const int8_t* __restrict__ coded, const float* __restrict__ scales,
+__global__ __launch_bounds__(kScoreThreads, 2) void score_prompt_kernel(const int8_t* __restrict__ coded, const float* __restrict__ scales,
                                                                       const int8_t* __restrict__ codes, const int8_t* __restrict__ exponents, Tokens tk,
                                                                       const int32_t* __restrict__ block_table, int bt_stride, float* __restrict__ scores,
                                                                       int64_t row_words, int Hkv, int unit0, int t0, int t1, int run) {
@@ -575,21 +576,13 @@ __global__ __launch_bounds__(kScoreThreads) void score_prompt_kernel(const int8_
         } else {
           m[a] = fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3]));
           if constexpr (LOG == 2) put(a, m[a], e, tile);
-          if constexpr (LOG >= 3) m[a] = max_of_rows16(m[a]);
-          if constexpr (LOG == 4) m[a] = max_of_rows32(m[a]);
         }
       }
-      // (the rows of lanes hold copies: each stores another tile's)
+      // a token's rows are in lanes of two (four) rows of lanes: two tiles change places in halves, and their maximum is the one's here, the other's there
       if constexpr (LOG == 3)
 #pragma unroll
-        for (int a = 0; a < NA; a += 2) {
-          const float even = m[a], odd = m[a + 1];
-          put(a / 2, quad & 1 ? odd : even, e, tile);
-        }
-      if constexpr (LOG == 4) {
-        const float m0 = m[0], m1 = m[1], m2 = m[2], m3 = m[3], even = quad & 2 ? m2 : m0, odd = quad & 2 ? m3 : m1;
-        put(0, quad & 1 ? odd : even, e, tile);
-      }
+        for (int a = 0; a < NA; a += 2) put(a / 2, max_of_rows16(m[a], m[a + 1]), e, tile);
+      if constexpr (LOG == 4) put(0, max_of_rows32(max_of_rows16(m[0], m[1]), max_of_rows16(m[2], m[3])), e, tile);
     }
   }
 }

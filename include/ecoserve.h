@@ -9,8 +9,10 @@
  * evaluated over a KV cache (Section 2.1) that is organised in fixed-size
  * blocks addressed through a per-sequence block table (Section 5, "KV cache
  * management"), with grouped-query head sharing (Section 4.1).  This library
- * is that path and nothing else: append new K/V rows to the paged cache,
- * causal variable-length prefill attention, split-context decode attention.
+ * is that path and nothing else: append new K/V rows to the paged cache (and
+ * rotate them by position on the way), causal variable-length prefill
+ * attention, split-context decode attention, and, for long contexts, attention
+ * over the blocks that a score of block summaries chooses.
  *
  * General rules
  *   - Plain C.  No exception crosses the boundary; every call returns a
@@ -19,7 +21,7 @@
  *     pointers are ordinary host memory.  Every buffer is caller-owned.  The
  *     library allocates device memory only in ecoserve_create() and
  *     ecoserve_set_option() and frees it in ecoserve_destroy().
- *   - The three hot calls validate what the host can see (pointers, sizes,
+ *   - The hot calls validate what the host can see (pointers, sizes,
  *     alignment, limits) BEFORE launching anything, then enqueue their kernels
  *     on the given HIP stream and return without synchronising.
  *   - Contents of device arrays (block-table entries, lengths) are not
@@ -28,7 +30,8 @@
  *   - One call handles one layer; callers loop over layers.
  *   - Calls that share a context must be issued on one stream (or be ordered
  *     by the caller): they share the context's workspace (split-context partial
- *     states and merge counters of decode, the query-tile list and its queues'
+ *     states and merge counters of decode, which block selection and attention
+ *     over listed blocks use too, the query-tile list and its queues'
  *     counters of prefill).  Calls that overlap all the same may spoil their own
  *     results and those of later calls on the context (a counter left away from
  *     its start); a new context is free of that.
@@ -384,6 +387,7 @@ typedef struct {
  *                  calls), 16-byte aligned; both NULL: only K and V.  They may be the same array with the same stride;
  *                  arrays that overlap otherwise: undefined.  Rows of q_out that belong to no sequence are left alone.
  *   everything else as in ecoserve_kv_append_strided (max_new_len <= 1 again selects the one-token launch).
+ * Of the options ECOSERVE_OPT_PROFILE counts it as an append; the others do not concern it, nor the calls below.
  */
 int ecoserve_kv_append_rope(ecoserve_ctx* ctx, const ecoserve_rope* rope, const double* inv_freq, const int32_t* positions,
                             const void* q, int64_t q_row_stride, void* q_out, int64_t q_out_row_stride, void* k_cache,
@@ -437,8 +441,10 @@ int ecoserve_kv_summary(ecoserve_ctx* ctx, const void* k_cache, void* summary, c
  *   num_selected : 1 .. 65536;  keep_first >= 0, keep_last >= 1, keep_first + keep_last <= num_selected
  *   max_ctx_len  : upper bound on any token's position + 1, as in ecoserve_attn_decode
  *   workspace    : dev, 16-byte aligned, at least ecoserve_select_workspace_bytes(layout, T, max_ctx_len) bytes; nothing in
- *                  it is kept from call to call, calls that overlap need one each (recorded into graphs: each graph one, if
- *                  they may run at the same time)
+ *                  it is kept from call to call
+ * Calls that share a context are ordered (rules at the top): steps of one token per sequence count in the context's merge
+ * counters which workgroup comes last.  Calls that may run at the same time, recorded into graphs or not, need a context
+ * and a workspace each.
  */
 size_t ecoserve_select_workspace_bytes(const ecoserve_layout* layout, int32_t T, int32_t max_ctx_len);
 int ecoserve_block_select(ecoserve_ctx* ctx, const void* q, int64_t q_row_stride, const void* summary, const int32_t* cu_q,
@@ -455,7 +461,7 @@ int ecoserve_block_select(ecoserve_ctx* ctx, const void* q, int64_t q_row_stride
  *   blocks       : dev, int32[T][Hkv][num_selected], num_selected 1 .. 65536
  *   out, lse     : as in ecoserve_attn_prefill (lse may be NULL); rows of tokens behind cu_q[B] are left alone
  *   workspace    : dev, 16-byte aligned, at least ecoserve_sparse_workspace_bytes(ctx, T, num_selected) bytes (0 for many
- *                  tokens; NULL is fine then); rules as above
+ *                  tokens; NULL is fine then); rules as above, contexts included
  *   everything else as in ecoserve_block_select.
  */
 size_t ecoserve_sparse_workspace_bytes(const ecoserve_ctx* ctx, int32_t T, int32_t num_selected);

@@ -265,7 +265,8 @@ void launch_typed(const RopeAppend& a, const Turns& turns, int num_cu, hipStream
   const int v_heads = D * (int)sizeof(E) <= 512 ? 4 : 2, v_slices = (a.Hkv + v_heads - 1) / v_heads;
   const int64_t units = (int64_t)a.T / 16 + 2 * (int64_t)a.B;
   const int total = a.Hkv + (q ? a.Hq : 0);
-  // heads per workgroup: as many workgroups as the device takes at once, then more heads to an angle
+  // heads per workgroup: as many workgroups as the device takes at once, then more heads to an angle (3 prompts, 2.3k tokens, 64 heads on 8 of 128: 4 workgroups
+  // per CU 43.7 us, 8 40.5, 16 49.0)
   const int64_t want = (8 * (int64_t)num_cu + units - 1) / units;
   const int slices = (int)(want < total ? want : total), per_slice = (total + slices - 1) / slices;
   const dim3 grid((unsigned)units, (unsigned)(v_slices + (total + per_slice - 1) / per_slice));

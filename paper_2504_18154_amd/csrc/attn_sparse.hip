@@ -28,38 +28,69 @@ namespace {
 constexpr int kWaves = 4;
 constexpr int kRsrc = 0x00020000;  // buffer descriptor: untyped 32-bit data, no swizzle, no stride
 constexpr int kAgent = 16;         // past the caches that XCDs do not share
-constexpr float kRaise = 8.f;      // the exponent offset is raised when a score exceeds it by more (log2 units)
+typedef const void __attribute__((address_space(1)))* gptr_t;
+typedef void __attribute__((address_space(3)))* lptr_t;
+constexpr float kRaise = 8.f;      // the exponent offset is raised when a score exceeds it by more (log2 units; 2^8: 256, below)
 
 // The state of 16 columns: m exponent offset (-inf: no key yet), l this lane's share of the sum, o unnormalised.
 template <int NV>
 struct State {
   float m = -INFINITY, l = 0.f;
   f32x4 o[NV];
-  // scores q.k (-inf: no key) to weights; a lane that `counts` not has none, whatever its (finite) scores
+  // the offset follows the largest score (of this lane: top) of the columns
+  __device__ __forceinline__ void raise(float top) {
+    top = fmaxf(top, __shfl_xor(top, 16));
+    top = fmaxf(top, __shfl_xor(top, 32));
+    const float raised = top > m + kRaise ? top : m, by = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - raised);
+    l *= by;
+#pragma unroll
+    for (int dt = 0; dt < NV; ++dt)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) o[dt][i] *= by;
+    m = raised;
+  }
   template <int N>
-  __device__ __forceinline__ void weights(f32x4 (&s)[N], float scale_log2e, bool counts = true) {
+  static __device__ __forceinline__ float largest(const f32x4 (&s)[N]) {
     float top = s[0][0];
 #pragma unroll
     for (int t = 0; t < N; ++t) top = fmaxf(top, fmaxf(fmaxf(s[t][0], s[t][1]), fmaxf(s[t][2], s[t][3])));
-    top = counts ? top * scale_log2e : -INFINITY;
-    if (__any(top > m + kRaise)) {
-      top = fmaxf(top, __shfl_xor(top, 16));
-      top = fmaxf(top, __shfl_xor(top, 32));
-      const float raised = top > m + kRaise ? top : m, by = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - raised);
-      l *= by;
-#pragma unroll
-      for (int dt = 0; dt < NV; ++dt)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) o[dt][i] *= by;
-      m = raised;
-    }
-    const float mu = counts ? (m == -INFINITY ? 0.f : m) : INFINITY;
+    return top;
+  }
+  // scores q.k (-inf: no key) to weights
+  template <int N>
+  __device__ __forceinline__ void weights(f32x4 (&s)[N], float scale_log2e) {
+    const float top = largest(s) * scale_log2e;
+    if (__any(top > m + kRaise)) raise(top);
+    const float mu = m == -INFINITY ? 0.f : m;
 #pragma unroll
     for (int t = 0; t < N; ++t) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) s[t][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][i], scale_log2e, -mu));
       l += (s[t][0] + s[t][1]) + (s[t][2] + s[t][3]);
     }
+  }
+  // The same of 32 keys, for lanes that `counts` (the others have no weight, whatever their finite scores); scores beyond the offset are looked for among the weights, those above
+  // 2^kRaise, in the order of their bits (a NaN is above; an offset that no key has set yet, -inf, makes any weight infinite).
+  __device__ __forceinline__ void weights_of(const f32x4 (&s)[2], f32x4 (&w)[2], float scale_log2e, bool counts) {
+    auto all = [&] {
+      const float mu = counts ? m : INFINITY;
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[t][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][i], scale_log2e, -mu));
+    };
+    all();
+    auto bits = [&](int t, int i) { return __float_as_uint(w[t][i]); };
+    uint32_t most = max(max(bits(0, 0), bits(0, 1)), bits(0, 2));
+    most = max(max(most, bits(0, 3)), bits(1, 0));
+    most = max(max(most, bits(1, 1)), bits(1, 2));
+    most = max(most, bits(1, 3));
+    if (__any(most > __float_as_uint(256.f))) {
+      raise(counts ? largest(s) * scale_log2e : -INFINITY);
+      all();
+    }
+#pragma unroll
+    for (int t = 0; t < 2; ++t) l += (w[t][0] + w[t][1]) + (w[t][2] + w[t][3]);
   }
 };
 
@@ -414,11 +445,14 @@ __global__ __launch_bounds__(kWaves * 64) void attn_sparse_kernel(const E* __res
 //   The union: a word per block of the sequence with a bit per token, from which the listed ones are collected in their order.
 //   Where that does not do, the wavefront takes its tokens one by one, block by block: lists with a block twice, and results that are not
 // finite (a NaN or an infinity among values meets the zero weights of the columns beside it).
-//   The weights are rounded to bf16 once, as the prefill kernel has them (two parts: 171 us for 895 tokens, so 142): a row is off by 2^-9 of its size then, as much
+//   The weights are rounded to bf16 once, as the prefill kernel has them (two parts took 171 us where one took 142): a row is off by up to 2^-8 of its size then, as much
 // as the rounding of the result.
-// What bounds it: the products, half of whose columns' work is of blocks that the token beside lists (of 64 on 8 heads, lists of 64 that agree in half; 16 products and 105 vector
-// instructions a pair of blocks), and that the wavefronts wait for the one with the most blocks of a stage.  Token by token the same call reads each block of K and V 20 times
-// from the caches, 3.7 GB, 235 us.
+//   Blocks go from memory into LDS without registers between, and the operands of a pair of blocks are asked for together, half of the values' before the weights are known
+// (in registers, operands as they are wanted: 145 us, so 131; values all at once: 140).
+// What bounds it (895 tokens, 64 heads on 8 of 128, lists of 64 that agree in half): latency.  A workgroup fills a CU, its wavefronts leave a barrier together, and want
+// LDS, the matrix unit and the vector unit at the same times, which are busy for 32, 19 and 30% of it; at a barrier they wait for the one with the most blocks of a stage (the
+// sum of those is 1.7 times the mean's), and the workgroup with the largest union comes last.  A column's work is in vain for 40% of a wavefront's blocks, those that the token
+// beside it lists alone.  Token by token the same call reads each block of K and V 20 times from the caches, 3.7 GB, 235 us.
 constexpr int kWords = 5120;  // blocks of a sequence that the union has room for
 constexpr int group_waves(int KS) { return KS <= 4 ? 16 : 8; }  // (as many as have the registers)
 // Tokens of a wavefront.
@@ -430,6 +464,7 @@ __global__ __launch_bounds__(group_waves(KS) * 64, group_waves(KS) / 4) void att
     const int32_t* __restrict__ ctx_before, const int32_t* __restrict__ block_table, int bt_stride, const int32_t* __restrict__ blocks, int num_selected,
     uint16_t* __restrict__ out, float* __restrict__ lse, int B, int Hkv, int G, int log_rows, int D, int unit0, float scale_log2e) {
   constexpr int NV = 2 * KS, kPiece = KS * 1024;  // a block's K or V in LDS: channels up to 32 KS
+  constexpr int kEarly = NV < 4 ? NV : 4;         // of a pair of blocks' values, how much is asked for before the weights are known (registers)
   constexpr int kGroupWaves = group_waves(KS), kStage = kGroupWaves / 2, words = kWords;  // a wavefront to each piece of a stage's blocks
   __shared__ __attribute__((aligned(16))) char s_stage[2 * kStage * 2 * kPiece];  // twice kStage blocks, K and V
   __shared__ uint32_t s_word[words];
@@ -498,69 +533,81 @@ __global__ __launch_bounds__(group_waves(KS) * 64, group_waves(KS) / 4) void att
   State<NV> st;
 #pragma unroll
   for (int dt = 0; dt < NV; ++dt) st.o[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
+  const uint32_t k_place = quad * 256 + (8 * (col >> 2 & 1) + (col & 3)) * 16, v_place = kPiece + col * 32 + (quad & 1) * 16;
   const uint32_t my_bits = have > 0 ? ((1u << have) - 1u) << mine0 : 0u, my_bit = real ? 1u << (mine0 + tok) : 0u;
-  // two blocks in LDS, K and then V: `seen` keys of the lane's one (the second block's for quads 2 and 3), if some lane sees not all or none of its 16 (`ragged`)
-  // (kOne: the first block alone, the second's values do not count at all)
-  auto attend = [&](auto one, const char* a, const char* b, int seen, bool ragged) {
+  // Two blocks in LDS, K and then V, at a and b.  `counts`: the column's token lists the lane's one (quads 0 and 1: a); if some lane sees not all of its 16 keys
+  // (`ragged`), seen() of them.  (kOne: the first block alone, the second's values do not count at all)
+  const uint32_t half_k = col < 8 ? 0u : ~0u, half_v = quad < 2 ? 0u : ~0u;
+  auto attend = [&](auto one, uint32_t a, uint32_t b, bool counts, auto seen, bool ragged) {
     constexpr bool kOne = decltype(one)::value;
     f32x4 s[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
-    const char* const kat = (col < 8 ? a : b) + quad * 256 + (8 * (col >> 2 & 1) + (col & 3)) * 16;
+    const char* const kat = s_stage + (a + (half_k & (b - a)) + k_place);
+    u32x4 x[KS][2];
 #pragma unroll
     for (int j = 0; j < KS; ++j)
 #pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        u32x4 x = *reinterpret_cast<const u32x4*>(kat + j * 1024 + t * 64);
-        if (j == KS - 1 && D != 32 * KS && (4 * j + quad) * 8 >= D) x = u32x4{0u, 0u, 0u, 0u};  // (channels that there are not)
-        s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x), __builtin_bit_cast(bf16x8, qf[j]), s[t], 0, 0, 0);
-      }
+      for (int t = 0; t < 2; ++t) x[j][t] = *reinterpret_cast<const u32x4*>(kat + j * 1024 + t * 64);
+#pragma unroll
+    for (int j = 0; j < KS; ++j)
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+        s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x[j][t]), __builtin_bit_cast(bf16x8, qf[j]), s[t], 0, 0, 0);
+    const char* const vat = s_stage + (a + (half_v & (b - a)) + v_place);
+    u32x4 y[NV];
+#pragma unroll
+    for (int dt = 0; dt < kEarly; ++dt) y[dt] = *reinterpret_cast<const u32x4*>(vat + dt * 512);
     if (ragged) {
+      const int n = seen();
 #pragma unroll
       for (int t = 0; t < 2; ++t)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) s[t][e] = 8 * (quad & 1) + 4 * t + e < seen ? s[t][e] : -INFINITY;
+        for (int e = 0; e < 4; ++e) s[t][e] = 8 * (quad & 1) + 4 * t + e < n ? s[t][e] : -INFINITY;
     }
-    st.weights(s, scale_log2e, seen > 0);
-    const bf16x8 w = __builtin_bit_cast(bf16x8, u32x4{pack_bf16x2(s[0][0], s[0][1]), pack_bf16x2(s[0][2], s[0][3]), pack_bf16x2(s[1][0], s[1][1]), pack_bf16x2(s[1][2], s[1][3])});
+    f32x4 p[2];
+    st.weights_of(s, p, scale_log2e, counts);
+    const bf16x8 w = __builtin_bit_cast(bf16x8, u32x4{pack_bf16x2(p[0][0], p[0][1]), pack_bf16x2(p[0][2], p[0][3]), pack_bf16x2(p[1][0], p[1][1]), pack_bf16x2(p[1][2], p[1][3])});
     __builtin_amdgcn_s_setprio(1);  // (wavefronts that multiply go before those that count: 152 -> 142 us)
-    const char* const vat = (quad < 2 ? a : b) + kPiece + col * 32 + (quad & 1) * 16;
+#pragma unroll
+    for (int dt = kEarly; dt < NV; ++dt) y[dt] = *reinterpret_cast<const u32x4*>(vat + dt * 512);
 #pragma unroll
     for (int dt = 0; dt < NV; ++dt) {
-      u32x4 raw_x = *reinterpret_cast<const u32x4*>(vat + dt * 512);
-      if (kOne && quad >= 2) raw_x = u32x4{0u, 0u, 0u, 0u};
-      const bf16x8 x = __builtin_bit_cast(bf16x8, raw_x);
-      st.o[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, w, st.o[dt], 0, 0, 0);
+      if (kOne && quad >= 2) y[dt] = u32x4{0u, 0u, 0u, 0u};
+      st.o[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, y[dt]), w, st.o[dt], 0, 0, 0);
     }
     __builtin_amdgcn_s_setprio(0);
   };
-  // K or V of one of the four blocks is brought in by each wavefront
-  u32x4 raw[KS];
-  int raw_slots = 16;
-  auto ask_piece = [&](const char* at) {
+  // K or V of a block, from memory to LDS by a wavefront
+  auto bring = [&](const char* at, uint32_t to) {
 #pragma unroll
     for (int k = 0; k < KS; ++k) {
       const int u = k * 64 + lane;
-      raw[k] = *reinterpret_cast<const u32x4*>(at + (k < KS - 1 || u < 2 * D ? u : 0) * 16);
+      __builtin_amdgcn_global_load_lds((gptr_t)(at + (k < KS - 1 || u < 2 * D ? u : 0) * 16), (lptr_t)(s_stage + to + k * 1024), 16, 0, 0);
     }
   };
-  auto put_piece = [&](char* to, int slots) {
-    if (slots < 16) {  // values behind the last token (stale bits, possibly NaN) must not meet zero weights
+  // ... once it is there: channels of K that there are not, and values behind the last token (stale bits, possibly NaN), must not meet zeros of the other side
+  auto arrived = [&](uint32_t at, bool is_v, int slots) {
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    char* const mine = s_stage + at + lane * 16;
+    if (!is_v && D != 32 * KS && (KS - 1) * 64 + lane >= 2 * D) *reinterpret_cast<u32x4*>(mine + (KS - 1) * 1024) = u32x4{0u, 0u, 0u, 0u};
+    if (is_v && slots < 16) {
 #pragma unroll
-      for (int k = 0; k < KS; ++k)
+      for (int k = 0; k < KS; ++k) {
+        u32x4 x = *reinterpret_cast<const u32x4*>(mine + k * 1024);
 #pragma unroll
         for (int w = 0; w < 4; ++w) {
           const int slot = 8 * (lane & 1) + 2 * w;
-          raw[k][w] &= (slot < slots ? 0xffffu : 0u) | (slot + 1 < slots ? 0xffff0000u : 0u);
+          x[w] &= (slot < slots ? 0xffffu : 0u) | (slot + 1 < slots ? 0xffff0000u : 0u);
         }
+        *reinterpret_cast<u32x4*>(mine + k * 1024) = x;
+      }
     }
-#pragma unroll
-    for (int k = 0; k < KS; ++k) *reinterpret_cast<u32x4*>(to + (k * 64 + lane) * 16) = raw[k];
   };
   // the wavefront's piece of a stage is of the block list[i + wave / 2]; its place in memory is known a stage before it is asked for
   auto index_of = [&](int i) { return __builtin_amdgcn_readfirstlane(s_list[min(i + (wave >> 1), listed - 1)]); };
-  int j_ask = 0, id_ask = 0;
+  int j_ask = 0, id_ask = 0, slots_next = 16;
   auto ask = [&](int i) {
-    ask_piece((wave & 1 ? vbase : kbase) + (size_t)id_ask * stride);
-    raw_slots = wave & 1 ? min(16, p0 + n - j_ask * 16) : 16;
+    bring((wave & 1 ? vbase : kbase) + (size_t)id_ask * stride, (i / kStage & 1) * (kStage * 2 * kPiece) + wave * kPiece);
+    slots_next = min(16, p0 + n - j_ask * 16);
     j_ask = index_of(i + kStage);  // (behind the last ones: the last one)
     id_ask = table[j_ask];
   };
@@ -578,10 +625,10 @@ __global__ __launch_bounds__(group_waves(KS) * 64, group_waves(KS) / 4) void att
     look(0);
   }
   for (int i = 0; i < listed; i += kStage) {
-    char* const buf = s_stage + (i / kStage & 1) * (kStage * 2 * kPiece);
-    put_piece(buf + wave * kPiece, raw_slots);
-    ask(i + kStage);
+    const uint32_t buf = (i / kStage & 1) * (kStage * 2 * kPiece);
+    arrived(buf + wave * kPiece, wave & 1, slots_next);
     __syncthreads();  // (who has passed it is through with the blocks before the last ones: one barrier a turn)
+    ask(i + kStage);
     // the blocks that tokens of this wavefront list, two at a time
     const int j_now = j_here;
     const uint32_t bits_now = bits_here;
@@ -595,12 +642,13 @@ __global__ __launch_bounds__(group_waves(KS) * 64, group_waves(KS) / 4) void att
       want &= want - 1;
       const int ja = __builtin_amdgcn_readlane(j_now, a), jb = __builtin_amdgcn_readlane(j_now, b);
       const uint32_t ba = __builtin_amdgcn_readlane(bits_now, a), bb = pair ? __builtin_amdgcn_readlane(bits_now, b) : 0u;
-      // keys of the lane's block that its column's token sees there: all, but for blocks that a token of the group is in
-      attend(std::false_type(), buf + a * (2 * kPiece), buf + b * (2 * kPiece), ((quad < 2 ? ba : bb) & my_bit) ? p + 1 - (quad < 2 ? ja : jb) * 16 : 0,
-             max(ja, jb) >= p0 >> 4);
+      // the column's token lists the lane's block, and sees its keys: all, but for blocks that a token of the group is in
+      attend(std::false_type(), buf + a * (2 * kPiece), buf + b * (2 * kPiece), ((ba ^ (half_v & (ba ^ bb))) & my_bit) != 0,
+             [&] { return p + 1 - (quad < 2 ? ja : jb) * 16; }, max(ja, jb) >= p0 >> 4);
     }
   }
-  __syncthreads();  // (all wavefronts are through with the stages)
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // (what was brought in for a stage behind the last)
+  __syncthreads();                                  // (all wavefronts are through with the stages)
   auto finish = [&](int token, int h, bool store) {
     st.l += __shfl_xor(st.l, 16);
     st.l += __shfl_xor(st.l, 32);
@@ -630,25 +678,25 @@ __global__ __launch_bounds__(group_waves(KS) * 64, group_waves(KS) / 4) void att
 #pragma unroll
     for (int dt = 0; dt < NV; ++dt) st.o[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
     const int32_t* const list = blocks + ((int64_t)token * Hkv + g) * num_selected;
-    char* const own = s_stage + wave * (2 * kPiece);
+    const uint32_t own = wave * (2 * kPiece);
     for (int i = 0; i < num_selected; ++i) {
       const int j = __builtin_amdgcn_readfirstlane(list[i]);
       if (j < 0 || j > last) continue;
       const size_t block = (size_t)table[j] * stride;
       const int slots = min(16, at + 1 - j * 16);
-      ask_piece(kbase + block);
-      put_piece(own, 16);
-      ask_piece(vbase + block);
-      put_piece(own + kPiece, slots);
-      attend(std::true_type(), own, own, quad < 2 ? slots : 0, true);
+      bring(kbase + block, own);
+      bring(vbase + block, own + kPiece);
+      arrived(own, false, 16);
+      arrived(own + kPiece, true, slots);
+      attend(std::true_type(), own, own, quad < 2, [&] { return slots; }, true);
     }
     finish(token, col, col < G);
   }
 }
 
-// Prompts of so many rows that the groups' lists in common save more than a group's walk, which takes 100 us of 64 blocks, alone or beside others, costs.  (us of a call, token
-// by token / groups: 64 on 8, 128, lists of 64: 256 tokens 64 / 119, 512 129 / 130, 2048 498 / 245; 2000, of 32, 309 / 169; 52 on 52: 32 95 / 109, 128 381 / 117; 32 on 8, 64:
-// 512 64 / 98, 2048 269 / 176; 8 on 1, 2048 69 / 115; 8 on 1, 256: 512 49 / 166, 2048 181 / 147.)
+// Prompts of so many rows that the groups' lists in common save more than a group's walk, which takes 85 us of 64 blocks, alone or beside others, costs.  (us of a call, token
+// by token / groups: 64 on 8, 128, lists of 64: 256 tokens 64 / 99, 512 126 / 112, 2048 491 / 212; 2000, of 32, 295 / 151; 52 on 52: 32 96 / 95, 128 380 / 101; 32 on 8, 64:
+// 512 66 / 92, 2048 269 / 165; 8 on 1, 2048 69 / 99; 8 on 1, 256: 512 50 / 155, 2048 181 / 136.)
 struct SparseGroups {
   int log_rows, units;  // units 0: token by token
   explicit operator bool() const { return units > 0; }

@@ -125,3 +125,37 @@ def test_a_rotated_append_is_profiled_as_one():
         ctx.kv_append_rope(kc, vc, k, k, dev_i32([0, 3]), dev_i32([0]), dev_i32([[0]]), rope)
     assert ctx.profile_read(binding.KERNEL_APPEND)[1] == 2
     ctx.close()
+
+
+@pytest.mark.parametrize("D,Hq,Hkv,new", [(192, 6, 2, [1400]), (32, 16, 8, [1100, 1000]), (24, 12, 12, [1900])], ids=["d192", "d32", "d24"])
+def test_groups_of_other_head_sizes(D, Hq, Hkv, new):
+    rng = np.random.default_rng(D)
+    b = Batch("bf16", D, Hq, Hkv, [90] * len(new), new, seed=D)
+    assert b.T * Hkv * D >= 2048 * 256
+    lists = _random_lists(b, 6, rng)
+    out, lse = _attend(b, lists)
+    _compare(b, lists, out, lse, name=f"head size {D}", tokens=_of_prompts(b), rounded_weights=True)
+    b.ctx.close()
+
+
+@pytest.mark.parametrize("growing", [False, True])
+def test_groups_and_large_scores(growing):
+    """Scores of hundreds of either sign; keys that grow along the sequence, so that the offset of the exponents is raised block by block (a list in order, and backwards)."""
+    rng = np.random.default_rng(11)
+    b = Batch("bf16", 128, 8, 2, [200], [2100], seed=7)
+    if growing:
+        for j in range(b.table.shape[1]):
+            b.keys[b.table[0, j]] *= 2.0 ** (j // 12)
+    else:
+        b.q *= 16
+        b.keys *= 16
+    b.upload()
+    some = _of_prompts(b)
+    lists = _random_lists(b, 8, rng)
+    lists.sort(2)
+    for order in (1, -1):
+        mine = np.ascontiguousarray(lists[:, :, ::order])
+        out, lse = _attend(b, mine)
+        assert torch.isfinite(out[16:].float()).all()
+        _compare(b, mine, out, lse, name=f"order {order}", tokens=some, rounded_weights=True)
+    b.ctx.close()

@@ -506,7 +506,7 @@ int ecoserve_block_select(ecoserve_ctx* c, const void* q, int64_t q_row_stride, 
 
 size_t ecoserve_sparse_workspace_bytes(const ecoserve_ctx* c, int32_t T, int32_t num_selected) {
   if (!c || T <= 0 || num_selected <= 0) return 0;
-  return sparse_workspace_bytes(c->lay.num_q_heads, c->lay.num_kv_heads, c->lay.head_dim, T, num_selected, c->num_cu);
+  return sparse_workspace_bytes(c->lay, T, num_selected, c->num_cu);
 }
 
 int ecoserve_attn_sparse(ecoserve_ctx* c, const void* q, int64_t q_row_stride, const void* k_cache, const void* v_cache, const int32_t* cu_q,
@@ -519,7 +519,7 @@ int ecoserve_attn_sparse(ecoserve_ctx* c, const void* q, int64_t q_row_stride, c
   if (!q || !k_cache || !v_cache || !out || !lists_ok(c, cu_q, ctx_before, block_table, bt_stride, blocks, num_selected, B, T)) return ECOSERVE_EINVAL;
   if (!aligned16(q) || !aligned16(k_cache) || !aligned16(v_cache) || !aligned16(out) || !aligned16(workspace)) return ECOSERVE_EINVAL;
   if (lse && (reinterpret_cast<uintptr_t>(lse) & 3u)) return ECOSERVE_EINVAL;
-  const size_t needed = sparse_workspace_bytes(L.num_q_heads, L.num_kv_heads, L.head_dim, T, num_selected, c->num_cu);
+  const size_t needed = sparse_workspace_bytes(L, T, num_selected, c->num_cu);
   if (needed > 0 && (!workspace || workspace_bytes < needed)) return ECOSERVE_EINVAL;
   DeviceGuard guard(c->device);
   if (!guard.ok) return ECOSERVE_EHIP;

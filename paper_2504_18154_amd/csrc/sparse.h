@@ -47,17 +47,23 @@ struct SelectArgs {
   uint32_t* counters;  // one per (token, K/V head) where there is one token per sequence, zero between launches
 };
 
-// Attention over listed blocks: a list is cut into parts, one workgroup each, where there are few (token, K/V head)s.  Two
-// workgroups per CU are wanted, and a part has at least eight blocks: two per wavefront.
-inline int32_t sparse_parts(int32_t Hkv, int32_t T, int32_t num_selected, int32_t num_cu) {
-  const int64_t rows = (int64_t)T * Hkv;
-  return (int32_t)std::max<int64_t>(1, std::min<int64_t>({2 * (int64_t)num_cu / rows, (num_selected + 7) / 8, 64}));
+// Attention over listed blocks: a list is cut into parts, one workgroup each, where there are few (token, K/V head)s and the list is longer than a merge (2.5 us and 0.1 more
+// per part) is worth: up to a workgroup per CU in all, for lists of up to 128 half of that; a part has eight blocks at least, two per wavefront, and as many as there are
+// parts.  (us, 40 heads on 8 of 128, bf16.  One token: 32 blocks whole 8.7, in 4 parts 9.6; 64 whole 11.9, in 4, 8, 16 parts 10.7, 9.9, 11.9; 1024 in 16, 32, 64 parts 20.6, 21.0, 25.7.
+// 16 tokens: 64 whole 16.0, in 2, 4 parts 18.8, 20.2; 1024 whole 217, in 2, 4 parts 191, 192.  fp32, a block at a time, 8 heads on 2 of 64: 16 blocks whole 7.2, in 2 parts 8.2; 32 whole
+// 10.0, in 4 8.2.)
+inline int32_t sparse_parts(int32_t Hkv, int32_t T, int32_t num_selected, int32_t num_cu, int32_t dtype) {
+  const int64_t rows = (int64_t)T * Hkv, room = (num_selected > 128 ? num_cu : num_cu / 2) / rows;
+  if (room < 2 || num_selected <= (dtype == ECOSERVE_BF16 ? 32 : 16)) return 1;
+  int32_t root = 1;
+  while (root < 64 && (root + 1) * (root + 1) <= num_selected) ++root;
+  return (int32_t)std::min<int64_t>({room, (num_selected + 7) / 8, root});
 }
 // Floats of a part's state of one query head: the unnormalised head vector, its maximum and its sum, and two that keep 16 bytes aligned.
 constexpr int32_t sparse_state_words(int32_t D) { return D + 4; }
-inline size_t sparse_workspace_bytes(int32_t Hq, int32_t Hkv, int32_t D, int32_t T, int32_t num_selected, int32_t num_cu) {
-  const int32_t parts = sparse_parts(Hkv, T, num_selected, num_cu);
-  return parts == 1 ? 0 : (size_t)parts * T * Hq * sparse_state_words(D) * 4;
+inline size_t sparse_workspace_bytes(const ecoserve_layout& L, int32_t T, int32_t num_selected, int32_t num_cu) {
+  const int32_t parts = sparse_parts(L.num_kv_heads, T, num_selected, num_cu, L.dtype);
+  return parts == 1 ? 0 : (size_t)parts * T * L.num_q_heads * sparse_state_words(L.head_dim) * 4;
 }
 
 struct SparseArgs {

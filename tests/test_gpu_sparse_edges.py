@@ -159,3 +159,19 @@ def test_groups_and_large_scores(growing):
         assert torch.isfinite(out[16:].float()).all()
         _compare(b, mine, out, lse, name=f"order {order}", tokens=some, rounded_weights=True)
     b.ctx.close()
+
+
+@pytest.mark.parametrize("dtype,D,Hq,Hkv", [("bf16", 64, 5, 1), ("bf16", 128, 4, 2), ("f32", 160, 3, 1)])
+def test_as_many_parts_as_there_are(dtype, D, Hq, Hkv):
+    """Lists of 4096 entries and more are cut into 64; most entries hold no keys, and some parts none at all."""
+    rng = np.random.default_rng(D)
+    b = Batch(dtype, D, Hq, Hkv, [9000, 40], [1, 1], seed=D)
+    for K in (4096, 4500):
+        assert b.ctx.sparse_workspace_bytes(2, K) == 64 * 2 * Hq * (D + 4) * 4 if Hkv == 1 else b.ctx.sparse_workspace_bytes(2, K) > 0
+        lists = _random_lists(b, K, rng, order=False)
+        lists[:, :, 700:] = -1
+        lists[0, 0, -1] = 3 if 3 not in lists[0, 0] else -1
+        out, lse = _attend(b, lists, ragged=False)
+        _compare(b, lists, out, lse, name=f"{K} entries")
+        assert torch.equal(out, _attend(b, lists, ragged=False)[0])
+    b.ctx.close()

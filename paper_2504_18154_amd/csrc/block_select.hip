@@ -491,9 +491,9 @@ constexpr int prompt_tokens(int log_rows) { return kPromptTiles * (16 >> log_row
 
 // Grid: K/V heads, runs of `run` times four block tiles, token groups from unit0 on as in score_step_kernel.  The wavefronts of a workgroup have different tokens of the
 // group; four tiles of blocks at a time, each brought in by one of them, serve all.  (Two workgroups per CU at least: of at most 256 registers the products' results are in those
-// that other instructions can read.)
+// that other instructions can read; head sizes above 224 would spill for that: 512 tokens, 8 heads on 1 of 256, 20000 before them 33.5 us so, 26.1 with one.)
 template <int NF, int LOG>
-__global__ __launch_bounds__(kScoreThreads, 2) void score_prompt_kernel(const int8_t* __restrict__ coded, const float* __restrict__ scales,
+__global__ __launch_bounds__(kScoreThreads, NF < 8 ? 2 : 1) void score_prompt_kernel(const int8_t* __restrict__ coded, const float* __restrict__ scales,
                                                                       const int8_t* __restrict__ codes, const int8_t* __restrict__ exponents, Tokens tk,
                                                                       const int32_t* __restrict__ block_table, int bt_stride, float* __restrict__ scores,
                                                                       int64_t row_words, int Hkv, int unit0, int t0, int t1, int run) {

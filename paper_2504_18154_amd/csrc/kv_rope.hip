@@ -12,6 +12,8 @@
 //
 // The blocks of the batch are numbered as in kv_append.hip (cu_q[b] / 16 + 2 b); a workgroup takes the tokens of one
 // block and a run of heads of K and Q, or up to four heads of V, whose transposition goes through LDS.
+#include <type_traits>
+
 #include "common.h"
 
 namespace eco {
@@ -59,7 +61,11 @@ __device__ __forceinline__ E rounded(float x) {
 }
 
 // WV elements at a time: a 16-byte unit, or half of one where the halves of the pairs do not begin with a unit.
-template <typename E, int WV, bool kAdjacent>
+// kEach (halves, of heads that are not turned as a whole and whose units a wavefront has together): a thread turns one unit and reads the other half of its pairs besides;
+// otherwise it turns both.  (Of accesses to the second half few lanes would have any: 32 elements turned, 86 k tokens, 8 heads on 1 of 256 264 us, so 227; 16 k tokens, 64 on 8 of 128
+// 173, so 163.  Heads that are turned as a whole: 3 prompts, 2.3 k tokens, 64 on 8 of 128 40.6 us, so 48.6.)  In place the other half's owner has it from memory before either stores: loads
+// and stores are instructions of the one wavefront, in this order.
+template <typename E, int WV, bool kAdjacent, bool kEach>
 __global__ __launch_bounds__(kRopeThreads) void kv_append_rope_kernel(
     E* __restrict__ k_cache, E* __restrict__ v_cache, const E* __restrict__ k_new, const E* __restrict__ v_new, int new_row_stride, const E* q, E* q_out,
     int q_row_stride, int q_out_row_stride, const Turns turns, const int32_t* __restrict__ cu_q, const int32_t* __restrict__ ctx_before,
@@ -114,14 +120,14 @@ __global__ __launch_bounds__(kRopeThreads) void kv_append_rope_kernel(
   // K heads, then Q heads: h_begin .. h_end - 1 of the list
   const int R = turns.rotary, half = R >> 1, total = Hkv + (q ? Hq : 0);
   const int h_begin = ((int)blockIdx.y - v_slices) * per_slice, h_end = min(h_begin + per_slice, total);
-  const int turned = kAdjacent ? R / WV : half / WV, places = turned + (D - R) / WV;  // of a head vector, a thread each
+  const int turned = kAdjacent || kEach ? R / WV : half / WV, places = turned + (D - R) / WV;  // of a head vector, a thread each
   const int per_head = 16 * places, at_once = max(1, kRopeThreads / per_head);
   E* const kdst = k_cache + (size_t)blk * Hkv * 16 * D;
   for (int base = 0; base < per_head; base += kRopeThreads) {
     const int sub = tid / per_head, it = base + tid - sub * per_head, slot = it / places, c = it - slot * places;
     if (sub >= at_once || it >= per_head || slot < lo || slot >= hi) continue;
     const int tok = t_slot0 + slot;
-    const bool turn = c < turned;
+    const bool turn = c < turned, second = kEach && turn && c * WV >= half;  // second: of the second half
     const int e0 = turn ? c * WV : R + (c - turned) * WV;
     constexpr int kPairs = kAdjacent ? WV / 2 : WV;
     Angle an[kPairs];
@@ -129,7 +135,7 @@ __global__ __launch_bounds__(kRopeThreads) void kv_append_rope_kernel(
     for (int i = 0; i < kPairs; ++i) an[i] = Angle{1.f, 0.f};
     if (turn)
 #pragma unroll
-      for (int i = 0; i < kPairs; ++i) an[i] = angle_of_pair(turns, c * kPairs + i, tok, (j << 4) + slot);
+      for (int i = 0; i < kPairs; ++i) an[i] = angle_of_pair(turns, (second ? c - half / WV : c) * kPairs + i, tok, (j << 4) + slot);
     const E* const krow = k_new + (size_t)tok * new_row_stride + e0;
     const E* const qrow = q + (size_t)tok * q_row_stride + e0;
     E* const orow = q_out + (size_t)tok * q_out_row_stride + e0;
@@ -144,7 +150,7 @@ __global__ __launch_bounds__(kRopeThreads) void kv_append_rope_kernel(
         const int h = min(h0 + n * at_once, h_end - 1);
         const E* const src = h < Hkv ? krow + h * D : qrow + (h - Hkv) * D;
         a[n] = *reinterpret_cast<const Unit*>(src);
-        if (two) d[n] = *reinterpret_cast<const Unit*>(src + half);
+        if (two) d[n] = *reinterpret_cast<const Unit*>(second ? src - half : src + half);
       }
 #pragma unroll
       for (int n = 0; n < kAhead; ++n) {
@@ -156,13 +162,13 @@ __global__ __launch_bounds__(kRopeThreads) void kv_append_rope_kernel(
             E& ea = a[n].e[kAdjacent ? 2 * i : i];
             E& eb = kAdjacent ? a[n].e[2 * i + 1] : d[n].e[i];
             const float x = value(ea), y = value(eb);
-            ea = rounded<E>(x * an[i].c - y * an[i].s);
-            eb = rounded<E>(x * an[i].s + y * an[i].c);
+            ea = rounded<E>(second ? y * an[i].s + x * an[i].c : x * an[i].c - y * an[i].s);
+            if (!kEach) eb = rounded<E>(x * an[i].s + y * an[i].c);
           }
         }
         E* const to = h < Hkv ? kplace + (size_t)h * 16 * D : orow + (h - Hkv) * D;
         *reinterpret_cast<Unit*>(to) = a[n];
-        if (two) *reinterpret_cast<Unit*>(h < Hkv ? kplace2 + (size_t)h * 16 * D : to + half) = d[n];
+        if (two && !kEach) *reinterpret_cast<Unit*>(h < Hkv ? kplace2 + (size_t)h * 16 * D : to + half) = d[n];
       }
     }
   }
@@ -277,10 +283,15 @@ void launch_typed(const RopeAppend& a, const Turns& turns, int num_cu, hipStream
   };
   constexpr int X = Elem<E>::X;
   if constexpr (kAdjacent) {
-    go(&kv_append_rope_kernel<E, X, true>);
+    go(&kv_append_rope_kernel<E, X, true, false>);
   } else {
-    if (turns.rotary / 2 % X == 0) go(&kv_append_rope_kernel<E, X, false>);
-    else go(&kv_append_rope_kernel<E, X / 2, false>);
+    auto halves = [&](auto units) {
+      constexpr int WV = decltype(units)::value;
+      if (turns.rotary < D && 64 % (D / WV) == 0) go(&kv_append_rope_kernel<E, WV, false, true>);
+      else go(&kv_append_rope_kernel<E, WV, false, false>);
+    };
+    if (turns.rotary / 2 % X == 0) halves(std::integral_constant<int, X>());
+    else halves(std::integral_constant<int, X / 2>());
   }
 }
 

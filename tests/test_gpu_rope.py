@@ -158,3 +158,13 @@ def test_what_the_binding_refuses():
         ctx.kv_append_rope(kc, vc, k, k, cu, before, bt, rope)          # two coordinates and no positions
     ctx.kv_append_rope(kc, vc, k, k, cu, before, bt, rope, **good)
     ctx.close()
+
+
+@pytest.mark.parametrize("dtype,D,Hq,Hkv,rotary", [("bf16", 128, 8, 2, 32), ("bf16", 256, 6, 1, 64), ("bf16", 64, 4, 4, 8), ("bf16", 80, 4, 2, 32), ("f32", 128, 4, 2, 44),
+                                                   ("f32", 256, 2, 1, 32), ("f32", 8, 3, 3, 4)])
+def test_parts_of_heads_in_place(dtype, D, Hq, Hkv, rotary):
+    """Halves of a part of the head, each turned where it lies; slices of a projection's rows."""
+    for new, before in (([40, 1, 700], [9, 16, 3]), ([2000], [5])):
+        _check(dtype, D, Hq, Hkv, before, new, rotary=rotary, in_place=True, pad=2)
+        _check(dtype, D, Hq, Hkv, before, new, rotary=rotary, in_place=True, fused=True)
+        _check(dtype, D, Hq, Hkv, before, new, rotary=rotary, axes=2, seed=3)

@@ -708,7 +708,11 @@ hipError_t launch_block_select(const ecoserve_layout& L, const SelectArgs& a, co
     auto go = [&](auto kernel, int threads, int at_once) {
       hipLaunchKernelGGL(kernel, dim3((unsigned)((rows + at_once - 1) / at_once)), dim3(threads), 0, s, a.scores, row_words, x.tk, to, a.Hkv, t0, rows);
     };
-    if (row_words <= 2048) go(&choose_kernel<1, 32, 512>, 256, 4);
+    // A wavefront to a row, or, of few and of long rows, several (64 heads on 8, us of a call.  2048 blocks: 128 rows 19.5, with four 15.9, 2048 34.3 / 30.1, 8192 69.0 / 72.8; 6900
+    // blocks, four / sixteen: 128 rows 23.6 / 21.6, 512 30.1 / 29.7, 1024 40.1 / 43.4, 4096 101 / 123).
+    if (row_words <= 2048 && rows > 8 * a.num_cu) go(&choose_kernel<1, 32, 512>, 256, 4);
+    else if (row_words <= 2048) go(&choose_kernel<4, 8, 1024>, 256, 1);
+    else if (row_words <= 8192 && rows > 3 * a.num_cu) go(&choose_kernel<4, 32, 1024>, 256, 1);
     else if (row_words <= 8192) go(&choose_kernel<16, 8, 1024>, 1024, 1);
     else if (row_words <= 32768) go(&choose_kernel<16, 32, 1024>, 1024, 1);
     else go(&choose_kernel<16, 0, 1024>, 1024, 1);

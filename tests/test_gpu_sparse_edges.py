@@ -175,3 +175,26 @@ def test_as_many_parts_as_there_are(dtype, D, Hq, Hkv):
         _compare(b, lists, out, lse, name=f"{K} entries")
         assert torch.equal(out, _attend(b, lists, ragged=False)[0])
     b.ctx.close()
+
+
+@pytest.mark.parametrize("blocks", [300, 2040, 2100, 8190])
+def test_few_and_many_rows_choose_alike(blocks):
+    """Prompts of as many tokens as each way of choosing takes: the lists of a step of the token alone."""
+    from paper_2504_18154_amd import binding
+    rng = np.random.default_rng(blocks)
+    Hq, Hkv, D, pool = 8, 4, 32, 400
+    ctx = binding.Context(Hq, Hkv, D, pool, "bf16", 2, blocks)
+    summary = torch.randint(-100, 100, ctx.new_summary().shape, dtype=torch.int8, device="cuda")
+    table = rng.integers(0, pool, size=(2, blocks)).astype(np.int32)
+    for T in (20, 250, 700):
+        new = np.array([T // 3, T - T // 3])
+        before = np.array([blocks * 16 - T, blocks * 16 - T - 500], dtype=np.int32)
+        q = torch.randn(T, Hq, D, device="cuda").to(torch.bfloat16)
+        lists = torch.full((T, Hkv, 12), -7, dtype=torch.int32, device="cuda")
+        ctx.block_select(q, summary, dev_i32(before), dev_i32(table), lists, blocks * 16, keep_first=1, keep_last=2, cu_q=dev_i32(wl.cu_from_lengths(new)))
+        seq, pos = np.repeat(np.arange(2), new), np.concatenate([b + np.arange(n) for b, n in zip(before, new)])
+        one = torch.full((1, Hkv, 12), -7, dtype=torch.int32, device="cuda")
+        for t in range(0, T, max(1, T // 40)):
+            ctx.block_select(q[t:t + 1], summary, dev_i32(pos[t:t + 1]), dev_i32(table[seq[t]:seq[t] + 1]), one, blocks * 16, keep_first=1, keep_last=2)
+            assert torch.equal(one[0], lists[t]), (T, t)
+    ctx.close()

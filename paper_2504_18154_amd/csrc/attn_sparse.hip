@@ -31,8 +31,9 @@ constexpr int kAgent = 16;         // past the caches that XCDs do not share
 typedef const void __attribute__((address_space(1)))* gptr_t;
 typedef void __attribute__((address_space(3)))* lptr_t;
 constexpr float kRaise = 8.f;      // the exponent offset is raised when a score exceeds it by more (log2 units; 2^8: 256, below)
+constexpr float kLowest = -3.402823466e38f;  // the offset of keys that all score -inf: their weights are 0, and there are keys
 
-// The state of 16 columns: m exponent offset (-inf: no key yet), l this lane's share of the sum, o unnormalised.
+// The state of 16 columns: m exponent offset (-inf: no key yet, kLowest or more: keys), l this lane's share of the sum, o unnormalised.
 template <int NV>
 struct State {
   float m = -INFINITY, l = 0.f;
@@ -56,21 +57,20 @@ struct State {
     for (int t = 0; t < N; ++t) top = fmaxf(top, fmaxf(fmaxf(s[t][0], s[t][1]), fmaxf(s[t][2], s[t][3])));
     return top;
   }
-  // scores q.k (-inf: no key) to weights
+  // scores q.k to weights; -inf: no key, or one that scores so (every column has a key: m is above -inf from here on)
   template <int N>
   __device__ __forceinline__ void weights(f32x4 (&s)[N], float scale_log2e) {
-    const float top = largest(s) * scale_log2e;
+    const float top = fmaxf(largest(s) * scale_log2e, kLowest);
     if (__any(top > m + kRaise)) raise(top);
-    const float mu = m == -INFINITY ? 0.f : m;
 #pragma unroll
     for (int t = 0; t < N; ++t) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) s[t][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][i], scale_log2e, -mu));
+      for (int i = 0; i < 4; ++i) s[t][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][i], scale_log2e, -m));
       l += (s[t][0] + s[t][1]) + (s[t][2] + s[t][3]);
     }
   }
   // The same of 32 keys, for lanes that `counts` (the others have no weight, whatever their finite scores); scores beyond the offset are looked for among the weights, those above
-  // 2^kRaise, in the order of their bits (a NaN is above; an offset that no key has set yet, -inf, makes any weight infinite).
+  // 2^kRaise, in the order of their bits (a NaN is above; an offset that no key has set yet, -inf, makes any weight infinite or a NaN).
   __device__ __forceinline__ void weights_of(const f32x4 (&s)[2], f32x4 (&w)[2], float scale_log2e, bool counts) {
     auto all = [&] {
       const float mu = counts ? m : INFINITY;
@@ -86,7 +86,7 @@ struct State {
     most = max(max(most, bits(1, 1)), bits(1, 2));
     most = max(most, bits(1, 3));
     if (__any(most > __float_as_uint(256.f))) {
-      raise(counts ? largest(s) * scale_log2e : -INFINITY);
+      raise(counts ? fmaxf(largest(s) * scale_log2e, kLowest) : -INFINITY);
       all();
     }
 #pragma unroll
@@ -285,15 +285,16 @@ struct Walk<float, KS> {
 __device__ __forceinline__ void store4(float* p, const f32x4& v) { *reinterpret_cast<f32x4*>(p) = v; }
 __device__ __forceinline__ void store4(uint16_t* p, const f32x4& v) { *reinterpret_cast<u32x2*>(p) = u32x2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])}; }
 
-// The result of a row: o / l and the log of the sum of its weights; without keys 0 and -inf.
+// The result of a row: o / l and the log of the sum of its weights; without keys (m -inf) 0 and -inf; of keys that all score -inf (l 0) 0 / 0.
 template <typename E>
-__device__ __forceinline__ void store_row(E* out, f32x4 o, float l) {
-  const float inv = l == 0.f ? 0.f : 1.f / l;
+__device__ __forceinline__ void store_row(E* out, f32x4 o, float m, float l) {
+  const bool none = m == -INFINITY;
+  const float inv = l == 0.f ? NAN : 1.f / l;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) o[i] = l == 0.f ? 0.f : o[i] * inv;
+  for (int i = 0; i < 4; ++i) o[i] = none ? 0.f : o[i] * inv;
   store4(out, o);
 }
-__device__ __forceinline__ float row_lse(float m, float l) { return l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2; }
+__device__ __forceinline__ float row_lse(float m, float l) { return m == -INFINITY ? m : l == 0.f ? NAN : (m + log2f(l)) * kLn2; }
 
 // Workgroup x: K/V head x % Hkv, then part, then token, from t0 on.  With several parts: counters [T][Hkv] are zero and stay so.
 template <typename E, int KS>
@@ -383,7 +384,7 @@ __global__ __launch_bounds__(kWaves * 64) void attn_sparse_kernel(const E* __res
       E* const to = out + (row0 + col) * D + quad * 4;
 #pragma unroll
       for (int dt = 0; dt < NV; ++dt)
-        if (dt * 16 + quad * 4 < D) store_row(to + dt * 16, st.o[dt], total);
+        if (dt * 16 + quad * 4 < D) store_row(to + dt * 16, st.o[dt], M, total);
       if (lse && quad == 0) lse[row0 + col] = row_lse(M, total);
     } else {
       const __amdgpu_buffer_rsrc_t to = __builtin_amdgcn_make_buffer_rsrc(my_states, 0, range, kRsrc);
@@ -441,7 +442,7 @@ __global__ __launch_bounds__(kWaves * 64) void attn_sparse_kernel(const E* __res
     for (int s = kLanes; s < 64; s <<= 1)
 #pragma unroll
       for (int e = 0; e < 4; ++e) o[e] += __shfl_xor(o[e], s);
-    if (side == 0 && el < D) store_row(out + (row0 + h) * D + el, o, total);
+    if (side == 0 && el < D) store_row(out + (row0 + h) * D + el, o, M, total);
     if (lse && lane == 0) lse[row0 + h] = row_lse(M, total);
   }
 }
@@ -663,7 +664,7 @@ __global__ __launch_bounds__(group_waves(KS) * 64, group_waves(KS) / 4) void att
     const size_t row = (size_t)token * (Hkv * G) + g * G + h;
 #pragma unroll
     for (int dt = 0; dt < NV; ++dt)
-      if (dt * 16 + quad * 4 < D) store_row(out + row * D + dt * 16 + quad * 4, st.o[dt], st.l);
+      if (dt * 16 + quad * 4 < D) store_row(out + row * D + dt * 16 + quad * 4, st.o[dt], st.m, st.l);
     if (lse && quad == 0) lse[row] = row_lse(st.m, st.l);
   };
   float odd = 0.f;  // not a number once a sum is not finite

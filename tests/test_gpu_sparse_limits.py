@@ -1,0 +1,72 @@
+"""Attention over listed blocks, block summaries and selection at the ends of their ranges: scores of minus infinity, sizes of keys far apart, scores beyond what fp32 holds."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import sparse_oracle as so
+from tests.parity_util import dev_i32, say
+from tests.test_gpu_sparse import Batch, _all_summarised, _attend, _compare, _of_prompts, _random_lists, _select, _summary_host
+
+pytestmark = pytest.mark.gpu
+
+
+# ---- scores of minus infinity ---------------------------------------------------------------------
+# A key of -inf in a channel in which the queries are positive scores -inf: its weight is 0, and a row whose keys all score so is 0 / 0.
+
+
+def _with_a_block_of_minus_infinity(dtype, D, Hq, Hkv, before, new, block, seed):
+    b = Batch(dtype, D, Hq, Hkv, before, new, seed=seed)
+    b.q[:, :, 0] = b.q[:, :, 0].abs() + 0.5
+    b.keys[b.table[:, block], 0, :, 0] = -float("inf")
+    b.upload()
+    return b
+
+
+def _check_minus_infinity(b, lists, out, lse, block, tokens, name, **kw):
+    """Rows of K/V head 0 that list `block` and others: as if they did not list it; that list it alone: NaN.  Rows without keys: 0 and -inf."""
+    o, l = out.float().cpu().numpy(), lse.cpu().numpy()
+    others = lists.copy()
+    others[:, 0][others[:, 0] == block] = -1
+    keys = lambda j, t: any(0 <= x <= b.pos[t] // 16 for x in j)
+    undefined = [t for t in range(b.T) if keys(lists[t, 0], t) and not keys(others[t, 0], t)]
+    assert undefined and np.isnan(o[undefined][:, :b.G]).all() and np.isnan(l[undefined][:, :b.G]).all()
+    assert np.isfinite(np.delete(o[:, :b.G], undefined, 0)).all()
+    empty = [t for t in range(b.T) if not keys(lists[t, 0], t)]
+    assert empty and (o[empty][:, :b.G] == 0).all() and np.isneginf(l[empty][:, :b.G]).all()
+    _compare(b, others, out, lse, name=name, tokens=[t for t in tokens if t not in set(undefined)], **kw)
+
+
+@pytest.mark.parametrize("dtype,D,Hq,Hkv", [("bf16", 128, 16, 2), ("bf16", 64, 4, 2), ("f32", 64, 4, 2), ("f32", 256, 3, 1)])
+def test_scores_of_minus_infinity_in_a_step(dtype, D, Hq, Hkv):
+    b = _with_a_block_of_minus_infinity(dtype, D, Hq, Hkv, [3000] * 6, [1] * 6, 1, D)
+    rng = np.random.default_rng(D)
+    for K in (6, 200):                                           # whole lists, and parts
+        lists = np.full((6, Hkv, K), -1, dtype=np.int32)
+        for t in range(6):
+            for g in range(Hkv):
+                lists[t, g, K // 2:] = rng.choice(np.arange(2, 188), K - K // 2)
+        lists[0, 0, 0] = 1
+        lists[1, 0, :K // 2] = 1                                 # (parts that have nothing else)
+        lists[2, 0] = lists[2, 0, ::-1]
+        lists[2, 0, -1] = 1
+        lists[3, 0] = np.where(np.arange(K) < K // 2, 1, -1)     # alone
+        lists[4, 0] = -1
+        out, lse = _attend(b, lists, ragged=False)
+        _check_minus_infinity(b, lists, out, lse, 1, range(6), f"{K} entries")
+    b.ctx.close()
+
+
+def test_scores_of_minus_infinity_among_prompts():
+    b = _with_a_block_of_minus_infinity("bf16", 128, 16, 2, [100], [2100], 1, 1)
+    lists = _random_lists(b, 5, np.random.default_rng(1))
+    for t in range(b.T):
+        n = b.pos[t] // 16 + 1
+        lists[t, 0] = [[1, 3, n - 1, -1, -1], [1, -1, -1, -1, -1], [3, 5, -1, -1, -1], [-1] * 5, [n - 1, 2, 0, 1, -1]][t % 5]
+    out, lse = _attend(b, lists)
+    _check_minus_infinity(b, lists, out, lse, 1, _of_prompts(b), "prompts", rounded_weights=True)
+    lists[1000, 0, 3:] = 3                                       # (a block twice: the tokens around it are taken one by one)
+    out, lse = _attend(b, lists)
+    _check_minus_infinity(b, lists, out, lse, 1, range(960, 1040), "prompts, one by one", rounded_weights=True)
+    b.ctx.close()

@@ -427,7 +427,7 @@ __global__ __launch_bounds__(kWaves * 64) void attn_sparse_kernel(const E* __res
         for (int i = 0; i < kAhead; ++i) {
           const int k = k0 + i * kAtOnce + side;
           const float w = __shfl(f, min(k, 63));
-          if (k < parts && w != 0.f)
+          if (k < parts)  // (also parts whose weight is 0: an infinite value there is no number times it)
 #pragma unroll
             for (int e = 0; e < 4; ++e) o[e] += x[i][e] * w;
         }

@@ -70,3 +70,21 @@ def test_scores_of_minus_infinity_among_prompts():
     out, lse = _attend(b, lists)
     _check_minus_infinity(b, lists, out, lse, 1, range(960, 1040), "prompts, one by one", rounded_weights=True)
     b.ctx.close()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("key", [-float("inf"), -1e4], ids=["minus-infinity", "far-below"])
+def test_an_infinite_value_under_the_smallest_weights(dtype, key):
+    """It reaches the row whichever part of a list, wavefront or group the block is in, also where fp32 holds no weight so small (zero times infinity)."""
+    b = _with_a_block_of_minus_infinity(dtype, 64, 4, 2, [3000] * 2, [1] * 2, 1, 3)
+    b.keys[b.table[:, 1], 0, :, 0] = key
+    b.vals[b.table[:, 1], 0, :, 9] = float("inf")
+    b.upload()
+    for K in (6, 200):
+        for n in range(1, min(K, 33)):                           # (as many entries as the first part has, among others)
+            lists = np.tile(2 + np.arange(K, dtype=np.int32) % 184, (2, 2, 1))
+            lists[0, 0, :n] = 1
+            out, _ = _attend(b, lists, ragged=False)
+            o = out.float().cpu().numpy()
+            assert not np.isfinite(o[0, :2, 9]).any() and np.isfinite(np.delete(o[0, :2], 9, 1)).all() and np.isfinite(o[0, 2:]).all() and np.isfinite(o[1]).all(), (K, n)
+    b.ctx.close()

@@ -387,6 +387,8 @@ typedef struct {
  *                  calls), 16-byte aligned; both NULL: only K and V.  They may be the same array with the same stride;
  *                  arrays that overlap otherwise: undefined.  Rows of q_out that belong to no sequence are left alone.
  *   everything else as in ecoserve_kv_append_strided (max_new_len <= 1 again selects the one-token launch).
+ * Tokens at negative positions (ctx_before[b] + i < 0: places of a padded batch) store nothing, and their rows of q_out are
+ * left alone.
  * Of the options ECOSERVE_OPT_PROFILE counts it as an append; the others do not concern it, nor the calls below.
  */
 int ecoserve_kv_append_rope(ecoserve_ctx* ctx, const ecoserve_rope* rope, const double* inv_freq, const int32_t* positions,

@@ -81,6 +81,7 @@ __global__ __launch_bounds__(kRopeThreads) void kv_append_rope_kernel(
   const int nth = (int)blockIdx.x - first_unit(tok0, b);
   if (S <= 0 || nth > ((cb + S - 1) >> 4) - (cb >> 4)) return;
   const int tid = threadIdx.x, j = (cb >> 4) + nth;
+  if (j < 0) return;  // (tokens at negative positions: places of a padded batch)
   const int lo = max(0, cb - (j << 4)), hi = min(16, cb + S - (j << 4));  // addressed slots of the block
   const int t_slot0 = tok0 + (j << 4) - cb;                               // packed token of slot 0 (may lie before tok0)
   const int64_t blk = block_table[(size_t)b * bt_stride + j];

@@ -1,0 +1,56 @@
+"""Places of a padded batch, which stand at negative positions, in the calls for long contexts: nothing is stored for them, and what the other tokens leave is what they leave
+without them."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import sparse_oracle as so
+from paper_2504_18154_amd import workloads as wl
+from tests.parity_util import dev_i32, say
+
+pytestmark = pytest.mark.gpu
+
+STEP = [-1, 5, -20, 15, -16, -1], [1, 1, 1, 1, 1, 0]
+PROMPTS = [-1, 5, -20, -3, -16, -40, 0], [1, 3, 7, 20, 49, 41, 2]
+
+
+def _tables(before, new):
+    """Rows of distinct blocks for what is at positions of 0 and more; in every other place one block that belongs to nobody."""
+    per = (np.maximum(before + new, 0) + 15) // 16
+    table = np.full((len(new), int(per.max()) + 2), int(per.sum()), dtype=np.int32)
+    at = 0
+    for b, n in enumerate(per):
+        table[b, :n] = np.arange(at, at + n)
+        at += n
+    return table, at + 1
+
+
+@pytest.mark.parametrize("dtype,D,Hq,Hkv,rotary,adjacent", [("bf16", 128, 8, 2, None, False), ("bf16", 128, 8, 2, 32, False), ("bf16", 72, 3, 3, 24, True), ("f32", 64, 4, 1, None, False)])
+@pytest.mark.parametrize("in_place", [False, True])
+@pytest.mark.parametrize("batch,most", [(STEP, 1), (STEP, None), (PROMPTS, None)], ids=["step", "step-as-prompts", "prompts"])
+def test_rotated_append(batch, most, in_place, dtype, D, Hq, Hkv, rotary, adjacent):
+    from paper_2504_18154_amd import binding
+    before, new = (np.array(x) for x in batch)
+    table, blocks = _tables(before, new)
+    B, T = len(new), int(new.sum())
+    say(f"{dtype}, D {D}, heads {Hq}/{Hkv}, new {new.tolist()} behind {before.tolist()}")
+    ctx = binding.Context(Hq, Hkv, D, blocks, dtype, B, table.shape[1])
+    rope = binding.Rope(10000.0 ** (-torch.arange((rotary or D) // 2, dtype=torch.float64, device="cuda") / 32), "adjacent" if adjacent else "halves")
+    q, k, v = (wl.randn((T, h, D), dtype, 7 + n).cuda() for n, h in enumerate((Hq, Hkv, Hkv)))
+
+    def append(before, new, q, k, v, most):
+        kc, vc = ctx.new_cache()
+        out = q.clone() if in_place else torch.full_like(q, 7.0)
+        ctx.kv_append_rope(kc, vc, k, v, dev_i32(wl.cu_from_lengths(new)), dev_i32(before), dev_i32(table), rope, q=out if in_place else q, q_out=out, max_new_len=most)
+        return kc, vc, out
+
+    place = np.concatenate([b + np.arange(n) for b, n in zip(before, new)])
+    there = torch.as_tensor(place >= 0)
+    got = append(before, new, q, k, v, most)
+    skipped = np.minimum(np.maximum(-before, 0), new)
+    want = append(before + skipped, new - skipped, *(t[there].contiguous() for t in (q, k, v)), most)
+    bits = lambda t: t.contiguous().view(torch.uint8)
+    assert torch.equal(bits(got[0]), bits(want[0])) and torch.equal(bits(got[1]), bits(want[1]))
+    assert torch.equal(bits(got[2][there]), bits(want[2])) and torch.equal(bits(got[2][~there]), bits(q[~there] if in_place else torch.full_like(q[~there], 7.0)))
+    assert ctx.k_logical(got[0])[blocks - 1].isnan().all() and ctx.v_logical(got[1])[blocks - 1].isnan().all()      # (the sentinel of new_cache)
+    ctx.close()

@@ -421,6 +421,7 @@ size_t ecoserve_summary_bytes(const ecoserve_layout* layout); /* 0 if the layout
 /*
  * Summarises the blocks that the call's tokens have filled: those of which a new token took slot 15.  Call it behind every
  * append, with the same arguments; blocks that are not full yet keep what their summary holds, and nothing reads it.
+ * Tokens at negative positions fill nothing.
  *   k_cache : dev, 16-byte aligned;  summary : dev, in/out, layout above, 16-byte aligned
  *   cu_q, ctx_before, block_table, bt_stride, B, T, max_new_len, stream : as in ecoserve_kv_append
  */

@@ -72,9 +72,9 @@ __global__ __launch_bounds__(kSummaryThreads) void kv_summary_kernel(const E* __
   typedef uint32_t u4 __attribute__((ext_vector_type(4)));
   auto first_unit = [](int cu, int b) { return (cu >> 4) + b; };
   const SeqOf seq = find_sequence(cu_q, ctx_before, B, blockIdx.x, first_unit);
-  const int j = (seq.cb >> 4) + (int)blockIdx.x - first_unit(seq.tok0, seq.b);
+  const int j = (max(seq.cb, 0) >> 4) + (int)blockIdx.x - first_unit(seq.tok0, seq.b);  // (tokens at negative positions fill nothing)
   const int g = blockIdx.y * (kSummaryThreads / 64) + (threadIdx.x >> 6), lane = threadIdx.x & 63;
-  if (seq.S <= 0 || seq.cb < 0 || j >= (seq.cb + seq.S) >> 4 || g >= Hkv) return;
+  if (seq.S <= 0 || j >= (seq.cb + seq.S) >> 4 || g >= Hkv) return;
   const int64_t blk = block_table[(size_t)seq.b * bt_stride + j];
   const E* const src = k_cache + ((size_t)blk * Hkv + g) * 16 * D;
   const int units = D / X, Dp = summary_channels(D);

@@ -7,6 +7,7 @@ import torch
 from oracle import sparse_oracle as so
 from paper_2504_18154_amd import workloads as wl
 from tests.parity_util import dev_i32, say
+from tests.test_gpu_sparse import Batch, _summary_host
 
 pytestmark = pytest.mark.gpu
 
@@ -54,3 +55,22 @@ def test_rotated_append(batch, most, in_place, dtype, D, Hq, Hkv, rotary, adjace
     assert torch.equal(bits(got[2][there]), bits(want[2])) and torch.equal(bits(got[2][~there]), bits(q[~there] if in_place else torch.full_like(q[~there], 7.0)))
     assert ctx.k_logical(got[0])[blocks - 1].isnan().all() and ctx.v_logical(got[1])[blocks - 1].isnan().all()      # (the sentinel of new_cache)
     ctx.close()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("batch", [([-1, 15, -20, 31, -16, -1], [1, 1, 1, 1, 1, 0]), (PROMPTS[0] + [-2, -5], PROMPTS[1] + [34, 21])], ids=["step", "prompts"])
+def test_summaries(batch, dtype):
+    """A sequence that begins with places of the padding has its blocks summarised all the same."""
+    b = Batch(dtype, 40, 6, 2, *batch, seed=3)
+    summary = torch.full_like(b.ctx.new_summary(), 85)
+    codes, exps = _summary_host(b.ctx.layout, b.summarise(summary))
+    filled = {int(b.table[s, j]) for s in range(b.B) for j in range(max(b.before[s], 0) // 16, b.total[s] // 16) if b.new[s]}
+    assert len(filled) >= 2
+    for blk in range(codes.shape[0]):
+        for g in range(b.Hkv):
+            if blk not in filled:
+                assert (codes[blk, g] == 85).all() and exps[blk, g] == 85, blk
+                continue
+            want, e = so.summarise(b.keys[blk, g].float().numpy())
+            assert exps[blk, g] == e and np.array_equal(codes[blk, g, :, :b.D], want), (blk, g)
+    b.ctx.close()

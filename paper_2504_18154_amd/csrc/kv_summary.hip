@@ -129,7 +129,9 @@ __global__ __launch_bounds__(kSummaryThreads) void kv_summary_kernel(const E* __
       out[w] = 0;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const float x = (lane & 1) ? floorf(ldexpf(low[r][4 * w + i], -e)) : ceilf(ldexpf(top[r][4 * w + i], -e));
+        // (so far below the block's largest that fp32 scales it to zero, a key still takes a unit outward)
+        const float key = (lane & 1) ? low[r][4 * w + i] : top[r][4 * w + i], scaled = ldexpf(key, -e);
+        const float x = (lane & 1) ? (key < 0.f ? fminf(floorf(scaled), -1.f) : floorf(scaled)) : (key > 0.f ? fmaxf(ceilf(scaled), 1.f) : ceilf(scaled));
         out[w] |= (fine ? (uint32_t)(int)x & 0xffu : 0u) << (8 * i);
       }
     }

@@ -88,3 +88,23 @@ def test_an_infinite_value_under_the_smallest_weights(dtype, key):
             o = out.float().cpu().numpy()
             assert not np.isfinite(o[0, :2, 9]).any() and np.isfinite(np.delete(o[0, :2], 9, 1)).all() and np.isfinite(o[0, 2:]).all() and np.isfinite(o[1]).all(), (K, n)
     b.ctx.close()
+
+
+# ---- keys of sizes far apart ----------------------------------------------------------------------
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_codes_bound_keys_far_below_the_largest(dtype):
+    """Rounded outward however small a key is beside the block's largest: below a unit of the code by more than fp32 can say, it still takes one."""
+    b = Batch(dtype, 32, 4, 2, [0], [64], seed=2)
+    b.keys[:, :, :, 0] = 1e30
+    for j, small in enumerate((1e-30, -1e-30, 1e-38, 3.0)):
+        b.keys[b.table[0, j], :, :, 1:] = small
+    b.keys[b.table[0, 3], :, :, 2] = 0
+    b.upload()
+    codes, exps = _summary_host(b.ctx.layout, b.summarise())
+    for j in range(4):
+        for g in range(2):
+            want, e = so.summarise(b.keys[b.table[0, j], g].float().numpy())
+            assert exps[b.table[0, j], g] == e and np.array_equal(codes[b.table[0, j], g], want), (j, g)
+    b.ctx.close()

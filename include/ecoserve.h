@@ -443,8 +443,9 @@ int ecoserve_kv_summary(ecoserve_ctx* ctx, const void* k_cache, void* summary, c
  *                  table), ascending, -1 behind the last.  Rows of tokens behind cu_q[B] are left alone.
  *   num_selected : 1 .. 65536;  keep_first >= 0, keep_last >= 1, keep_first + keep_last <= num_selected
  *   max_ctx_len  : upper bound on any token's position + 1, as in ecoserve_attn_decode
- *   workspace    : dev, 16-byte aligned, at least ecoserve_select_workspace_bytes(layout, T, max_ctx_len) bytes; nothing in
- *                  it is kept from call to call
+ *   workspace    : dev, 16-byte aligned, at least ecoserve_select_workspace_bytes(layout, T, max_ctx_len) bytes, which may
+ *                  be those of a larger T or max_ctx_len, though they can be fewer (long calls take some of their tokens at a
+ *                  time, and are content with room for fewer); nothing in it is kept from call to call
  * Calls that share a context are ordered (rules at the top): steps of one token per sequence count in the context's merge
  * counters which workgroup comes last.  Calls that may run at the same time, recorded into graphs or not, need a context
  * and a workspace each.
@@ -466,10 +467,12 @@ int ecoserve_block_select(ecoserve_ctx* ctx, const void* q, int64_t q_row_stride
  *   blocks       : dev, int32[T][Hkv][num_selected], num_selected 1 .. 65536
  *   out, lse     : as in ecoserve_attn_prefill (lse may be NULL); rows of tokens behind cu_q[B] are left alone
  *   workspace    : dev, 16-byte aligned, at least ecoserve_sparse_workspace_bytes(ctx, T, num_selected) bytes (0 for many
- *                  tokens; NULL is fine then); rules as above, contexts included
+ *                  tokens; NULL is fine then); they neither grow nor shrink with T, and no call of the context takes more
+ *                  than ecoserve_sparse_workspace_most(ctx); rules as above, contexts included
  *   everything else as in ecoserve_block_select.
  */
 size_t ecoserve_sparse_workspace_bytes(const ecoserve_ctx* ctx, int32_t T, int32_t num_selected);
+size_t ecoserve_sparse_workspace_most(const ecoserve_ctx* ctx);
 int ecoserve_attn_sparse(ecoserve_ctx* ctx, const void* q, int64_t q_row_stride, const void* k_cache, const void* v_cache,
                          const int32_t* cu_q, const int32_t* ctx_before, const int32_t* block_table, int32_t bt_stride,
                          const int32_t* blocks, int32_t num_selected, void* out, float* lse, int32_t B, int32_t T,

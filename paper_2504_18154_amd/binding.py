@@ -32,7 +32,7 @@ EXPORTS = [
     "ecoserve_attn_decode_append", "ecoserve_attn_decode_noalloc", "ecoserve_probe_mfma_valu",
     "ecoserve_debug_prefill_queue_shares",
     "ecoserve_kv_append_rope", "ecoserve_summary_bytes", "ecoserve_kv_summary", "ecoserve_select_workspace_bytes",
-    "ecoserve_block_select", "ecoserve_sparse_workspace_bytes", "ecoserve_attn_sparse",
+    "ecoserve_block_select", "ecoserve_sparse_workspace_bytes", "ecoserve_sparse_workspace_most", "ecoserve_attn_sparse",
 ]
 ROPE_HALVES, ROPE_ADJACENT = 0, 1
 
@@ -89,7 +89,8 @@ def _load(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.ecoserve_select_workspace_bytes.argtypes = [ctypes.POINTER(Layout), i32, i32]
     lib.ecoserve_block_select.argtypes = [vp, vp, i64, vp, i32p, i32p, i32p, i32, i32p, i32, i32, i32, i32, i32, i32, vp, sz, vp]
     lib.ecoserve_sparse_workspace_bytes.argtypes = [vp, i32, i32]
-    for f in (lib.ecoserve_summary_bytes, lib.ecoserve_select_workspace_bytes, lib.ecoserve_sparse_workspace_bytes):
+    lib.ecoserve_sparse_workspace_most.argtypes = [vp]
+    for f in (lib.ecoserve_summary_bytes, lib.ecoserve_select_workspace_bytes, lib.ecoserve_sparse_workspace_bytes, lib.ecoserve_sparse_workspace_most):
         f.restype = sz
     lib.ecoserve_attn_sparse.argtypes = [vp, vp, i64, vp, vp, i32p, i32p, i32p, i32, i32p, i32, vp, vp, i32, i32, vp, sz, vp]
     lib.ecoserve_debug_validate.argtypes = [vp, i32p, i32p, i32p, i32, i32]
@@ -496,6 +497,10 @@ class Context:
 
     def sparse_workspace_bytes(self, T: int, entries: int) -> int:
         return int(_lib.ecoserve_sparse_workspace_bytes(self._h, int(T), int(entries)))
+
+    def sparse_workspace_most(self) -> int:
+        """As many as any call of attn_sparse takes."""
+        return int(_lib.ecoserve_sparse_workspace_most(self._h))
 
     def attn_sparse(self, q, k_cache, v_cache, ctx_before, block_table, blocks, out, lse=None, cu_q=None, workspace=None):
         """Attention over the listed blocks; cu_q None: one token per sequence."""

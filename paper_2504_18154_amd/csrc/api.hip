@@ -493,14 +493,14 @@ int ecoserve_block_select(ecoserve_ctx* c, const void* q, int64_t q_row_stride, 
   if (max_ctx_len < 1 || (int64_t)max_ctx_len > (int64_t)c->max_blocks_per_seq * kBlockSize || (int64_t)max_ctx_len > (int64_t)bt_stride * kBlockSize)
     return ECOSERVE_EINVAL;
   if (!aligned16(q) || !aligned16(summary) || !aligned16(workspace)) return ECOSERVE_EINVAL;
-  if (workspace_bytes < select_workspace_bytes(L, T, max_ctx_len)) return ECOSERVE_EINVAL;
+  if (workspace_bytes < select_workspace_least(L, T, max_ctx_len)) return ECOSERVE_EINVAL;
   DeviceGuard guard(c->device);
   if (!guard.ok) return ECOSERVE_EHIP;
-  const int64_t at_a_time = select_tokens_at_a_time(L, T, max_ctx_len);
+  const int64_t at_a_time = std::min<int64_t>(select_tokens_at_a_time(L, T, max_ctx_len), (int64_t)(workspace_bytes / (size_t)select_token_bytes(L, max_ctx_len)));
   int8_t* const coded = (int8_t*)workspace + at_a_time * select_score_bytes(L, max_ctx_len);
   float* const scales = (float*)(coded + at_a_time * select_coded_bytes(L));
   const SelectArgs a = {q, (int32_t)q_row_stride, cu_q, ctx_before, block_table, bt_stride, blocks, num_selected, keep_first, keep_last, B, T,
-                        L.num_q_heads, L.num_kv_heads, L.head_dim, c->num_cu, (float*)workspace, coded, scales, c->ws_count};
+                        L.num_q_heads, L.num_kv_heads, L.head_dim, c->num_cu, (float*)workspace, coded, scales, c->ws_count, (int32_t)at_a_time};
   return launch_block_select(L, a, summary, max_ctx_len, (hipStream_t)stream) == hipSuccess ? ECOSERVE_OK : ECOSERVE_EHIP;
 }
 
@@ -508,6 +508,8 @@ size_t ecoserve_sparse_workspace_bytes(const ecoserve_ctx* c, int32_t T, int32_t
   if (!c || T <= 0 || num_selected <= 0) return 0;
   return sparse_workspace_bytes(c->lay, T, num_selected, c->num_cu);
 }
+
+size_t ecoserve_sparse_workspace_most(const ecoserve_ctx* c) { return c ? sparse_workspace_most(c->lay, c->num_cu) : 0; }
 
 int ecoserve_attn_sparse(ecoserve_ctx* c, const void* q, int64_t q_row_stride, const void* k_cache, const void* v_cache, const int32_t* cu_q,
                          const int32_t* ctx_before, const int32_t* block_table, int32_t bt_stride, const int32_t* blocks, int32_t num_selected, void* out,

@@ -693,7 +693,7 @@ hipError_t launch_block_select(const ecoserve_layout& L, const SelectArgs& a, co
   const int8_t* const codes = (const int8_t*)summary;
   const Chosen to = {a.blocks, a.num_selected, a.keep_first, a.keep_last};
   const int64_t row_words = select_row_words(max_ctx_len);
-  const int at_a_time = select_tokens_at_a_time(L, a.T, max_ctx_len);
+  const int at_a_time = a.at_a_time;
   // (rows of no more blocks than are asked for, whatever the lengths: nothing is scored)
   const bool scored = row_words > a.num_selected, fused = scored && !a.cu_q && row_words <= kFusedBlocks;
   for (int t0 = 0; t0 < a.T; t0 += at_a_time) {

@@ -24,13 +24,22 @@ inline int32_t select_log_rows(const ecoserve_layout& L) {
 inline int64_t select_score_bytes(const ecoserve_layout& L, int32_t max_ctx_len) { return 4 * select_row_words(max_ctx_len) * L.num_kv_heads; }
 inline int64_t select_coded_bytes(const ecoserve_layout& L) { return ((int64_t)L.num_kv_heads << select_log_rows(L)) * (2 * summary_channels(L.head_dim)); }
 inline int64_t select_scale_bytes(const ecoserve_layout& L) { return ((int64_t)L.num_kv_heads << select_log_rows(L)) * 4; }
-// Tokens whose scores are held at a time: as many as 192 MiB take, which stay in the last-level cache (256 MiB) between the launches.
+inline int64_t select_token_bytes(const ecoserve_layout& L, int32_t max_ctx_len) {
+  return select_score_bytes(L, max_ctx_len) + select_coded_bytes(L) + select_scale_bytes(L);
+}
+// Tokens that are taken at a time: as many as 192 MiB of scores, and 256 MiB in all, take, which stay in the last-level cache (256 MiB) between the launches.
+// (8 prompts of 4096 tokens, 64 heads on 8 of 128: 256 MiB 577 us, with the scores bounded alone 610 MB 562; behind longer contexts the scores are what counts.)
 inline int32_t select_tokens_at_a_time(const ecoserve_layout& L, int32_t T, int32_t max_ctx_len) {
-  return (int32_t)std::max<int64_t>(1, std::min<int64_t>({(int64_t)T, ((int64_t)192 << 20) / select_score_bytes(L, max_ctx_len), 32768}));
+  return (int32_t)std::max<int64_t>(1, std::min<int64_t>({(int64_t)T, ((int64_t)192 << 20) / select_score_bytes(L, max_ctx_len),
+                                                          ((int64_t)256 << 20) / select_token_bytes(L, max_ctx_len), 32768}));
 }
 inline size_t select_workspace_bytes(const ecoserve_layout& L, int32_t T, int32_t max_ctx_len) {
-  const int64_t bytes = select_score_bytes(L, max_ctx_len) + select_coded_bytes(L) + select_scale_bytes(L);
-  return ((size_t)select_tokens_at_a_time(L, T, max_ctx_len) * bytes + 15) / 16 * 16;
+  return ((size_t)select_tokens_at_a_time(L, T, max_ctx_len) * select_token_bytes(L, max_ctx_len) + 15) / 16 * 16;
+}
+// What a call is content with: 96 MiB or a token's bytes, if it could use more.  That many any call of more tokens or longer contexts has been given: whole tokens
+// of at most 192 MiB of scores take more than half of those, and of at most 256 MiB in all more than half of these.
+inline size_t select_workspace_least(const ecoserve_layout& L, int32_t T, int32_t max_ctx_len) {
+  return std::min(select_workspace_bytes(L, T, max_ctx_len), std::max((size_t)96 << 20, select_workspace_bytes(L, 1, max_ctx_len)));
 }
 
 struct SelectArgs {
@@ -45,6 +54,7 @@ struct SelectArgs {
   int8_t* coded;
   float* scales;
   uint32_t* counters;  // one per (token, K/V head) where there is one token per sequence, zero between launches
+  int32_t at_a_time;   // tokens that the workspace has room for, or all that are taken at a time
 };
 
 // Attention over listed blocks: a list is cut into parts, one workgroup each, where there are few (token, K/V head)s and the list is longer than a merge (2.5 us and 0.1 more
@@ -64,6 +74,10 @@ constexpr int32_t sparse_state_words(int32_t D) { return D + 4; }
 inline size_t sparse_workspace_bytes(const ecoserve_layout& L, int32_t T, int32_t num_selected, int32_t num_cu) {
   const int32_t parts = sparse_parts(L.num_kv_heads, T, num_selected, num_cu, L.dtype);
   return parts == 1 ? 0 : (size_t)parts * T * L.num_q_heads * sparse_state_words(L.head_dim) * 4;
+}
+// The largest that takes: parts of all lists are a workgroup per CU at most.
+inline size_t sparse_workspace_most(const ecoserve_layout& L, int32_t num_cu) {
+  return (size_t)num_cu * (L.num_q_heads / L.num_kv_heads) * sparse_state_words(L.head_dim) * 4;
 }
 
 struct SparseArgs {

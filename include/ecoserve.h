@@ -413,8 +413,10 @@ int ecoserve_kv_append_rope(ecoserve_ctx* ctx, const ecoserve_rope* rope, const 
  * of ecoserve_summary_bytes(layout) bytes.  A query head is coded the same way, q8[d] = rint(q[d] / 2^eq) (half to even; a
  * head with a NaN, an infinity or an element beyond 127 * 2^100: zeros), and the score of block j for K/V head g of a token is
  *     max over the heads h of g of  2^(eq[h] + e) * sum_d max(q8[h][d] * top[d], q8[h][d] * low[d]),
- * +inf if e = 127.  The sums are integers below 2^22, so scores are exact in fp32 and which blocks are chosen does not
- * depend on the order of any sum.
+ * +inf if e = 127.  The sums are integers below 2^22, so scores are exact in fp32 wherever -149 <= eq[h] + e <= 106, and which
+ * blocks are chosen does not depend on the order of any sum.  Beyond that range a score is the fp32 number next to it: of
+ * 2^128 and more infinite, as a block's that is not finite, below 2^-126 a multiple of 2^-149; blocks whose scores become
+ * equal so go by their index.
  */
 size_t ecoserve_summary_bytes(const ecoserve_layout* layout); /* 0 if the layout is invalid */
 

@@ -2,7 +2,8 @@
 //
 // score(j) = max_h 2^(eq_h + e_j) sum_d max(q8 top_d, q8 low_d) is a product of whole numbers: max(q8 top, q8 low) =
 // max(q8, 0) top + min(q8, 0) low, so with [max(q8, 0) | min(q8, 0)] as a row of 2 Dp and a block's record [top | low] as a
-// column it is v_mfma_i32_16x16x64_i8, exact in 32 bits; scaled by a power of two it is exact in fp32 too.  Hence no
+// column it is v_mfma_i32_16x16x64_i8, exact in 32 bits; scaled by a power of two it is exact in fp32 too (a sum of exponents
+// outside -149 .. 106 takes it beyond fp32: it is infinite there, or rounded to subnormals).  Hence no
 // order of sums, number of tokens or split of the blocks changes which blocks are chosen.
 //
 // The rows of a product are (token, head of the group), a token's padded to a power of two with copies of its last head, so that the

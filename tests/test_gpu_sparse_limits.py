@@ -108,3 +108,39 @@ def test_codes_bound_keys_far_below_the_largest(dtype):
             want, e = so.summarise(b.keys[b.table[0, j], g].float().numpy())
             assert exps[b.table[0, j], g] == e and np.array_equal(codes[b.table[0, j], g], want), (j, g)
     b.ctx.close()
+
+
+# ---- scores beyond the numbers of fp32 ------------------------------------------------------------
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("keys,queries", [(1e20, 1e20), (1e30, 1e10), (1e-20, 1e-20), (1e-30, 1e-12), (1e25, 1e-25)])
+def test_scores_at_the_ends_of_the_range(dtype, keys, queries):
+    """Scores are fp32 numbers: beyond the largest they are infinite, below the smallest zero, and equal ones go by index; in between (the last pair) the order is exact."""
+    b = Batch(dtype, 32, 4, 2, [1500, 700], [1, 1], seed=3)
+    b.keys *= keys
+    b.q *= queries
+    b.upload()
+    summary, codes, exps = _all_summarised(b)
+    ragged = Batch(dtype, 32, 4, 2, [1000], [500], seed=4)
+    ragged.keys *= keys
+    ragged.q *= queries
+    ragged.upload()
+    for x, one in ((b, True), (ragged, False)):
+        summary, codes, exps = _all_summarised(x)
+        got = _select(x, summary, 9, 1, 2, ragged=not one)
+        q, ties = x.q.float().numpy(), 0
+        for t in range(0, x.T, 1 if one else 31):
+            n = x.pos[t] // 16 + 1
+            ids = x.table[x.seq[t], :n - 1]
+            for g in range(x.Hkv):
+                s = so.scores(q[t, g * x.G:(g + 1) * x.G], codes[ids, g, :, :x.D], exps[ids, g])
+                with np.errstate(over="ignore", under="ignore"):
+                    held = s.astype(np.float32)
+                ties += len(held) - len(np.unique(held))
+                assert got[t, g].tolist() == so.choose(held, n, 9, 1, 2), (t, g)
+                if keys == 1e25:
+                    assert got[t, g].tolist() == so.choose(s, n, 9, 1, 2)
+        assert ties > 0 or keys == 1e25
+    b.ctx.close()
+    ragged.ctx.close()

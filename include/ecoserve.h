@@ -463,8 +463,7 @@ int ecoserve_block_select(ecoserve_ctx* ctx, const void* q, int64_t q_row_stride
  * blocks in its list.  Entries outside 0 .. p / 16 (-1 among them) hold no keys, in any place of the list; the order of a list
  * matters to rounding alone; a block listed twice counts twice.  Lists from ecoserve_block_select or any other source.
  * A token without keys: out 0, lse -inf; one whose keys all score -inf: NaN (0 / 0), as Eq. 2 has it.  Weights keep the bits
- * of fp32 in F32 layouts and 16 in BF16 ones, 8 where many tokens of prompts share blocks (those of the values alone, as in
- * ecoserve_attn_prefill; lse from fp32 sums).
+ * of fp32 in F32 layouts and 16 in BF16 ones; lse is from fp32 sums.
  *
  *   blocks       : dev, int32[T][Hkv][num_selected], num_selected 1 .. 65536
  *   out, lse     : as in ecoserve_attn_prefill (lse may be NULL); rows of tokens behind cu_q[B] are left alone

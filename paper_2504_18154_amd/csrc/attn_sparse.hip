@@ -453,8 +453,8 @@ __global__ __launch_bounds__(kWaves * 64) void attn_sparse_kernel(const E* __res
 //   The union: a word per block of the sequence with a bit per token, from which the listed ones are collected in their order.
 //   Where that does not do, the wavefront takes its tokens one by one, block by block: lists with a block twice, and results that are not
 // finite (a NaN or an infinity among values meets the zero weights of the columns beside it).
-//   The weights are rounded to bf16 once, as the prefill kernel has them (two parts took 171 us where one took 142): a row is off by up to 2^-8 of its size then, as much
-// as the rounding of the result.
+//   The weights go in two bf16 parts here too, so that what a token gets does not depend on the tokens beside it or on the table's width (one part, 8 bits: 120 us,
+// so 145; but 1.4 times the error that the result's rounding leaves).
 //   Blocks go from memory into LDS without registers between, and the operands of a pair of blocks are asked for together, half of the values' before the weights are known
 // (in registers, operands as they are wanted: 145 us, so 131; values all at once: 140).
 // What bounds it (895 tokens, 64 heads on 8 of 128, lists of 64 that agree in half): latency.  A workgroup fills a CU, its wavefronts leave a barrier together, and want
@@ -573,14 +573,16 @@ __global__ __launch_bounds__(group_waves(KS) * 64, group_waves(KS) / 4) void att
     }
     f32x4 p[2];
     st.weights_of(s, p, scale_log2e, counts);
-    const bf16x8 w = __builtin_bit_cast(bf16x8, u32x4{pack_bf16x2(p[0][0], p[0][1]), pack_bf16x2(p[0][2], p[0][3]), pack_bf16x2(p[1][0], p[1][1]), pack_bf16x2(p[1][2], p[1][3])});
+    bf16x8 part[2];
+    in_parts(p, part);
     __builtin_amdgcn_s_setprio(1);  // (wavefronts that multiply go before those that count: 152 -> 142 us)
 #pragma unroll
     for (int dt = kEarly; dt < NV; ++dt) y[dt] = *reinterpret_cast<const u32x4*>(vat + dt * 512);
 #pragma unroll
     for (int dt = 0; dt < NV; ++dt) {
       if (kOne && quad >= 2) y[dt] = u32x4{0u, 0u, 0u, 0u};
-      st.o[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, y[dt]), w, st.o[dt], 0, 0, 0);
+      st.o[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, y[dt]), part[0], st.o[dt], 0, 0, 0);
+      st.o[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, y[dt]), part[1], st.o[dt], 0, 0, 0);
     }
     __builtin_amdgcn_s_setprio(0);
   };
@@ -702,9 +704,10 @@ __global__ __launch_bounds__(group_waves(KS) * 64, group_waves(KS) / 4) void att
   }
 }
 
-// Prompts of so many rows that the groups' lists in common save more than a group's walk, which takes 85 us of 64 blocks, alone or beside others, costs.  (us of a call, token
-// by token / groups: 64 on 8, 128, lists of 64: 256 tokens 64 / 99, 512 126 / 112, 2048 491 / 212; 2000, of 32, 295 / 151; 52 on 52: 32 96 / 95, 128 380 / 101; 32 on 8, 64:
-// 512 66 / 92, 2048 269 / 165; 8 on 1, 2048 69 / 99; 8 on 1, 256: 512 50 / 155, 2048 181 / 136.)
+// Prompts of so many rows that the groups' lists in common save more than a group's walk, which takes 115 us of 64 blocks, alone or beside others, costs.  (us of a call, token
+// by token / groups: 64 on 8, 128, lists of 64: 256 tokens 66 / 126, 512 128 / 141 (behind 2000 tokens 126 / 95), 700 175 / 148, 4 x 512 479 / 270, 8 x 48 97 / 103; 2000, of 32,
+// 300 / 182; 52 on 52: 32 95 / 118, 64 185 / 120, 128 380 / 127; 32 on 8, 64: 512 65 / 113, 1024 133 / 121, 4 x 512 266 / 207; 8 on 1, 4 x 512 70 / 124; 8 on 1, 256: 1024 97 / 183,
+// 4 x 512 183 / 164, 2000, of 32, 128 / 113.  The line is drawn in channels of K rows; 64 tokens of 52 on 52 and the last one are on its wrong side.)
 struct SparseGroups {
   int log_rows, units;  // units 0: token by token
   explicit operator bool() const { return units > 0; }

@@ -144,3 +144,23 @@ def test_scores_at_the_ends_of_the_range(dtype, keys, queries):
         assert ties > 0 or keys == 1e25
     b.ctx.close()
     ragged.ctx.close()
+
+
+# ---- bits of the weights --------------------------------------------------------------------------
+
+
+@pytest.mark.parametrize("D,Hq,Hkv,new", [(128, 16, 2, [100, 0, 2600]), (72, 14, 2, [3700]), (256, 8, 1, [2100])], ids=["d128", "d72", "d256"])
+def test_prompts_keep_the_bits_of_a_step(D, Hq, Hkv, new):
+    """16 bits of a weight, whether a token is alone or one of many that share blocks; an infinite value meets no weight of zero."""
+    b = Batch("bf16", D, Hq, Hkv, [17 + 100 * i for i in range(len(new))], new, seed=D)
+    assert b.T * Hkv * D >= 2048 * 256
+    lists = _random_lists(b, 7, np.random.default_rng(D + 1))
+    out, lse = _attend(b, lists)
+    _compare(b, lists, out, lse, name="16 bits", tokens=_of_prompts(b))
+    b.vals[b.table[len(new) - 1, 2], 0, 5, 3] = float("inf")
+    b.upload()
+    out, _ = _attend(b, lists)
+    o = out.float().cpu().numpy()[:, :b.G]
+    hit = (lists[:, 0] == 2).any(1) & (b.seq == len(new) - 1) & (b.pos >= 2 * 16 + 5)
+    assert hit.any() and np.isposinf(o[hit][:, :, 3]).all() and np.isfinite(np.delete(o[hit], 3, 2)).all() and np.isfinite(o[~hit]).all()
+    b.ctx.close()

@@ -58,8 +58,8 @@ struct SelectArgs {
 };
 
 // Attention over listed blocks: a list is cut into parts, one workgroup each, where there are few (token, K/V head)s and the list is longer than a merge (2.5 us and 0.1 more
-// per part) is worth: up to a workgroup per CU in all, for lists of up to 128 half of that; a part has eight blocks at least, two per wavefront, and as many as there are
-// parts.  (us, 40 heads on 8 of 128, bf16.  One token: 32 blocks whole 8.7, in 4 parts 9.6; 64 whole 11.9, in 4, 8, 16 parts 10.7, 9.9, 11.9; 1024 in 16, 32, 64 parts 20.6, 21.0, 25.7.
+// per part) is worth: up to a workgroup per CU in all, for lists of up to 128 half of that; K entries are ceil(K / 8) parts at most, of about two blocks per wavefront (the shortest that
+// are cut: 33 in 4 of 7 and one of 5; fp32: 17 in 2 of 6 and one of 5), no more than the root of K, so that a part has as many entries as there are parts, and 64.  (us, 40 heads on 8 of 128, bf16.  One token: 32 blocks whole 8.7, in 4 parts 9.6; 64 whole 11.9, in 4, 8, 16 parts 10.7, 9.9, 11.9; 1024 in 16, 32, 64 parts 20.6, 21.0, 25.7.
 // 16 tokens: 64 whole 16.0, in 2, 4 parts 18.8, 20.2; 1024 whole 217, in 2, 4 parts 191, 192.  fp32, a block at a time, 8 heads on 2 of 64: 16 blocks whole 7.2, in 2 parts 8.2; 32 whole
 // 10.0, in 4 8.2.)
 inline int32_t sparse_parts(int32_t Hkv, int32_t T, int32_t num_selected, int32_t num_cu, int32_t dtype) {

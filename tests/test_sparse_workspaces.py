@@ -64,16 +64,52 @@ int main() {
 """
 
 
-def test_a_workspace_for_the_largest_call_serves_the_smaller_ones(tmp_path):
+def _run(tmp_path, program):
     if not os.path.exists(build.LIB):
         pytest.skip("the library is not built")
     src, exe = tmp_path / "sizes.cpp", tmp_path / "sizes"
-    src.write_text(ALLOCATOR + PROGRAM)
+    src.write_text(ALLOCATOR + program)
     rocm = os.path.dirname(os.path.dirname(os.path.realpath(build._hipcc())))
     subprocess.run(["g++", "-std=c++17", "-O1", "-I", build.INCLUDE, "-I", os.path.join(rocm, "include"), str(src), "-o", str(exe), "-rdynamic", build.LIB,
                     f"-Wl,-rpath,{os.path.dirname(build.LIB)}:{os.path.join(rocm, 'lib')}", f"-Wl,-rpath-link,{os.path.join(rocm, 'lib')}"], check=True)
     r = subprocess.run([str(exe)], capture_output=True, text=True, timeout=60)
-    assert r.returncode == 0 and r.stdout == "0\n", r.stdout[:2000] + r.stderr[-500:]
+    assert r.stderr == ""
+    return r.stdout
+
+
+def test_a_workspace_for_the_largest_call_serves_the_smaller_ones(tmp_path):
+    assert _run(tmp_path, PROGRAM) == "0\n"
+
+
+PARTS = r"""
+int main() {
+  room = (size_t)1 << 30;
+  int bad = 0;
+  for (int dtype : {ECOSERVE_BF16, ECOSERVE_F32}) {
+    ecoserve_layout lay = {};
+    lay.num_q_heads = 6, lay.num_kv_heads = 2, lay.head_dim = 64, lay.block_size = 16, lay.num_blocks = 4, lay.dtype = dtype;
+    ecoserve_ctx* c = nullptr;
+    if (ecoserve_create(&c, 0, &lay, 8, 1000)) return std::printf("not created\n"), 1;
+    const int bf[][3] = {{1, 1, 1}, {1, 32, 1}, {1, 33, 5}, {1, 41, 6}, {1, 49, 7}, {1, 64, 8}, {1, 65, 8}, {1, 128, 11}, {1, 4095, 63}, {1, 4096, 64}, {1, 65536, 64}, {8, 64, 8},
+                         {9, 64, 7}, {32, 64, 2}, {33, 64, 1}, {64, 129, 2}, {65, 129, 1}};
+    const int f32[][3] = {{1, 1, 1}, {1, 16, 1}, {1, 17, 3}, {1, 25, 4}, {1, 32, 4}, {1, 33, 5}, {1, 64, 8}, {64, 17, 1}, {32, 17, 2}};
+    auto check = [&](const int (&x)[3]) {
+      const size_t want = x[2] == 1 ? 0 : (size_t)x[2] * x[0] * 6 * 68 * 4, got = ecoserve_sparse_workspace_bytes(c, x[0], x[1]);
+      if (got != want) ++bad, std::printf("%d tokens, %d entries: %zu, not %zu (%d parts)\n", x[0], x[1], got, want, x[2]);
+    };
+    if (dtype == ECOSERVE_BF16) for (const auto& x : bf) check(x);
+    else for (const auto& x : f32) check(x);
+    ecoserve_destroy(c);
+  }
+  std::printf("%d\n", bad);
+  return bad != 0;
+}
+"""
+
+
+def test_parts_of_lists(tmp_path):
+    """How many a list is cut into, 256 CUs (the workspace holds a state of each)."""
+    assert _run(tmp_path, PARTS) == "0\n"
 
 
 def test_what_is_held_at_a_time_stays_in_the_last_level_cache():

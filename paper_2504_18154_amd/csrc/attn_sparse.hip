@@ -452,7 +452,8 @@ __global__ __launch_bounds__(kWaves * 64) void attn_sparse_kernel(const E* __res
 // has no weight there.
 //   The union: a word per block of the sequence with a bit per token, from which the listed ones are collected in their order.
 //   Where that does not do, the wavefront takes its tokens one by one, block by block: lists with a block twice, and results that are not
-// finite (a NaN or an infinity among values meets the zero weights of the columns beside it).
+// finite (a NaN or an infinity among values meets the zero weights of the columns beside it).  That loop goes through scratch memory for what the registers do not hold (up to 37 of them;
+// the main loop does not).
 //   The weights go in two bf16 parts here too, so that what a token gets does not depend on the tokens beside it or on the table's width (one part, 8 bits: 120 us,
 // so 145; but 1.4 times the error that the result's rounding leaves).
 //   Blocks go from memory into LDS without registers between, and the operands of a pair of blocks are asked for together, half of the values' before the weights are known

@@ -364,7 +364,8 @@ int ecoserve_attn_decode_noalloc(int device, const ecoserve_layout* layout, cons
  * embeddings; models encode a token's position by turning pairs of their elements).  Pair i of a head vector, i <
  * rotary_dim / 2, is turned by the angle  theta = position * inv_freq[i]:
  *     (a, b)  ->  (a cos theta - b sin theta,  a sin theta + b cos theta),
- * in fp32, rounded once to E; theta is formed and reduced in 64 bits, so positions may be as large as int32 goes.
+ * in fp32, rounded once to E; theta is formed and reduced in 64 bits, so positions may be as large as int32 goes (beyond
+ * 2^27 radians its rounding there, 3.4e-16 of theta at most, is more than fp32's).
  * Elements from rotary_dim on are not turned.  The rotated K rows and the V rows join the cache as ecoserve_kv_append
  * stores them, and the rotated Q rows go to q_out, in one launch.
  */

@@ -457,9 +457,9 @@ __global__ __launch_bounds__(kWaves * 64) void attn_sparse_kernel(const E* __res
 //   The weights go in two bf16 parts here too, so that what a token gets does not depend on the tokens beside it or on the table's width (one part, 8 bits: 120 us,
 // so 145; but 1.4 times the error that the result's rounding leaves).
 //   Blocks go from memory into LDS without registers between, and the operands of a pair of blocks are asked for together, half of the values' before the weights are known
-// (in registers, operands as they are wanted: 145 us, so 131; values all at once: 140).
+// (with weights in one part: in registers, operands as they are wanted: 145 us, so 131; values all at once: 140).
 // What bounds it (895 tokens, 64 heads on 8 of 128, lists of 64 that agree in half): latency.  A workgroup fills a CU, its wavefronts leave a barrier together, and want
-// LDS, the matrix unit and the vector unit at the same times, which are busy for 32, 19 and 30% of it; at a barrier they wait for the one with the most blocks of a stage (the
+// LDS, the matrix unit and the vector unit at the same times, which are busy for 27, 25 and 39% of it; at a barrier they wait for the one with the most blocks of a stage (the
 // sum of those is 1.7 times the mean's), and the workgroup with the largest union comes last.  A column's work is in vain for 40% of a wavefront's blocks, those that the token
 // beside it lists alone.  Token by token the same call reads each block of K and V 20 times from the caches, 3.7 GB, 235 us.
 constexpr int kWords = 5120;  // blocks of a sequence that the union has room for

@@ -1,10 +1,11 @@
 // KV-cache append with the position rotation on the way: K and Q rows are turned between the projection and the cache
 // (or q_out), V rows are stored as they are.
 //
-// Pair i of a head vector at position p is turned by theta = p f_i.  theta / 2 pi is a double product; its distance from
+// Pair i of a head vector at position p is turned by theta = p f_i.  theta / 2 pi is a double product, off by three
+// roundings of 64 bits at most (3.4e-16 of itself: less than fp32's own rounding up to 2^27 radians, 7e-7 at 2^31); its distance from
 // the nearest quarter turn, at most an eighth of a turn, goes to fp32, where the Taylor series of sine and cosine (to a^9 and a^10; the next
-// terms are below 2e-9 and 2e-10 there) are as good as the type: no table in memory, whatever the positions, and the
-// angle of a far position is as exact as that of a near one.  The products are fp32, rounded once on the way out.
+// terms are below 2e-9 and 2e-10 there) are as good as the type: no table in memory, whatever the positions.
+// The products are fp32, rounded once on the way out.
 //
 // Memory bounds the large calls (every Q, K and V element is read once and written once), launch latency and three
 // round trips the small ones.  An angle serves all heads of a token, so a thread keeps one place of the head vector (16
@@ -63,7 +64,7 @@ __device__ __forceinline__ E rounded(float x) {
 // WV elements at a time: a 16-byte unit, or half of one where the halves of the pairs do not begin with a unit.
 // kEach (halves, of heads that are not turned as a whole and whose units a wavefront has together): a thread turns one unit and reads the other half of its pairs besides;
 // otherwise it turns both.  (Of accesses to the second half few lanes would have any: 32 elements turned, 86 k tokens, 8 heads on 1 of 256 264 us, so 227; 16 k tokens, 64 on 8 of 128
-// 173, so 163.  Heads that are turned as a whole: 3 prompts, 2.3 k tokens, 64 on 8 of 128 40.6 us, so 48.6.)  In place the other half's owner has it from memory before either stores: loads
+// 173, so 163.  Heads that are turned as a whole: 3 prompts, 3.4 k tokens, 64 on 8 of 128 40.6 us, so 48.6.)  In place the other half's owner has it from memory before either stores: loads
 // and stores are instructions of the one wavefront, in this order.
 template <typename E, int WV, bool kAdjacent, bool kEach>
 __global__ __launch_bounds__(kRopeThreads) void kv_append_rope_kernel(
@@ -272,7 +273,7 @@ void launch_typed(const RopeAppend& a, const Turns& turns, int num_cu, hipStream
   const int v_heads = D * (int)sizeof(E) <= 512 ? 4 : 2, v_slices = (a.Hkv + v_heads - 1) / v_heads;
   const int64_t units = (int64_t)a.T / 16 + 2 * (int64_t)a.B;
   const int total = a.Hkv + (q ? a.Hq : 0);
-  // heads per workgroup: as many workgroups as the device takes at once, then more heads to an angle (3 prompts, 2.3k tokens, 64 heads on 8 of 128: 4 workgroups
+  // heads per workgroup: eight workgroups per CU, then more heads to an angle (3 prompts, 3.4 k tokens, 64 heads on 8 of 128, where registers leave four at once: 4 workgroups
   // per CU 43.7 us, 8 40.5, 16 49.0)
   const int64_t want = (8 * (int64_t)num_cu + units - 1) / units;
   const int slices = (int)(want < total ? want : total), per_slice = (total + slices - 1) / slices;

@@ -6,8 +6,8 @@
 // + 8, + 12 of one 16-byte unit (64 bytes in a row per four lanes), takes the extremes over them in registers and over its
 // three neighbours within the vector unit.  The extremes are taken of whole numbers in the keys' order (x ^ 0x7fff.. where x is negative), two bf16 keys an
 // instruction; NaNs lie beyond the infinities there, so that the extremes tell whether the block holds either.
-// Memory bounds a prompt's blocks (each is read once, for 1/16 of it written; 65536 tokens, 8 heads of 128, 134 MB: 32 us from memory, 26.0 from the
-// last-level cache, 28.0 with floats), latency a step's.
+// Memory bounds a prompt's blocks (each is read once, for 1/16 of it written; 65536 tokens, 8 heads of 128, 134 MB: 33 us from memory; 26 from the
+// last-level cache, where floats took 28), latency a step's.
 //
 // Blocks are numbered sequence after sequence, those of sequence b from cu_q[b] / 16 + b: S new tokens fill at most
 // S / 16 + 1 blocks.

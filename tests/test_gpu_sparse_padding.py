@@ -7,7 +7,7 @@ import torch
 from oracle import sparse_oracle as so
 from paper_2504_18154_amd import workloads as wl
 from tests.parity_util import dev_i32, say
-from tests.test_gpu_sparse import Batch, _summary_host
+from tests.test_gpu_sparse import Batch, _all_summarised, _attend, _compare, _expected_lists, _select, _summary_host
 
 pytestmark = pytest.mark.gpu
 
@@ -74,3 +74,61 @@ def test_summaries(batch, dtype):
             want, e = so.summarise(b.keys[blk, g].float().numpy())
             assert exps[blk, g] == e and np.array_equal(codes[blk, g, :, :b.D], want), (blk, g)
     b.ctx.close()
+
+
+@pytest.mark.parametrize("dtype,D,Hq,Hkv,before,new", [("bf16", 128, 8, 2, [-40, 100], [2100, 900]), ("bf16", 64, 6, 3, [-3, -100], [60, 90]), ("f32", 64, 4, 2, [-17, 20], [300, 9])])
+def test_selection_and_attention(dtype, D, Hq, Hkv, before, new):
+    """Prompts that begin with places of the padding, token by token and in groups."""
+    b = Batch(dtype, D, Hq, Hkv, before, new, seed=5)
+    summary, codes, exps = _all_summarised(b)
+    want = _expected_lists(b, codes, exps, 6, 1, 2)
+    assert np.array_equal(_select(b, summary, 6, 1, 2), want)
+    out, lse = _attend(b, want)
+    nothing = torch.as_tensor(b.pos < 0)
+    assert nothing.any() and (out.cpu()[nothing] == 0).all() and torch.isneginf(lse.cpu()[nothing]).all()
+    some = [t for t in range(b.T) if b.pos[t] >= 0 and (b.pos[t] < 70 or t % 41 == 0)]
+    _compare(b, want, out, lse, name="attention", tokens=some)
+    b.ctx.close()
+
+
+def test_a_prompt_recorded_into_a_graph():
+    """The four calls of a prompt's chunk whose batch has places of the padding, replayed with new inputs between eager work of the same shape: every replay the same bits as the eager calls."""
+    from paper_2504_18154_amd import binding
+    Hq, Hkv, D, K = 8, 2, 128, 5
+    before, new = np.array([200, -30, 700]), np.array([1400, 60, 700])
+    T, B = int(new.sum()), 3
+    table, nb = _tables(before, new)
+    ctx = binding.Context(Hq, Hkv, D, nb, "bf16", B, table.shape[1])
+    g = torch.Generator(device="cuda").manual_seed(5)
+    rand = lambda *s: torch.randn(*s, generator=g, device="cuda").to(torch.bfloat16)
+    pools = [rand(nb * Hkv * 16 * D) for _ in range(2)]
+    rope = binding.Rope(10000.0 ** (-torch.arange(64, dtype=torch.float64, device="cuda") / 64))
+    bt, cu, at = dev_i32(table), dev_i32(wl.cu_from_lengths(new)), dev_i32(before)
+    first = ctx.new_summary()
+    ctx.kv_summary(pools[0], first, dev_i32(wl.cu_from_lengths(np.maximum(before, 0))), dev_i32(np.zeros(B)), bt, int(np.maximum(before, 0).sum()))
+    q, k, v = rand(T, Hq, D), rand(T, Hkv, D), rand(T, Hkv, D)
+
+    def chunk(kc, vc, summ, lists, q_out, out, lse):
+        ctx.kv_append_rope(kc, vc, k, v, cu, at, bt, rope, q=q, q_out=q_out)
+        ctx.kv_summary(kc, summ, cu, at, bt, T)
+        ctx.block_select(q_out, summ, at, bt, lists, 1600, keep_last=2, cu_q=cu)
+        ctx.attn_sparse(q_out, kc, vc, at, bt, lists, out, lse=lse, cu_q=cu)
+
+    def buffers():
+        return (pools[0].clone(), pools[1].clone(), first.clone(), torch.zeros(T, Hkv, K, dtype=torch.int32, device="cuda"), torch.zeros_like(q), torch.zeros_like(q),
+                torch.zeros(T, Hq, device="cuda"))
+
+    mine, eager, graph = buffers(), buffers(), torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=torch.cuda.Stream()):
+        chunk(*mine)
+    for i in range(4):
+        for t in (q, k, v):
+            t.copy_(rand(*t.shape))
+        chunk(*eager)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(mine, eager):
+            assert torch.equal(a.view(torch.uint8), b.view(torch.uint8)), i
+    ctx.close()

@@ -481,6 +481,103 @@ int ecoserve_attn_sparse(ecoserve_ctx* ctx, const void* q, int64_t q_row_stride,
                          void* workspace, size_t workspace_bytes, void* stream);
 
 /*
+ * Caches of 8 bits, norms on the way into a cache, and attention with formed scores.  Table 2 has decode attention bound by the bytes of the cached
+ * keys and values: codes of 8 bits halve them, and let a pool of the same size hold twice the tokens.  The four calls below take the cache they work
+ * on as a struct; with ECOSERVE_CACHE_LAYOUT it is the bf16 cache of all other calls.
+ *
+ *   ECOSERVE_CACHE_INT8, ECOSERVE_CACHE_E4M3: one byte per element, int8 or OCP e4m3 (4 exponent, 3 fraction bits, largest 448, no infinities)
+ *     k      : uint8[num_blocks][Hkv][D / 16][bs][16]   (units of 16 bytes, as in the layout's cache)
+ *     v      : uint8[num_blocks][Hkv][D][bs]
+ *     scales : uint8[num_blocks][Hkv][2][bs]            of the keys, then of the values, a byte per token
+ *   A code c of a (token, head) with scale byte b stands for c * 2^(b - 127); b = 255: the row held a NaN or an infinity, and stands for NaN throughout.
+ *   Coding a row of largest magnitude A: e = the smallest integer >= -126 with A <= M * 2^e, M = 127 or 448; b = e + 127; the codes are the
+ *   row / 2^e, rounded once to nearest even.  (Relative to A an int8 row is within 2^-7, and to an element an e4m3 one within 2^-4: int8 is
+ *   the finer one unless a head has a few channels far above the others.)
+ *
+ * All four take BF16 layouts whose head_dim is a multiple of 16; others: ECOSERVE_EUNSUPPORTED.  k and v are 16-byte aligned, scales too.  Slots that no
+ * token was stored in may hold anything.  ecoserve_cache_bytes() / 2 is the size of an 8-bit k or v.
+ */
+enum { ECOSERVE_CACHE_LAYOUT = 0, ECOSERVE_CACHE_INT8 = 1, ECOSERVE_CACHE_E4M3 = 2 };
+typedef struct {
+  int32_t format; /* ECOSERVE_CACHE_* */
+  void* k;        /* dev */
+  void* v;        /* dev */
+  uint8_t* scales; /* dev; NULL with ECOSERVE_CACHE_LAYOUT */
+} ecoserve_cache;
+size_t ecoserve_cache_scale_bytes(const ecoserve_layout* layout); /* bytes of `scales`; 0 if the layout is invalid */
+
+/*
+ * Norm of a head vector x:  x[d] / sqrt(mean(x^2) + eps) * w[d], in fp32; squares are summed in fp32 (elements beyond 2^60 make
+ * them infinite, and the row 0).
+ */
+typedef struct {
+  float eps;              /* >= 0, finite */
+  int32_t per_head;       /* 0: weights are float[D], for all heads; 1: float[Hq][D] and float[Hkv][D] */
+  const float* q_weight;  /* dev, 16-byte aligned, or NULL: 1 */
+  const float* k_weight;
+} ecoserve_norm;
+
+/*
+ * KV-cache append with each head of K and Q normed, then rotated, and K and V coded, on the way: in fp32 from the given rows to one rounding, to a
+ * code or to bf16 (the cache with ECOSERVE_CACHE_LAYOUT, and q_out).
+ *
+ *   cache : host struct;  norm : host, or NULL: no norm;  rope : host, or NULL: no rotation (inv_freq and positions are not read)
+ *   everything else, tokens at negative positions among it, as in ecoserve_kv_append_rope.
+ * K and V alone, neither normed nor rotated, is allowed: the append of a quantised cache.
+ */
+int ecoserve_kv_append_norm(ecoserve_ctx* ctx, const ecoserve_cache* cache, const ecoserve_norm* norm, const ecoserve_rope* rope, const double* inv_freq,
+                            const int32_t* positions, const void* q, int64_t q_row_stride, void* q_out, int64_t q_out_row_stride, const void* k_new,
+                            const void* v_new, int64_t new_row_stride, const int32_t* cu_q, const int32_t* ctx_before, const int32_t* block_table,
+                            int32_t bt_stride, int32_t B, int32_t T, int32_t max_new_len, void* stream);
+
+/*
+ * Reads cached tokens back as rows of bf16 (a sequence that moves to another instance; a look at what a cache holds).  Token i of sequence b is
+ * position first[b] + i; it goes to packed row cu[b] + i.  Exact: a code times its scale is a bf16 number, of magnitudes from 2^-126 on (below: rounded).
+ *   cu          : dev, int32[B+1], prefix sums of the counts, cu[B] = T
+ *   first       : dev, int32[B]; tokens at negative positions are not read, their rows left alone
+ *   k_rows, v_rows : dev, E[T][Hkv][D], rows row_stride elements apart (rules of the strided calls), 16-byte aligned; one of them may be NULL
+ */
+int ecoserve_kv_read(ecoserve_ctx* ctx, const ecoserve_cache* cache, void* k_rows, void* v_rows, int64_t row_stride, const int32_t* cu,
+                     const int32_t* first, const int32_t* block_table, int32_t bt_stride, int32_t B, int32_t T, void* stream);
+
+/*
+ * What the scores of Eq. 2 become.  The score of the token at position p and query head h for key j:
+ *     s = softmax_scale * q.k[j];   softcap > 0:  s = softcap * tanh(s / softcap);   slopes:  s = s + slopes[h] * (j - p)
+ * for the keys  key_begin[t] <= j < key_end[t]  of its sequence (t: the packed token), which leaves room for windows (begin = p + 1 - window),
+ * documents packed into one sequence (begin = the document's first position) and prefixes that are seen from everywhere (end = max(p + 1, prefix)).
+ * Begins below 0 are 0; ends above the tokens that the sequence holds, ctx_before[b] + its new tokens, are that many: a token may see
+ * keys behind itself.  Cache blocks without a key of any token's range are not read, nor are their entries of the block table.
+ * A token without keys: out 0, lse -inf.  One whose keys all score -inf: NaN.  Values that are not finite reach the tokens that see them, and no
+ * others.
+ */
+typedef struct {
+  float softcap;             /* 0: none; otherwise positive and finite */
+  const float* slopes;       /* dev, float[Hq], or NULL */
+  const int32_t* key_begin;  /* dev, int32[T], or NULL: 0 */
+  const int32_t* key_end;    /* dev, int32[T], or NULL: p + 1 */
+} ecoserve_scores;
+
+/*
+ * Attention over a cache of any of the formats, as ecoserve_attn_prefill_strided and ecoserve_attn_decode_strided compute it over the layout's:
+ * prompts (chunks of them, behind what is cached), and one token per sequence at position ctx_len[b] - 1 (T = B; ctx_len[b] <= 0: without keys).
+ * The tokens themselves must already be in the cache.  Tokens at negative positions have no keys.  out and lse are packed; lse may be NULL.
+ *
+ *   scores    : host, or NULL: Eq. 2 as it is
+ *   workspace : dev, 16-byte aligned, of at least the bytes that the function of the same call says (0: NULL is fine); nothing in it is kept from call to call
+ * Weights are rounded to bf16 before the product with the values; maxima, sums and lse are fp32.
+ * Calls that share a context are ordered (rules at the top): work that is split is counted in the context's merge counters.  Calls that may
+ * run at the same time, recorded into graphs or not, need a context and a workspace each.  The options do not concern these calls.
+ */
+size_t ecoserve_prefill_scored_workspace_bytes(const ecoserve_ctx* ctx, int32_t B, int32_t T);
+int ecoserve_attn_prefill_scored(ecoserve_ctx* ctx, const ecoserve_cache* cache, const ecoserve_scores* scores, const void* q, int64_t q_row_stride,
+                                 const int32_t* cu_q, const int32_t* ctx_before, const int32_t* block_table, int32_t bt_stride, void* out, float* lse,
+                                 int32_t B, int32_t T, void* workspace, size_t workspace_bytes, void* stream);
+size_t ecoserve_decode_scored_workspace_bytes(const ecoserve_ctx* ctx);
+int ecoserve_attn_decode_scored(ecoserve_ctx* ctx, const ecoserve_cache* cache, const ecoserve_scores* scores, const void* q, int64_t q_row_stride,
+                                const int32_t* block_table, int32_t bt_stride, const int32_t* ctx_len, void* out, float* lse, int32_t B,
+                                int32_t max_ctx_len, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
  * Machine ceilings for the roofline reasoning of Section 2.1 (Table 2 prices
  * decode attention in bytes read, prefill attention in matrix FLOPs): what
  * `device` sustains on each resource, to be reported beside the published

@@ -33,8 +33,11 @@ EXPORTS = [
     "ecoserve_debug_prefill_queue_shares",
     "ecoserve_kv_append_rope", "ecoserve_summary_bytes", "ecoserve_kv_summary", "ecoserve_select_workspace_bytes",
     "ecoserve_block_select", "ecoserve_sparse_workspace_bytes", "ecoserve_sparse_workspace_most", "ecoserve_attn_sparse",
+    "ecoserve_cache_scale_bytes", "ecoserve_kv_append_norm", "ecoserve_kv_read", "ecoserve_prefill_scored_workspace_bytes",
+    "ecoserve_attn_prefill_scored", "ecoserve_decode_scored_workspace_bytes", "ecoserve_attn_decode_scored",
 ]
 ROPE_HALVES, ROPE_ADJACENT = 0, 1
+CACHE_LAYOUT, CACHE_INT8, CACHE_E4M3 = 0, 1, 2
 
 
 class Layout(ctypes.Structure):
@@ -45,6 +48,18 @@ class Layout(ctypes.Structure):
 
 class RopeStruct(ctypes.Structure):
     _fields_ = [("rotary_dim", ctypes.c_int32), ("pairing", ctypes.c_int32), ("num_axes", ctypes.c_int32), ("axis", ctypes.c_uint8 * 128)]
+
+
+class CacheStruct(ctypes.Structure):
+    _fields_ = [("format", ctypes.c_int32), ("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("scales", ctypes.c_void_p)]
+
+
+class NormStruct(ctypes.Structure):
+    _fields_ = [("eps", ctypes.c_float), ("per_head", ctypes.c_int32), ("q_weight", ctypes.c_void_p), ("k_weight", ctypes.c_void_p)]
+
+
+class ScoresStruct(ctypes.Structure):
+    _fields_ = [("softcap", ctypes.c_float), ("slopes", ctypes.c_void_p), ("key_begin", ctypes.c_void_p), ("key_end", ctypes.c_void_p)]
 
 
 class EcoserveError(RuntimeError):
@@ -93,6 +108,17 @@ def _load(path: str = LIB_PATH) -> ctypes.CDLL:
     for f in (lib.ecoserve_summary_bytes, lib.ecoserve_select_workspace_bytes, lib.ecoserve_sparse_workspace_bytes, lib.ecoserve_sparse_workspace_most):
         f.restype = sz
     lib.ecoserve_attn_sparse.argtypes = [vp, vp, i64, vp, vp, i32p, i32p, i32p, i32, i32p, i32, vp, vp, i32, i32, vp, sz, vp]
+    cache, scores = ctypes.POINTER(CacheStruct), ctypes.POINTER(ScoresStruct)
+    lib.ecoserve_cache_scale_bytes.argtypes = [ctypes.POINTER(Layout)]
+    lib.ecoserve_kv_append_norm.argtypes = [vp, cache, ctypes.POINTER(NormStruct), ctypes.POINTER(RopeStruct), vp, i32p, vp, i64, vp, i64, vp, vp, i64, i32p, i32p, i32p, i32,
+                                            i32, i32, i32, vp]
+    lib.ecoserve_kv_read.argtypes = [vp, cache, vp, vp, i64, i32p, i32p, i32p, i32, i32, i32, vp]
+    lib.ecoserve_prefill_scored_workspace_bytes.argtypes = [vp, i32, i32]
+    lib.ecoserve_attn_prefill_scored.argtypes = [vp, cache, scores, vp, i64, i32p, i32p, i32p, i32, vp, vp, i32, i32, vp, sz, vp]
+    lib.ecoserve_decode_scored_workspace_bytes.argtypes = [vp]
+    lib.ecoserve_attn_decode_scored.argtypes = [vp, cache, scores, vp, i64, i32p, i32, i32p, vp, vp, i32, i32, vp, sz, vp]
+    for f in (lib.ecoserve_cache_scale_bytes, lib.ecoserve_prefill_scored_workspace_bytes, lib.ecoserve_decode_scored_workspace_bytes):
+        f.restype = sz
     lib.ecoserve_debug_validate.argtypes = [vp, i32p, i32p, i32p, i32, i32]
     lib.ecoserve_debug_prefill_queue_shares.argtypes = [vp, ctypes.POINTER(ctypes.c_float)]
     lib.ecoserve_profile_read.argtypes = [vp, i32, ctypes.POINTER(ctypes.c_double), ctypes.POINTER(ctypes.c_int64)]
@@ -120,6 +146,11 @@ _fast.bind_sparse(*(ctypes.cast(f, ctypes.c_void_p).value for f in (_lib.ecoserv
                                                                     _lib.ecoserve_sparse_workspace_bytes, _lib.ecoserve_attn_sparse)))
 
 
+_fast.bind_scored(*(ctypes.cast(f, ctypes.c_void_p).value for f in (_lib.ecoserve_kv_append_norm, _lib.ecoserve_kv_read, _lib.ecoserve_prefill_scored_workspace_bytes,
+                                                                    _lib.ecoserve_attn_prefill_scored, _lib.ecoserve_decode_scored_workspace_bytes,
+                                                                    _lib.ecoserve_attn_decode_scored)))
+
+
 def strerror(status: int) -> str:
     return _lib.ecoserve_strerror(int(status)).decode()
 
@@ -141,6 +172,11 @@ def cache_bytes(layout: Layout) -> int:
 def summary_bytes(layout: Layout) -> int:
     """Bytes of one layer's block summaries."""
     return int(_lib.ecoserve_summary_bytes(ctypes.byref(layout)))
+
+
+def cache_scale_bytes(layout: Layout) -> int:
+    """Bytes of the scales of one layer's 8-bit cache."""
+    return int(_lib.ecoserve_cache_scale_bytes(ctypes.byref(layout)))
 
 
 def select_workspace_bytes(layout: Layout, T: int, max_ctx_len: int) -> int:
@@ -237,6 +273,48 @@ class Rope:
         self.inv_freq = inv_freq
         self.struct = RopeStruct(2 * pairs, {"halves": ROPE_HALVES, "adjacent": ROPE_ADJACENT}[pairing], max(axis, default=0) + 1,
                                  (ctypes.c_uint8 * 128)(*axis))
+        self._address = ctypes.addressof(self.struct)
+
+
+class PagedCache:
+    """One layer's cache: pools k and v and, of 8-bit formats, scales.  Formats: "bf16" (the pools of Context.new_cache), "int8" and "e4m3" (uint8 pools of as
+    many elements, uint8 scales [num_blocks, Hkv, 2, 16]).  It holds on to the tensors; a program makes it once and keeps it."""
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, scales: torch.Tensor | None = None, format: str = "bf16"):
+        code = {"bf16": CACHE_LAYOUT, "int8": CACHE_INT8, "e4m3": CACHE_E4M3}[format]
+        want = torch.bfloat16 if code == CACHE_LAYOUT else torch.uint8
+        if (scales is None) != (code == CACHE_LAYOUT):
+            raise ValueError("8-bit formats have scales, bf16 has none")
+        for t, dtype in ((k, want), (v, want), (scales, torch.uint8)):
+            if t is not None and not (torch.is_tensor(t) and t.dtype == dtype and t.is_contiguous()):
+                raise ValueError(f"{format}: k and v must be contiguous {want} tensors, scales uint8")
+        self.k, self.v, self.scales, self.format = k, v, scales, format
+        self.struct = CacheStruct(code, k.data_ptr(), v.data_ptr(), _ptr(scales))
+        self._address = ctypes.addressof(self.struct)
+
+
+class HeadNorm:
+    """Norm of each head of Q and K: x / sqrt(mean(x^2) + eps) * weight; weights float32 [D] for all heads or [Hq, D] and [Hkv, D], or None: 1."""
+
+    def __init__(self, eps: float, q_weight: torch.Tensor | None = None, k_weight: torch.Tensor | None = None):
+        given = [w for w in (q_weight, k_weight) if w is not None]
+        if any(not torch.is_tensor(w) or w.dtype != torch.float32 or not w.is_contiguous() or w.dim() not in (1, 2) for w in given) or len({w.dim() for w in given}) > 1:
+            raise ValueError("weights must be contiguous float32 tensors, [D] or [heads, D], both alike")
+        self.q_weight, self.k_weight = q_weight, k_weight
+        self.struct = NormStruct(float(eps), int(bool(given) and given[0].dim() == 2), _ptr(q_weight), _ptr(k_weight))
+        self._address = ctypes.addressof(self.struct)
+
+
+class Scores:
+    """What the scores of attention become: softcap (0: none), slopes float32 [Hq] (score + slope (key - position)), the keys [key_begin, key_end) that each token
+    sees, int32 [tokens] (None: from 0, to its own position).  It holds on to the tensors."""
+
+    def __init__(self, softcap: float = 0.0, slopes: torch.Tensor | None = None, key_begin: torch.Tensor | None = None, key_end: torch.Tensor | None = None):
+        for t, dtype in ((slopes, torch.float32), (key_begin, torch.int32), (key_end, torch.int32)):
+            if t is not None and not (torch.is_tensor(t) and t.dtype == dtype and t.is_contiguous()):
+                raise ValueError("slopes must be a contiguous float32 tensor, key_begin and key_end int32 ones")
+        self.slopes, self.key_begin, self.key_end = slopes, key_begin, key_end
+        self.struct = ScoresStruct(float(softcap), _ptr(slopes), _ptr(key_begin), _ptr(key_end))
         self._address = ctypes.addressof(self.struct)
 
 
@@ -517,6 +595,123 @@ class Context:
                                          entries, self._same(out, "out", self.torch_dtype, T * self._q_row),
                                          self._same(lse, "lse", torch.float32, T * L.num_q_heads) if lse is not None else None, B, T, at, room, self._stream_here()),
                "ecoserve_attn_sparse")
+
+    # ---- norms and codes on the way into the cache, reading back, attention with formed scores ----
+    def new_paged_cache(self, format: str) -> PagedCache:
+        """One layer's cache of a format, every code 0 (bf16: NaN, as new_cache has it)."""
+        if format == "bf16":
+            return PagedCache(*self.new_cache())
+        L = self.layout
+        n = L.num_blocks * L.num_kv_heads * L.block_size * L.head_dim
+        k = torch.zeros(n, dtype=torch.uint8, device=self.device)
+        scales = torch.full((L.num_blocks, L.num_kv_heads, 2, L.block_size), 127, dtype=torch.uint8, device=self.device)
+        return PagedCache(k, k.clone(), scales, format=format)
+
+    def _cache(self, cache: PagedCache):
+        """The struct, its tensors looked at."""
+        L, s = self.layout, cache.struct
+        n, dtype = L.num_blocks * L.num_kv_heads * L.block_size * L.head_dim, self.torch_dtype if s.format == CACHE_LAYOUT else torch.uint8
+        if self._same(cache.k, "k", dtype, n) != s.k or self._same(cache.v, "v", dtype, n) != s.v or (
+                cache.scales is not None and self._same(cache.scales, "scales", torch.uint8, 32 * L.num_blocks * L.num_kv_heads) != s.scales):
+            raise ValueError("the cache's tensors have moved since it was made")
+        return ctypes.byref(s)
+
+    def _form(self, scores: Scores | None, T: int):
+        if scores is None:
+            return None
+        s = scores.struct
+        for t, what, dtype, least, at in ((scores.slopes, "slopes", torch.float32, self.layout.num_q_heads, s.slopes), (scores.key_begin, "key_begin", torch.int32, T, s.key_begin),
+                                          (scores.key_end, "key_end", torch.int32, T, s.key_end)):
+            if t is not None and self._same(t, what, dtype, least) != (at or 0):
+                raise ValueError(f"{what} has moved since the scores' form was made")
+        return ctypes.byref(s)
+
+    def kv_append_norm(self, cache: PagedCache, k_new, v_new, cu_q, ctx_before, block_table, norm: HeadNorm | None = None, rope: Rope | None = None, positions=None, q=None,
+                       q_out=None, max_new_len=None):
+        """kv_append_strided into a cache of any format, with each head of K normed and rotated on the way, and of Q (if given) into q_out."""
+        status = _fast.kv_append_norm(self._address, self._layout_address, self._device_index, cache._address, cache.k, cache.v, cache.scales,
+                                      norm._address if norm else 0, norm.q_weight if norm else None, norm.k_weight if norm else None, rope._address if rope else 0,
+                                      rope.inv_freq if rope else None, positions, k_new, v_new, cu_q, ctx_before, block_table, q, q_out, max_new_len)
+        if status >= 0:
+            return _check(status, "ecoserve_kv_append_norm")
+        T, L = k_new.shape[0], self.layout
+        kn, new_stride = self._rows(k_new, "k_new", T, L.num_kv_heads)
+        vn, v_stride = self._rows(v_new, "v_new", T, L.num_kv_heads)
+        if new_stride != v_stride:
+            raise ValueError("k_new and v_new must have the same row stride")
+        if norm is not None:
+            for w, what, heads, at in ((norm.q_weight, "q_weight", L.num_q_heads, norm.struct.q_weight), (norm.k_weight, "k_weight", L.num_kv_heads, norm.struct.k_weight)):
+                if w is not None and (tuple(w.shape) != ((heads, L.head_dim) if norm.struct.per_head else (L.head_dim,)) or self._same(w, what, torch.float32) != at):
+                    raise ValueError(f"{what} must be [D] or [heads, D], where it was when the norm was made")
+        freq = None
+        if rope is not None:
+            freq = self._same(rope.inv_freq, "inv_freq", torch.float64, rope.struct.rotary_dim // 2)
+            if positions is not None and not (torch.is_tensor(positions) and tuple(positions.shape) == (rope.struct.num_axes, T)):
+                raise ValueError("positions must be [axes, tokens]")
+        if (q is None) != (q_out is None):
+            raise ValueError("q and q_out go together")
+        q_at, q_stride = self._rows(q, "q", T, L.num_q_heads) if q is not None else (None, 0)
+        out_at, out_stride = self._rows(q_out, "q_out", T, L.num_q_heads) if q is not None else (None, 0)
+        cu, before, table, width, B = self._batch(cu_q, ctx_before, block_table)
+        _check(_lib.ecoserve_kv_append_norm(self._h, self._cache(cache), ctypes.byref(norm.struct) if norm else None, ctypes.byref(rope.struct) if rope else None, freq,
+                                            self._same(positions, "positions", torch.int32) if rope is not None and positions is not None else None, q_at, q_stride, out_at,
+                                            out_stride, kn, vn, new_stride, cu, before, table, width, B, T, T if max_new_len is None else int(max_new_len),
+                                            self._stream_here()), "ecoserve_kv_append_norm")
+
+    def kv_read(self, cache: PagedCache, k_rows, v_rows, cu, first, block_table):
+        """Cached tokens first[b] + i of each sequence as rows cu[b] + i; k_rows or v_rows may be None."""
+        status = _fast.kv_read(self._address, self._layout_address, self._device_index, cache._address, cache.k, cache.v, cache.scales, k_rows, v_rows, cu, first, block_table)
+        if status >= 0:
+            return _check(status, "ecoserve_kv_read")
+        given = [t for t in (k_rows, v_rows) if t is not None]
+        if not given:
+            raise ValueError("one of k_rows and v_rows must be given")
+        T = given[0].shape[0]
+        rows = [self._rows(t, "rows", T, self.layout.num_kv_heads) for t in given]
+        if rows[0][1] != rows[-1][1]:
+            raise ValueError("k_rows and v_rows must have the same row stride")
+        cu_at, first_at, table, width, B = self._batch(cu, first, block_table)
+        _check(_lib.ecoserve_kv_read(self._h, self._cache(cache), rows[0][0] if k_rows is not None else None, rows[-1][0] if v_rows is not None else None, rows[0][1], cu_at,
+                                     first_at, table, width, B, T, self._stream_here()), "ecoserve_kv_read")
+
+    def prefill_scored_workspace_bytes(self, B: int, T: int) -> int:
+        return int(_lib.ecoserve_prefill_scored_workspace_bytes(self._h, int(B), int(T)))
+
+    def decode_scored_workspace_bytes(self) -> int:
+        return int(_lib.ecoserve_decode_scored_workspace_bytes(self._h))
+
+    def attn_prefill_scored(self, q, cache: PagedCache, cu_q, ctx_before, block_table, out, lse=None, scores: Scores | None = None, workspace=None):
+        """Attention of prompts over a cache of any format, with formed scores."""
+        f = scores
+        status = _fast.attn_prefill_scored(self._address, self._layout_address, self._device_index, cache._address, cache.k, cache.v, cache.scales, f._address if f else 0,
+                                           f.slopes if f else None, f.key_begin if f else None, f.key_end if f else None, q, cu_q, ctx_before, block_table, out, lse, workspace)
+        if status >= 0:
+            return _check(status, "ecoserve_attn_prefill_scored")
+        T, L = q.shape[0], self.layout
+        q_at, q_stride = self._rows(q, "q", T, L.num_q_heads)
+        cu, before, table, width, B = self._batch(cu_q, ctx_before, block_table)
+        at, room, _held = self._workspace(workspace, self.prefill_scored_workspace_bytes(B, T))
+        _check(_lib.ecoserve_attn_prefill_scored(self._h, self._cache(cache), self._form(scores, T), q_at, q_stride, cu, before, table, width,
+                                                 self._same(out, "out", self.torch_dtype, T * self._q_row),
+                                                 self._same(lse, "lse", torch.float32, T * L.num_q_heads) if lse is not None else None, B, T, at, room, self._stream_here()),
+               "ecoserve_attn_prefill_scored")
+
+    def attn_decode_scored(self, q, cache: PagedCache, block_table, ctx_len, out, max_ctx_len, lse=None, scores: Scores | None = None, workspace=None):
+        """Attention of one token per sequence over a cache of any format, with formed scores."""
+        f = scores
+        status = _fast.attn_decode_scored(self._address, self._layout_address, self._device_index, cache._address, cache.k, cache.v, cache.scales, f._address if f else 0,
+                                          f.slopes if f else None, f.key_begin if f else None, f.key_end if f else None, q, block_table, ctx_len, out, lse, max_ctx_len,
+                                          workspace)
+        if status >= 0:
+            return _check(status, "ecoserve_attn_decode_scored")
+        L = self.layout
+        _cu, length, table, width, B = self._batch(None, ctx_len, block_table)
+        q_at, q_stride = self._rows(q, "q", B, L.num_q_heads)
+        at, room, _held = self._workspace(workspace, self.decode_scored_workspace_bytes())
+        _check(_lib.ecoserve_attn_decode_scored(self._h, self._cache(cache), self._form(scores, B), q_at, q_stride, table, width, length,
+                                                self._same(out, "out", self.torch_dtype, B * self._q_row),
+                                                self._same(lse, "lse", torch.float32, B * L.num_q_heads) if lse is not None else None, B, int(max_ctx_len), at, room,
+                                                self._stream_here()), "ecoserve_attn_decode_scored")
 
     # ---- debugging / profiling -----------------------------------------------------------
     def debug_validate(self, cu_q, ctx_total, block_table):

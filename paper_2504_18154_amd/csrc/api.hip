@@ -12,6 +12,8 @@
 #include "decode_slices.h"
 #include "prefill_shares.h"
 #include "prefill_short.h"
+#include "quant.h"
+#include "scored.h"
 #include "sparse.h"
 #include "summary.h"
 
@@ -401,18 +403,23 @@ int ecoserve_kv_append_strided(ecoserve_ctx* c, void* k_cache, void* v_cache, co
   return e == hipSuccess ? ECOSERVE_OK : ECOSERVE_EHIP;
 }
 
+static bool rope_ok(const ecoserve_ctx* c, const ecoserve_rope* rope, const int32_t* positions, int32_t T) {
+  const int32_t unit = c->lay.dtype == ECOSERVE_BF16 ? 8 : 4;
+  if (rope->rotary_dim <= 0 || rope->rotary_dim > c->lay.head_dim || rope->rotary_dim % unit != 0) return false;
+  if (rope->pairing != ECOSERVE_ROPE_HALVES && rope->pairing != ECOSERVE_ROPE_ADJACENT) return false;
+  if (rope->num_axes < 1 || rope->num_axes > ECOSERVE_ROPE_MAX_AXES || (rope->num_axes > 1 && !positions && T > 0)) return false;
+  for (int i = 0; i < rope->rotary_dim / 2; ++i)
+    if (rope->axis[i] >= rope->num_axes) return false;
+  return true;
+}
+
 int ecoserve_kv_append_rope(ecoserve_ctx* c, const ecoserve_rope* rope, const double* inv_freq, const int32_t* positions, const void* q, int64_t q_row_stride,
                             void* q_out, int64_t q_out_row_stride, void* k_cache, void* v_cache, const void* k_new, const void* v_new, int64_t new_row_stride,
                             const int32_t* cu_q, const int32_t* ctx_before, const int32_t* block_table, int32_t bt_stride, int32_t B, int32_t T,
                             int32_t max_new_len, void* stream) {
   if (!c || !rope || B < 0 || T < 0 || max_new_len < 0) return ECOSERVE_EINVAL;
   const ecoserve_layout& L = c->lay;
-  const int32_t unit = L.dtype == ECOSERVE_BF16 ? 8 : 4;
-  if (rope->rotary_dim <= 0 || rope->rotary_dim > L.head_dim || rope->rotary_dim % unit != 0) return ECOSERVE_EINVAL;
-  if (rope->pairing != ECOSERVE_ROPE_HALVES && rope->pairing != ECOSERVE_ROPE_ADJACENT) return ECOSERVE_EINVAL;
-  if (rope->num_axes < 1 || rope->num_axes > ECOSERVE_ROPE_MAX_AXES || (rope->num_axes > 1 && !positions && T > 0)) return ECOSERVE_EINVAL;
-  for (int i = 0; i < rope->rotary_dim / 2; ++i)
-    if (rope->axis[i] >= rope->num_axes) return ECOSERVE_EINVAL;
+  if (!rope_ok(c, rope, positions, T)) return ECOSERVE_EINVAL;
   if (!stride_ok(c, new_row_stride, L.num_kv_heads)) return ECOSERVE_EINVAL;
   if ((q == nullptr) != (q_out == nullptr)) return ECOSERVE_EINVAL;
   if (q && (!stride_ok(c, q_row_stride, L.num_q_heads) || !stride_ok(c, q_out_row_stride, L.num_q_heads))) return ECOSERVE_EINVAL;
@@ -528,6 +535,125 @@ int ecoserve_attn_sparse(ecoserve_ctx* c, const void* q, int64_t q_row_stride, c
   const SparseArgs a = {q, (int32_t)q_row_stride, k_cache, v_cache, cu_q, ctx_before, block_table, bt_stride, blocks, num_selected, out, lse, B, T,
                         L.num_q_heads, L.num_kv_heads, L.head_dim, c->num_cu, L.dtype, c->scale * kLog2e, (float*)workspace, c->ws_count};
   return launch_attn_sparse(a, (hipStream_t)stream) == hipSuccess ? ECOSERVE_OK : ECOSERVE_EHIP;
+}
+
+size_t ecoserve_cache_scale_bytes(const ecoserve_layout* L) {
+  int st;
+  return layout_ok(L, &st) ? (size_t)L->num_blocks * L->num_kv_heads * kScaleBytes : 0;
+}
+
+// What the calls on an ecoserve_cache ask of it.  (Its addresses are looked at where there is something to do.)
+static int cache_status(const ecoserve_ctx* c, const ecoserve_cache* cache) {
+  if (!cache || !quant_format_ok(cache->format)) return ECOSERVE_EINVAL;
+  return c->lay.dtype == ECOSERVE_BF16 && c->lay.head_dim % 16 == 0 ? ECOSERVE_OK : ECOSERVE_EUNSUPPORTED;
+}
+static bool cache_there(const ecoserve_cache* cache) {
+  return cache->k && cache->v && aligned16(cache->k) && aligned16(cache->v) && (cache->format == kNative || (cache->scales && aligned16(cache->scales)));
+}
+int ecoserve_kv_append_norm(ecoserve_ctx* c, const ecoserve_cache* cache, const ecoserve_norm* norm, const ecoserve_rope* rope, const double* inv_freq,
+                            const int32_t* positions, const void* q, int64_t q_row_stride, void* q_out, int64_t q_out_row_stride, const void* k_new, const void* v_new,
+                            int64_t new_row_stride, const int32_t* cu_q, const int32_t* ctx_before, const int32_t* block_table, int32_t bt_stride, int32_t B, int32_t T,
+                            int32_t max_new_len, void* stream) {
+  if (!c || B < 0 || T < 0 || max_new_len < 0) return ECOSERVE_EINVAL;
+  if (const int st = cache_status(c, cache); st != ECOSERVE_OK) return st;
+  const ecoserve_layout& L = c->lay;
+  if (norm && (!(norm->eps >= 0.f) || isinf(norm->eps) || (norm->per_head != 0 && norm->per_head != 1) || !aligned16(norm->q_weight) || !aligned16(norm->k_weight)))
+    return ECOSERVE_EINVAL;
+  if (rope && !rope_ok(c, rope, positions, T)) return ECOSERVE_EINVAL;
+  if (!stride_ok(c, new_row_stride, L.num_kv_heads)) return ECOSERVE_EINVAL;
+  if ((q == nullptr) != (q_out == nullptr)) return ECOSERVE_EINVAL;
+  if (q && (!stride_ok(c, q_row_stride, L.num_q_heads) || !stride_ok(c, q_out_row_stride, L.num_q_heads))) return ECOSERVE_EINVAL;
+  if (B == 0 || T == 0) return ECOSERVE_OK;
+  if (!cache_there(cache) || !k_new || !v_new || !cu_q || !ctx_before || !block_table || (rope && !inv_freq)) return ECOSERVE_EINVAL;
+  if (B > c->max_batch || bt_stride <= 0 || max_new_len > T || max_new_len == 0) return ECOSERVE_EINVAL;
+  if (!aligned16(k_new) || !aligned16(v_new) || !aligned16(q) || !aligned16(q_out)) return ECOSERVE_EINVAL;
+  if (rope && ((reinterpret_cast<uintptr_t>(inv_freq) & 7u) || (reinterpret_cast<uintptr_t>(positions) & 3u))) return ECOSERVE_EINVAL;
+  DeviceGuard guard(c->device);
+  if (!guard.ok) return ECOSERVE_EHIP;
+  hipStream_t s = (hipStream_t)stream;
+  const NormAppend a = {q, (int32_t)q_row_stride, q_out, (int32_t)q_out_row_stride, cache->k, cache->v, cache->scales, k_new, v_new, (int32_t)new_row_stride, cu_q,
+                        ctx_before, block_table, bt_stride, B, T, max_new_len, L.num_q_heads, L.num_kv_heads, L.head_dim, cache->format, c->num_cu, norm != nullptr,
+                        norm ? norm->eps : 0.f, norm ? norm->q_weight : nullptr, norm ? norm->k_weight : nullptr, norm && norm->per_head ? L.head_dim : 0};
+  ProfileScope prof(c, ECOSERVE_KERNEL_APPEND, s);
+  return launch_kv_append_norm(a, rope, inv_freq, positions, s) == hipSuccess ? ECOSERVE_OK : ECOSERVE_EHIP;
+}
+
+int ecoserve_kv_read(ecoserve_ctx* c, const ecoserve_cache* cache, void* k_rows, void* v_rows, int64_t row_stride, const int32_t* cu, const int32_t* first,
+                     const int32_t* block_table, int32_t bt_stride, int32_t B, int32_t T, void* stream) {
+  if (!c || B < 0 || T < 0) return ECOSERVE_EINVAL;
+  if (const int st = cache_status(c, cache); st != ECOSERVE_OK) return st;
+  const ecoserve_layout& L = c->lay;
+  if (!stride_ok(c, row_stride, L.num_kv_heads)) return ECOSERVE_EINVAL;
+  if (B == 0 || T == 0) return ECOSERVE_OK;
+  if (!cache_there(cache) || (!k_rows && !v_rows) || !cu || !first || !block_table) return ECOSERVE_EINVAL;
+  if (B > c->max_batch || bt_stride <= 0 || !aligned16(k_rows) || !aligned16(v_rows)) return ECOSERVE_EINVAL;
+  DeviceGuard guard(c->device);
+  if (!guard.ok) return ECOSERVE_EHIP;
+  const ReadBack a = {cache->k, cache->v, cache->scales, k_rows, v_rows, (int32_t)row_stride, cu, first, block_table, bt_stride, B, T, L.num_kv_heads, L.head_dim,
+                      cache->format, c->num_cu};
+  return launch_kv_read(a, (hipStream_t)stream) == hipSuccess ? ECOSERVE_OK : ECOSERVE_EHIP;
+}
+
+static bool scores_ok(const ecoserve_scores* scores) {
+  if (!scores) return true;
+  auto aligned4 = [](const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; };
+  return scores->softcap >= 0.f && !isinf(scores->softcap) && aligned4(scores->slopes) && aligned4(scores->key_begin) && aligned4(scores->key_end);
+}
+// (prompts of more rows than 32 bits count are refused)
+static bool scored_rows_ok(const ecoserve_ctx* c, int32_t B, int32_t T) {
+  const int64_t G = c->lay.num_q_heads / c->lay.num_kv_heads;
+  return T * G <= 0x7fffffffLL - kTileRows && prefill_scored_tiles(B, T, (int32_t)G) * c->lay.num_kv_heads <= 0x7fffffffLL;
+}
+static ScoredArgs scored_args(const ecoserve_ctx* c, const ecoserve_cache* cache, const ecoserve_scores* scores, const void* q, int64_t q_row_stride,
+                              const int32_t* cu_q, const int32_t* ctx, const int32_t* block_table, int32_t bt_stride, void* out, float* lse, int32_t B, int32_t T,
+                              void* workspace) {
+  const ecoserve_layout& L = c->lay;
+  const ecoserve_scores s = scores ? *scores : ecoserve_scores{0.f, nullptr, nullptr, nullptr};
+  return {q, (int32_t)q_row_stride, cache->k, cache->v, cache->scales, cu_q, ctx, block_table, bt_stride, out, lse, s.slopes, s.key_begin, s.key_end, B, T, L.num_q_heads,
+          L.num_kv_heads, L.head_dim, cache->format, c->num_cu, c->scale * kLog2e, s.softcap, (float*)workspace, c->ws_count};
+}
+
+size_t ecoserve_prefill_scored_workspace_bytes(const ecoserve_ctx* c, int32_t B, int32_t T) {
+  if (!c || B <= 0 || T <= 0 || !scored_rows_ok(c, B, T)) return 0;
+  return prefill_scored_workspace(c->lay, B, T, c->num_cu);
+}
+
+int ecoserve_attn_prefill_scored(ecoserve_ctx* c, const ecoserve_cache* cache, const ecoserve_scores* scores, const void* q, int64_t q_row_stride, const int32_t* cu_q,
+                                 const int32_t* ctx_before, const int32_t* block_table, int32_t bt_stride, void* out, float* lse, int32_t B, int32_t T, void* workspace,
+                                 size_t workspace_bytes, void* stream) {
+  if (!c || B < 0 || T < 0) return ECOSERVE_EINVAL;
+  if (const int st = cache_status(c, cache); st != ECOSERVE_OK) return st;
+  if (!scores_ok(scores) || !stride_ok(c, q_row_stride, c->lay.num_q_heads)) return ECOSERVE_EINVAL;
+  if (B == 0 || T == 0) return ECOSERVE_OK;
+  if (!cache_there(cache) || !q || !cu_q || !ctx_before || !block_table || !out) return ECOSERVE_EINVAL;
+  if (B > c->max_batch || bt_stride <= 0 || !scored_rows_ok(c, B, T)) return ECOSERVE_EINVAL;
+  if (!aligned16(q) || !aligned16(out) || !aligned16(workspace) || (reinterpret_cast<uintptr_t>(lse) & 3u)) return ECOSERVE_EINVAL;
+  const size_t needed = prefill_scored_workspace(c->lay, B, T, c->num_cu);
+  if (needed > 0 && (!workspace || workspace_bytes < needed)) return ECOSERVE_EINVAL;
+  DeviceGuard guard(c->device);
+  if (!guard.ok) return ECOSERVE_EHIP;
+  const ScoredArgs a = scored_args(c, cache, scores, q, q_row_stride, cu_q, ctx_before, block_table, bt_stride, out, lse, B, T, workspace);
+  return launch_prefill_scored(a, prefill_scored_splits(c->lay, B, T, c->num_cu), (hipStream_t)stream) == hipSuccess ? ECOSERVE_OK : ECOSERVE_EHIP;
+}
+
+size_t ecoserve_decode_scored_workspace_bytes(const ecoserve_ctx* c) { return c ? decode_scored_workspace(c->lay, c->num_cu) : 0; }
+
+int ecoserve_attn_decode_scored(ecoserve_ctx* c, const ecoserve_cache* cache, const ecoserve_scores* scores, const void* q, int64_t q_row_stride,
+                                const int32_t* block_table, int32_t bt_stride, const int32_t* ctx_len, void* out, float* lse, int32_t B, int32_t max_ctx_len,
+                                void* workspace, size_t workspace_bytes, void* stream) {
+  if (!c || B < 0 || max_ctx_len < 0) return ECOSERVE_EINVAL;
+  if (const int st = cache_status(c, cache); st != ECOSERVE_OK) return st;
+  if (!scores_ok(scores) || !stride_ok(c, q_row_stride, c->lay.num_q_heads)) return ECOSERVE_EINVAL;
+  if (B == 0) return ECOSERVE_OK;
+  if (!cache_there(cache) || !q || !block_table || !ctx_len || !out) return ECOSERVE_EINVAL;
+  if (B > c->max_batch || bt_stride <= 0 || max_ctx_len < 1) return ECOSERVE_EINVAL;
+  if ((int64_t)max_ctx_len > (int64_t)c->max_blocks_per_seq * kBlockSize || (int64_t)max_ctx_len > (int64_t)bt_stride * kBlockSize) return ECOSERVE_EINVAL;
+  if (!aligned16(q) || !aligned16(out) || !aligned16(workspace) || (reinterpret_cast<uintptr_t>(lse) & 3u)) return ECOSERVE_EINVAL;
+  if (!workspace || workspace_bytes < decode_scored_workspace(c->lay, c->num_cu)) return ECOSERVE_EINVAL;
+  DeviceGuard guard(c->device);
+  if (!guard.ok) return ECOSERVE_EHIP;
+  const ScoredArgs a = scored_args(c, cache, scores, q, q_row_stride, nullptr, ctx_len, block_table, bt_stride, out, lse, B, B, workspace);
+  return launch_decode_scored(a, (hipStream_t)stream) == hipSuccess ? ECOSERVE_OK : ECOSERVE_EHIP;
 }
 
 static AttnArgs make_args(const ecoserve_ctx* c, const void* q, int64_t q_row_stride, const void* k_cache, const void* v_cache,

@@ -1,0 +1,528 @@
+// Attention of prompts (chunks of them, behind what is cached) over the caches of ecoserve_cache, with formed scores, on gfx950 matrix cores.
+//
+// Eq. 2 of Section 2.1 for the prefill phase, bound by the matrix units and the vector work of the softmax beside them.  A tile is 128 rows ((position,
+// query head of the group) pairs of one sequence and K/V head), 32 to each of four wavefronts, which share the tile's keys, 64 at a time:
+//   scores  S^T[key][row] = K . Q^T     v_mfma_f32_32x32x16_bf16
+//   values  O^T[d][row] += V^T . P^T    v_mfma_f32_32x32x16_bf16
+// A step's codes are loaded two steps ahead, and a step ahead turned into bf16, scales and all (exact: a code has 7 bits at most and the scales are powers
+// of two), on the way into LDS, once for the four wavefronts; the loop over the keys is the same for all formats.
+//   K in LDS: [16-byte unit of 8 channels][64 keys], V: [8 keys][channel][16 bytes]; both are read as A operands, 16 bytes a lane.
+// Rows of S^T stand for keys with bits 2 and 3 swapped, so that the 16 scores that a lane holds of 32 keys are two runs of 8 neighbouring keys: the B
+// operand of the second product, and P stays in registers.
+//
+// A row's keys are a range.  The tile walks the steps from the first range's begin to the last range's end; a wavefront passes over steps that none of its
+// rows sees, and masks only where a step is not inside all its rows' ranges.
+// Tiles are dealt heaviest first.  Where they are few, their steps are cut among several workgroups; each leaves its state in the workspace, and the last
+// one to arrive adds them up in order.
+//
+// Values that are not finite must not reach rows that do not see them (0 times NaN).  Codes: such a row is coded as zeros, its scale byte says 255, and rows that
+// see it are given NaN at the end.  bf16: results that are not finite are taken again, one row at a time, over the keys that it sees.
+//
+// Weights are rounded to bf16 for the second product (2^-9 of each, unbiased); maxima, sums and the log-sum-exp are fp32, from the weights before that.
+//
+// Lane layouts relied upon (lane = 32 half + col), 32x32x16:  A[row = col][k = 8 half .. + 7],  B[k = 8 half .. + 7][col],
+// C[row = 8 (i / 4) + 4 half + i % 4][col].
+#include <type_traits>
+
+#include "quant.h"
+#include "scored.h"
+
+namespace eco {
+
+namespace {
+
+constexpr int kThreads = 256, kKeys = 64;
+constexpr float kLowest = -3.0e38f;  // maximum before the first key: below every finite score, and no infinity to be subtracted from one
+constexpr float kTau = 8.f;          // the maximum in the exponent is raised when a score passes it by 2^8: weights reach that, and lose nothing by it
+constexpr int kRsrc = 0x00020000;
+constexpr int kAgent = 16;           // past the caches that XCDs do not share
+
+__device__ __forceinline__ float across_halves_max(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float across_halves_sum(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+  return r;
+}
+
+template <int F, int NC>
+struct Tile {
+  static constexpr bool kNarrow = F != kNative;
+  static constexpr int kD = 32 * NC;                                // channels that the instance holds
+  static constexpr int kUnits = kD / 8;                             // of 8 channels
+  static constexpr int kKBytes = kUnits * kKeys * 16;
+  static constexpr int kOctet = kD * 16 + 64;                       // 8 keys of V, and what moves the next ones to other banks
+  static constexpr int kVBytes = 8 * kOctet;
+  static constexpr int kBuffers = NC == 8 ? 1 : 2;                  // (heads of 256: a second one would leave a workgroup per CU)
+  static constexpr int kChunks = kNarrow ? NC / 2 : NC;             // 16-byte loads of K, and of V, per thread and step
+};
+
+// What a row of scores needs of the score's form.
+struct Form {
+  float scale_log2e, cap_in, cap_log2e;  // cap_in: 2 log2(e) scale / cap, or 0
+  const float* slopes;
+};
+
+// One row again, from its keys alone, by a wavefront: lane l has channels l, l + 64, ...  For results that are not finite, where a value that the row does not
+// see may be the cause.
+template <int NC, bool kForm>
+__device__ __attribute__((noinline)) void row_again(const uint16_t* __restrict__ q_row, const char* __restrict__ k_head, const char* __restrict__ v_head, long long blk_stride,
+                                                    const int32_t* __restrict__ table, int lo, int hi, int pos, float slope, Form form, int D, uint16_t* __restrict__ to) {
+  constexpr int kPer = NC == 8 ? 4 : NC == 4 ? 2 : 1;
+  const int lane = threadIdx.x & 63;
+  float qv[kPer], o[kPer], m = kLowest, l = 0.f;
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) {
+    const int d = lane + 64 * i;
+    qv[i] = d < D ? bf16_bits_to_float(q_row[d]) : 0.f;
+    o[i] = 0.f;
+  }
+  for (int j = lo; j < hi; ++j) {
+    const long long at = (long long)table[j >> 4] * blk_stride;
+    const uint16_t *const kp = reinterpret_cast<const uint16_t*>(k_head + at), *const vp = reinterpret_cast<const uint16_t*>(v_head + at);
+    float s = 0.f, v[kPer];
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      const int d = min(lane + 64 * i, D - 1);
+      s += lane + 64 * i < D ? qv[i] * bf16_bits_to_float(kp[(d >> 3) * 128 + (j & 15) * 8 + (d & 7)]) : 0.f;
+      v[i] = bf16_bits_to_float(vp[d * 16 + (j & 15)]);
+    }
+    s = wave_sum(s);
+    if (kForm && form.cap_in > 0.f) s = form.cap_log2e - 2.f * form.cap_log2e * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(s * form.cap_in));
+    else s *= form.scale_log2e;
+    if (kForm) s = __builtin_fmaf(slope, (float)(j - pos), s);
+    const float m_new = fmaxf(m, s), alpha = __builtin_amdgcn_exp2f(m - m_new), p = __builtin_amdgcn_exp2f(s - m_new);
+    l = l * alpha + p;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) o[i] = o[i] * alpha + p * v[i];
+    m = m_new;
+  }
+#pragma unroll
+  for (int i = 0; i < kPer; ++i)
+    if (const int d = lane + 64 * i; d < D) to[d] = float_to_bf16_bits(o[i] / l);
+}
+
+// Workgroup (x, y): K/V head x % Hkv of tile x / Hkv, counted from the last one; y: which part of its steps.
+template <int F, int NC, bool kForm>
+__global__ __launch_bounds__(kThreads, NC == 8 ? 1 : 2) void prefill_scored_kernel(
+    const uint16_t* __restrict__ q, int q_row_stride, const char* __restrict__ k_cache, const char* __restrict__ v_cache, const uint8_t* __restrict__ scales,
+    const int32_t* __restrict__ cu_q, const int32_t* __restrict__ ctx_before, const int32_t* __restrict__ block_table, int bt_stride,
+    const int32_t* __restrict__ key_begin, const int32_t* __restrict__ key_end, uint16_t* __restrict__ out, float* __restrict__ lse, float* states,
+    uint32_t* counters, int B, int Hq, int Hkv, int G, Divisor div_g, Divisor div_hkv, int D, int units, Form form) {
+  typedef Cached<F> C;
+  typedef Tile<F, NC> W;
+  __shared__ __attribute__((aligned(16))) char s_k[W::kBuffers][W::kKBytes], s_v[W::kBuffers][W::kVBytes];
+  __shared__ int s_lo[4], s_hi[4], s_order, s_bad[2];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 31, half = lane >> 5;
+
+  // ---- the tile, its rows and their keys
+  const int xu = fast_div((int)blockIdx.x, div_hkv), g = (int)blockIdx.x - xu * Hkv, unit = units - 1 - xu;
+  auto first_unit = [&](int cu, int b) { return (long long)cu * G / kTileRows + b; };
+  const SeqOf seq = find_sequence(cu_q, ctx_before, B, unit, first_unit);
+  const int rows = seq.S * G, row0 = (int)(unit - first_unit(seq.tok0, seq.b)) * kTileRows;
+  if (seq.S <= 0 || row0 >= rows) return;
+  const int rr = row0 + wave * 32 + col, place = fast_div(min(rr, rows - 1), div_g), head = g * G + min(rr, rows - 1) - place * G, tok = seq.tok0 + place;
+  const bool valid = rr < rows;
+  const int pos = seq.cb + place, total = seq.cb + seq.S;
+  int lo = key_begin ? max(key_begin[tok], 0) : 0, hi = key_end ? min(key_end[tok], total) : pos + 1;
+  if (!valid || pos < 0 || hi <= lo) lo = 0x7fffffff, hi = 0;
+  const bool none = hi == 0;
+  // over the wavefront's rows: first begin, last begin, first end, last end
+  const int w_lo = -lanes_max(0x7fffffff - lo) + 0x7fffffff, w_hi = lanes_max(hi), w_lo_last = lanes_max(none ? 0 : lo), w_hi_first = 0x7fffffff - lanes_max(none ? 0 : 0x7fffffff - hi);
+  if (lane == 0) s_lo[wave] = w_lo, s_hi[wave] = w_hi;
+  if (tid < 2) s_bad[tid] = 0;
+  __syncthreads();
+  const int t_lo = min(min(s_lo[0], s_lo[1]), min(s_lo[2], s_lo[3])), t_hi = max(max(s_hi[0], s_hi[1]), max(s_hi[2], s_hi[3]));
+  uint16_t* const out_row = out + ((size_t)tok * Hq + head) * D;
+  float* const lse_row = lse ? lse + (size_t)tok * Hq + head : nullptr;
+  const int j_first = t_hi > 0 ? t_lo / kKeys : 0, j_end = t_hi > 0 ? (t_hi - 1) / kKeys + 1 : 0;
+  const int splits = gridDim.y;
+  const int j0 = __builtin_amdgcn_readfirstlane(j_first + (int)((long long)(j_end - j_first) * blockIdx.y / splits));
+  const int j1 = __builtin_amdgcn_readfirstlane(j_first + (int)((long long)(j_end - j_first) * (blockIdx.y + 1) / splits));
+  const int wj0 = __builtin_amdgcn_readfirstlane(w_hi > 0 ? w_lo / kKeys : 0), wj1 = __builtin_amdgcn_readfirstlane(w_hi > 0 ? (w_hi - 1) / kKeys + 1 : 0);
+
+  bf16x8 qf[2 * NC];
+  const uint16_t* const q_row = q + (size_t)tok * q_row_stride + (size_t)head * D;
+#pragma unroll
+  for (int t = 0; t < 2 * NC; ++t) {
+    const bf16x8 zero = {0, 0, 0, 0, 0, 0, 0, 0};
+    qf[t] = valid && 16 * t + 8 * half < D ? *reinterpret_cast<const bf16x8*>(q_row + 16 * t + 8 * half) : zero;
+  }
+  const float slope = kForm && form.slopes ? form.slopes[head] * kLog2e : 0.f;
+
+  // ---- staging: a step's 16-byte pieces to registers, and from there to LDS as bf16
+  const int blk_bytes = kBlockSize * D * C::kBytes;
+  const long long blk_stride = (long long)Hkv * blk_bytes;
+  const char *const k_head = k_cache + (size_t)g * blk_bytes, *const v_head = v_cache + (size_t)g * blk_bytes;
+  const int32_t* const table = block_table + (size_t)seq.b * bt_stride;
+  const int blk_lo = t_lo >> 4, blk_hi = (t_hi - 1) >> 4;
+  // (blocks without keys of the tile are not named: their neighbour stands in, and is masked)
+  auto id_of = [&](int blk) { return table[min(max(blk, blk_lo), blk_hi)]; };
+  u32x4 kr[W::kChunks], vr[W::kChunks];
+  uint32_t k_scale = 127, v_scale[4] = {0x7f7f7f7fu, 0x7f7f7f7fu, 0x7f7f7f7fu, 0x7f7f7f7fu};
+  int id_k = 0, id_v = 0;
+  auto load_ids = [&](int j) {
+    id_k = id_of(4 * j + (lane >> 4));
+    id_v = id_of(4 * j + wave);
+  };
+  auto load = [&]() {
+    const char* const kp = k_head + (long long)id_k * blk_stride + (lane & 15) * 16;
+    const char* const vp = v_head + (long long)id_v * blk_stride;
+#pragma unroll
+    for (int i = 0; i < W::kChunks; ++i) {
+      const int u = 4 * i + wave;  // unit of 16 bytes
+      if (u * C::kUnit < D) kr[i] = *reinterpret_cast<const u32x4*>(kp + u * 256);
+      const int piece = 64 * i + lane;  // of a block's V: 16 bytes of a channel
+      if (piece * 16 < blk_bytes) vr[i] = *reinterpret_cast<const u32x4*>(vp + piece * 16);
+    }
+    if constexpr (W::kNarrow) {
+      const uint8_t* const sc = scales + (size_t)g * kScaleBytes;
+      k_scale = sc[(long long)id_k * Hkv * kScaleBytes + (lane & 15)];
+      const u32x4 v = *reinterpret_cast<const u32x4*>(sc + (long long)id_v * Hkv * kScaleBytes + kBlockSize);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v_scale[i] = v[i];
+    }
+  };
+  // (j: the step that lies in the registers)
+  auto store = [&](int j) {
+    char* const kb = s_k[W::kBuffers == 2 ? j & 1 : 0];
+    char* const vb = s_v[W::kBuffers == 2 ? j & 1 : 0];
+    const u32x4 zero = {0, 0, 0, 0};
+    const float ks = scale_of_byte(k_scale);
+    bool bad = false;
+#pragma unroll
+    for (int i = 0; i < W::kChunks; ++i) {
+      const int u = 4 * i + wave;
+      if constexpr (W::kNarrow) {
+        u32x4 a = zero, b = zero;
+        if (u * 16 < D) {
+          a = __builtin_bit_cast(u32x4, codes_to_bf16x8<F>(kr[i][0], kr[i][1], ks));
+          b = __builtin_bit_cast(u32x4, codes_to_bf16x8<F>(kr[i][2], kr[i][3], ks));
+        }
+        *reinterpret_cast<u32x4*>(kb + ((2 * u) * kKeys + lane) * 16) = a;
+        *reinterpret_cast<u32x4*>(kb + ((2 * u + 1) * kKeys + lane) * 16) = b;
+      } else {
+        *reinterpret_cast<u32x4*>(kb + (u * kKeys + lane) * 16) = u * 8 < D ? kr[i] : zero;
+      }
+    }
+    // V: slots behind the tile's last key (nobody sees them) may hold anything: zeros.  So are those in front of the first.
+    const int key0 = j * kKeys + 16 * wave, keep_lo = t_lo - key0, keep_hi = t_hi - key0;  // of the block's 16 slots
+    if constexpr (W::kNarrow) {
+      float f[16];
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        const uint32_t sw = (uint32_t)__builtin_amdgcn_readfirstlane((int)v_scale[w]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int slot = 4 * w + e;
+          const uint32_t byte = (sw >> (8 * e)) & 255u;
+          const bool there = slot >= keep_lo && slot < keep_hi;
+          bad |= there && byte == kBadScale;
+          f[slot] = there && byte != kBadScale ? scale_of_byte(byte) : 0.f;
+        }
+      }
+      const bool edge = keep_lo > 0 || keep_hi < 16;
+#pragma unroll
+      for (int i = 0; i < W::kChunks; ++i) {
+        const int d = 64 * i + lane;
+        if (d >= D) continue;
+        u32x4 c = vr[i];
+        if (edge) {
+#pragma unroll
+          for (int w = 0; w < 4; ++w) {
+            uint32_t keep = 0;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) keep |= 4 * w + e >= keep_lo && 4 * w + e < keep_hi ? 0xffu << (8 * e) : 0u;
+            c[w] &= keep;
+          }
+        }
+        u32x4 lo8, hi8;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+          const uint32_t x = pack_bf16x2(code_value<F, 0>(c[w]) * f[4 * w], code_value<F, 1>(c[w]) * f[4 * w + 1]);
+          const uint32_t y = pack_bf16x2(code_value<F, 2>(c[w]) * f[4 * w + 2], code_value<F, 3>(c[w]) * f[4 * w + 3]);
+          if (w < 2) lo8[2 * w] = x, lo8[2 * w + 1] = y;
+          else hi8[2 * w - 4] = x, hi8[2 * w - 3] = y;
+        }
+        *reinterpret_cast<u32x4*>(vb + (2 * wave) * W::kOctet + d * 16) = lo8;
+        *reinterpret_cast<u32x4*>(vb + (2 * wave + 1) * W::kOctet + d * 16) = hi8;
+      }
+      if (bad && lane == 0) s_bad[j & 1] = j + 1;
+    } else {
+#pragma unroll
+      for (int i = 0; i < W::kChunks; ++i) {
+        const int piece = 64 * i + lane, d = piece >> 1, h8 = piece & 1;
+        if (d >= D) continue;
+        u32x4 c = vr[i];
+        if (keep_lo > 8 * h8 || keep_hi < 8 * h8 + 8) {
+#pragma unroll
+          for (int w = 0; w < 4; ++w) {
+            const int slot = 8 * h8 + 2 * w;
+            c[w] &= (slot >= keep_lo && slot < keep_hi ? 0xffffu : 0u) | (slot + 1 >= keep_lo && slot + 1 < keep_hi ? 0xffff0000u : 0u);
+          }
+        }
+        *reinterpret_cast<u32x4*>(vb + (2 * wave + h8) * W::kOctet + d * 16) = c;
+      }
+    }
+  };
+
+  f32x16 o[NC];
+#pragma unroll
+  for (int dt = 0; dt < NC; ++dt)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) o[dt][i] = 0.f;
+  float m = kLowest, l = 0.f, poison = 0.f;
+
+  // A-operand row -> key inside 32 keys: bits 2 and 3 swapped
+  const int krow = (col & 0x13) | ((col & 4) << 1) | ((col & 8) >> 1);
+  const int a_k_off = (half * kKeys + krow) * 16, a_v_off = half * W::kOctet + col * 16;
+
+  auto step = [&](int j) {
+    const char* const kb = s_k[W::kBuffers == 2 ? j & 1 : 0] + a_k_off;
+    const char* const vb = s_v[W::kBuffers == 2 ? j & 1 : 0] + a_v_off;
+    f32x16 s[2];
+#pragma unroll
+    for (int sub = 0; sub < 2; ++sub)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[sub][i] = 0.f;
+#pragma unroll
+    for (int t = 0; t < 2 * NC; ++t)
+#pragma unroll
+      for (int sub = 0; sub < 2; ++sub) {
+        const bf16x8 a = *reinterpret_cast<const bf16x8*>(kb + (2 * t * kKeys + 32 * sub) * 16);
+        s[sub] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, qf[t], s[sub], 0, 0, 0);
+      }
+    const int k0 = j * kKeys;
+    // register i of half-tile sub is key k0 + 32 sub + 16 (i / 8) + 8 half + i % 8
+    if (kForm) {
+      const float away = (float)(k0 + 8 * half - pos);
+#pragma unroll
+      for (int sub = 0; sub < 2; ++sub)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          float x = s[sub][i];
+          if (form.cap_in > 0.f) x = form.cap_log2e - 2.f * form.cap_log2e * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(x * form.cap_in));
+          else x *= form.scale_log2e;
+          s[sub][i] = __builtin_fmaf(slope, away + (float)(32 * sub + 16 * (i >> 3) + (i & 7)), x);
+        }
+    }
+    if (k0 < w_lo_last || k0 + kKeys > w_hi_first) {
+      asm volatile("" ::: "memory");  // (a branch, and no selects in every step)
+      const int first = lo - k0 - 8 * half, last = hi - k0 - 8 * half;
+#pragma unroll
+      for (int sub = 0; sub < 2; ++sub)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const int at = 32 * sub + 16 * (i >> 3) + (i & 7);
+          if (at < first || at >= last) s[sub][i] = -INFINITY;
+        }
+    }
+    const float c = kForm ? 1.f : form.scale_log2e;  // (with a form the scores are in the exp2 domain already)
+    float top = max3(s[0][0], s[0][1], s[0][2]);
+#pragma unroll
+    for (int i = 3; i < 15; i += 2) top = max3(top, s[0][i], s[0][i + 1]);
+    top = max3(top, s[0][15], s[1][0]);
+#pragma unroll
+    for (int i = 1; i < 15; i += 2) top = max3(top, s[1][i], s[1][i + 1]);
+    top = across_halves_max(fmaxf(top, s[1][15])) * c;
+    if (__any(top - m > kTau)) {
+      const float m_new = fmaxf(m, top), alpha = __builtin_amdgcn_exp2f(m - m_new);
+      l *= alpha;
+#pragma unroll
+      for (int dt = 0; dt < NC; ++dt) o[dt] *= alpha;
+      m = m_new;
+    }
+    bf16x8 p[4];
+    float sums[2] = {0.f, 0.f};
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      u32x4 w;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int i = 8 * (u & 1) + 2 * e;
+        const float a = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u >> 1][i], c, -m)), b = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u >> 1][i + 1], c, -m));
+        sums[0] += a;
+        sums[1] += b;
+        w[e] = pack_bf16x2(a, b);
+      }
+      p[u] = __builtin_bit_cast(bf16x8, w);
+    }
+    l += sums[0] + sums[1];
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+#pragma unroll
+      for (int dt = 0; dt < NC; ++dt) {
+        const bf16x8 a = *reinterpret_cast<const bf16x8*>(vb + 2 * u * W::kOctet + 32 * dt * 16);
+        o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, p[u], o[dt], 0, 0, 0);
+      }
+    if (W::kNarrow && s_bad[j & 1] == j + 1) {
+      // a value's scale says NaN: rows that see it are NaN
+      for (int at = max(lo, k0); at < min(hi, k0 + kKeys); ++at) {
+        const int id = table[at >> 4];
+        if (scales[((size_t)id * Hkv + g) * kScaleBytes + kBlockSize + (at & 15)] == kBadScale) poison = NAN;
+      }
+    }
+  };
+
+  if (j0 < j1) {
+    load_ids(j0);
+    load();
+    if (j0 + 1 < j1) load_ids(j0 + 1);
+    store(j0);
+    if (j0 + 1 < j1) {
+      load();
+      if (j0 + 2 < j1) load_ids(j0 + 2);
+    }
+    __syncthreads();
+    for (int j = j0; j < j1; ++j) {
+      if constexpr (W::kBuffers == 2) {
+        if (j + 1 < j1) {
+          store(j + 1);
+          if (j + 2 < j1) {
+            load();
+            if (j + 3 < j1) load_ids(j + 3);
+          }
+        }
+        if (j >= wj0 && j < wj1) step(j);
+        __syncthreads();
+      } else {
+        if (j >= wj0 && j < wj1) step(j);
+        __syncthreads();
+        if (j + 1 < j1) {
+          store(j + 1);
+          if (j + 2 < j1) {
+            load();
+            if (j + 3 < j1) load_ids(j + 3);
+          }
+        }
+        __syncthreads();
+      }
+    }
+  }
+  l = across_halves_sum(l);
+  if constexpr (W::kNarrow) {
+#pragma unroll
+    for (int dt = 0; dt < NC; ++dt)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) o[dt][i] += poison;
+  }
+
+  if (splits > 1) {
+    // ---- parts of the steps: the states, in the lanes' own order; the last workgroup adds them up
+    constexpr int kStateFloats = kTileRows * (32 * NC + 2);
+    const size_t item = blockIdx.x;
+    const __amdgpu_buffer_rsrc_t mine = __builtin_amdgcn_make_buffer_rsrc(states + (item * splits + blockIdx.y) * kStateFloats, 0, kStateFloats * 4, kRsrc);
+    const int at = (wave * NC * 1024 + lane * 4) * 4, at_ml = (kTileRows * 32 * NC + 2 * (wave * 32 + col)) * 4;
+#pragma unroll
+    for (int dt = 0; dt < NC; ++dt)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const f32x4 v = {o[dt][4 * r], o[dt][4 * r + 1], o[dt][4 * r + 2], o[dt][4 * r + 3]};
+        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, v), mine, at + (dt * 4 + r) * 1024, 0, kAgent);
+      }
+    if (half == 0) __builtin_amdgcn_raw_buffer_store_b64(u32x2{__float_as_uint(m), __float_as_uint(l)}, mine, at_ml, 0, kAgent);
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    if (tid == 0) s_order = (int)atomicInc(counters + item, (unsigned)splits - 1);
+    __syncthreads();
+    if (s_order != splits - 1) return;
+    float M = kLowest;
+    for (int k = 0; k < splits; ++k) {
+      const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(states + (item * splits + k) * kStateFloats, 0, kStateFloats * 4, kRsrc);
+      M = fmaxf(M, __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(r, at_ml, 0, kAgent)));
+    }
+    m = M;
+    l = 0.f;
+#pragma unroll
+    for (int dt = 0; dt < NC; ++dt)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) o[dt][i] = 0.f;
+    for (int k = 0; k < splits; ++k) {
+      const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(states + (item * splits + k) * kStateFloats, 0, kStateFloats * 4, kRsrc);
+      const u32x2 ml = __builtin_amdgcn_raw_buffer_load_b64(r, at_ml, 0, kAgent);
+      const float w = __builtin_amdgcn_exp2f(__uint_as_float(ml[0]) - M);
+      l += __uint_as_float(ml[1]) * w;
+#pragma unroll
+      for (int dt = 0; dt < NC; ++dt)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const f32x4 v = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(r, at + (dt * 4 + e) * 1024, 0, kAgent));
+#pragma unroll
+          for (int x = 0; x < 4; ++x) o[dt][4 * e + x] += v[x] * w;
+        }
+    }
+  }
+
+  // ---- results
+  bool again = false;
+  if constexpr (!W::kNarrow) {
+    float odd = 0.f;  // NaN, if any result is not finite
+#pragma unroll
+    for (int dt = 0; dt < NC; ++dt)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) odd = __builtin_fmaf(o[dt][i], 0.f, odd);
+    again = !none && across_halves_sum(odd) != 0.f && l < INFINITY;
+    for (uint32_t left = (uint32_t)__ballot(again && half == 0); left; left &= left - 1) {
+      const int r = __builtin_ctz(left);
+      const int r_tok = __builtin_amdgcn_readlane(tok, r), r_head = __builtin_amdgcn_readlane(head, r);
+      row_again<NC, kForm>(q + (size_t)r_tok * q_row_stride + (size_t)r_head * D, k_head, v_head, blk_stride, table, __builtin_amdgcn_readlane(lo, r),
+                           __builtin_amdgcn_readlane(hi, r), __builtin_amdgcn_readlane(pos, r),
+                           __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(slope), r)), form, D, out + ((size_t)r_tok * Hq + r_head) * D);
+    }
+  }
+  // Registers 4 i .. 4 i + 3 of o[dt] hold channels 32 dt + 8 i + 4 half + (0 .. 3).  The two lanes of a row exchange halves, so that each stores 16 bytes.
+  const float inv = none ? 0.f : 1.f / l;
+  auto pack = [&](float a, float b) { return none ? 0u : pack_bf16x2(a * inv, b * inv); };
+#pragma unroll
+  for (int dt = 0; dt < NC; ++dt)
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+      const auto a = __builtin_amdgcn_permlane32_swap(pack(o[dt][8 * r], o[dt][8 * r + 1]), pack(o[dt][8 * r + 4], o[dt][8 * r + 5]), false, false);
+      const auto b = __builtin_amdgcn_permlane32_swap(pack(o[dt][8 * r + 2], o[dt][8 * r + 3]), pack(o[dt][8 * r + 6], o[dt][8 * r + 7]), false, false);
+      const int d = 32 * dt + 16 * r + 8 * half;
+      if (valid && !again && d < D) *reinterpret_cast<u32x4*>(out_row + d) = u32x4{a[0], b[0], a[1], b[1]};
+    }
+  if (lse_row && valid && half == 0) *lse_row = none ? -INFINITY : (m + log2f(l)) * kLn2;
+}
+
+template <int F, int NC>
+void launch_formed(const ScoredArgs& a, int32_t splits, hipStream_t s) {
+  const int G = a.Hq / a.Hkv, units = (int)prefill_scored_tiles(a.B, a.T, G);
+  const bool formed = a.softcap > 0.f || a.slopes;
+  const Form form = {a.scale_log2e, a.softcap > 0.f ? 2.f * a.scale_log2e / a.softcap : 0.f, a.softcap * kLog2e, a.slopes};
+  auto go = [&](auto kernel) {
+    hipLaunchKernelGGL(kernel, dim3((unsigned)units * a.Hkv, (unsigned)splits), dim3(kThreads), 0, s, (const uint16_t*)a.q, a.q_row_stride, (const char*)a.k_cache,
+                       (const char*)a.v_cache, a.scales, a.cu_q, a.ctx_before, a.block_table, a.bt_stride, a.key_begin, a.key_end, (uint16_t*)a.out, a.lse, a.states,
+                       a.counters, a.B, a.Hq, a.Hkv, G, make_divisor(G), make_divisor(a.Hkv), a.D, units, form);
+  };
+  if (formed) go(&prefill_scored_kernel<F, NC, true>);
+  else go(&prefill_scored_kernel<F, NC, false>);
+}
+
+template <int F>
+void launch_format(const ScoredArgs& a, int32_t splits, hipStream_t s) {
+  switch (scored_chunks(a.D)) {
+    case 2: return launch_formed<F, 2>(a, splits, s);
+    case 4: return launch_formed<F, 4>(a, splits, s);
+    default: return launch_formed<F, 8>(a, splits, s);
+  }
+}
+
+}  // namespace
+
+hipError_t launch_prefill_scored(const ScoredArgs& a, int32_t splits, hipStream_t s) {
+  switch (a.format) {
+    case kInt8: launch_format<kInt8>(a, splits, s); break;
+    case kE4m3: launch_format<kE4m3>(a, splits, s); break;
+    default: launch_format<kNative>(a, splits, s); break;
+  }
+  return hipGetLastError();
+}
+
+}  // namespace eco

@@ -37,6 +37,14 @@ struct SparseEntries {
   decltype(&ecoserve_sparse_workspace_bytes) sparse_bytes;
   decltype(&ecoserve_attn_sparse) sparse;
 } more;
+struct ScoredEntries {
+  decltype(&ecoserve_kv_append_norm) append;
+  decltype(&ecoserve_kv_read) read;
+  decltype(&ecoserve_prefill_scored_workspace_bytes) prefill_bytes;
+  decltype(&ecoserve_attn_prefill_scored) prefill;
+  decltype(&ecoserve_decode_scored_workspace_bytes) decode_bytes;
+  decltype(&ecoserve_attn_decode_scored) decode;
+} scored;
 
 // Reads the arguments of a call.  What is binding.py's business is noted, and not thrown: an exception takes 2.5 us, half of what the
 // other way takes for such a call.
@@ -328,6 +336,131 @@ PyObject* attn_sparse(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+// What binding.PagedCache holds: the address of its struct and the tensors that the struct names, so that each call sees that they are still what it says.
+// (struct, k, v, scales) at i .. i + 3
+const ecoserve_cache* paged_cache(LayerArguments& in, int i) {
+  const auto* const cache = static_cast<const ecoserve_cache*>(in.handle(i));
+  if (!in.taken || !cache) return in.taken = false, nullptr;
+  const bool native = cache->format == ECOSERVE_CACHE_LAYOUT;
+  const at::ScalarType type = native ? in.element() : at::kByte;
+  const int64_t elements = in.side(16) * in.l->head_dim;
+  if (in.whole(i + 1, type, elements) != cache->k || in.whole(i + 2, type, elements) != cache->v) in.taken = false;
+  if (!native && in.whole(i + 3, at::kByte, in.side(32)) != cache->scales) in.taken = false;
+  return cache;
+}
+// (struct, slopes, key_begin, key_end) at i .. i + 3, the struct 0: none
+const ecoserve_scores* score_form(LayerArguments& in, int i, int64_t tokens) {
+  const auto* const scores = static_cast<const ecoserve_scores*>(in.handle(i));
+  if (!in.taken || !scores) return nullptr;
+  if (in.a[i + 1] != Py_None && in.whole(i + 1, at::kFloat, in.l->num_q_heads) != scores->slopes) in.taken = false;
+  if (in.a[i + 2] != Py_None && in.ints(i + 2, tokens) != scores->key_begin) in.taken = false;
+  if (in.a[i + 3] != Py_None && in.ints(i + 3, tokens) != scores->key_end) in.taken = false;
+  return scores;
+}
+
+// (handle, address of the layout, device, cache 3-6, norm 7, its weights 8-9, rope 10, inv_freq 11, positions 12, k_new 13, v_new 14, cu_q 15, ctx_before 16, block_table 17,
+// q 18, q_out 19, max_new_len 20)
+PyObject* kv_append_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded_layer(a, n, 21, [](LayerArguments& in, ecoserve_ctx* c) {
+    const ecoserve_cache* const cache = paged_cache(in, 3);
+    const auto* const norm = static_cast<const ecoserve_norm*>(in.handle(7));
+    const auto* const rope = static_cast<const ecoserve_rope*>(in.handle(10));
+    if (!in.taken) return -1;
+    const int32_t T = in.size(13, 0), B = in.numel(16), width = in.size(17, 1), most = in.or_all(20, T);
+    if (norm) {
+      const int64_t D = in.l->head_dim, q_heads = norm->per_head ? in.l->num_q_heads : 1, k_heads = norm->per_head ? in.l->num_kv_heads : 1;
+      if (in.a[8] != Py_None && (in.whole(8, at::kFloat, q_heads * D) != norm->q_weight || in.numel(8) != q_heads * D)) in.taken = false;
+      if (in.a[9] != Py_None && (in.whole(9, at::kFloat, k_heads * D) != norm->k_weight || in.numel(9) != k_heads * D)) in.taken = false;
+    }
+    const double* freq = nullptr;
+    const int32_t* positions = nullptr;
+    if (rope) {
+      freq = static_cast<const double*>(in.whole(11, at::kDouble, rope->rotary_dim / 2));
+      if (in.a[12] != Py_None) {
+        positions = in.ints(12, (int64_t)rope->num_axes * T);
+        if (in.size(12, 0) != rope->num_axes || in.size(12, 1) != T) in.taken = false;
+      }
+    }
+    const auto kn = in.rows(13, T, in.l->num_kv_heads), vn = in.rows(14, T, in.l->num_kv_heads);
+    if (kn.stride != vn.stride) in.taken = false;
+    const int32_t *const cu = in.ints(15, (int64_t)B + 1), *const before = in.ints(16, B), *const table = in.table(17, B);
+    LayerArguments::Rows q, qo;
+    if ((in.a[18] == Py_None) != (in.a[19] == Py_None)) in.taken = false;
+    if (in.taken && in.a[18] != Py_None) q = in.rows(18, T, in.l->num_q_heads), qo = in.rows(19, T, in.l->num_q_heads);
+    return in.call([&](void* s) {
+      return scored.append(c, cache, norm, rope, freq, positions, q.at, q.stride, qo.at, qo.stride, kn.at, vn.at, kn.stride, cu, before, table, width, B, T, most, s);
+    });
+  });
+}
+
+// (handle, address of the layout, device, cache 3-6, k_rows 7, v_rows 8, cu 9, first 10, block_table 11)
+PyObject* kv_read(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded_layer(a, n, 12, [](LayerArguments& in, ecoserve_ctx* c) {
+    const ecoserve_cache* const cache = paged_cache(in, 3);
+    if (in.a[7] == Py_None && in.a[8] == Py_None) return -1;
+    const int32_t T = in.size(in.a[7] == Py_None ? 8 : 7, 0), B = in.numel(10), width = in.size(11, 1);
+    LayerArguments::Rows k, v;
+    if (in.a[7] != Py_None) k = in.rows(7, T, in.l->num_kv_heads);
+    if (in.a[8] != Py_None) v = in.rows(8, T, in.l->num_kv_heads);
+    if (k.at && v.at && k.stride != v.stride) in.taken = false;
+    const int32_t *const cu = in.ints(9, (int64_t)B + 1), *const first = in.ints(10, B), *const table = in.table(11, B);
+    const int64_t stride = in.a[7] == Py_None ? v.stride : k.stride;
+    return in.call([&](void* s) { return scored.read(c, cache, k.at, v.at, stride, cu, first, table, width, B, T, s); });
+  });
+}
+
+// (handle, address of the layout, device, cache 3-6, scores 7-10, q 11, cu_q 12, ctx_before 13, block_table 14, out 15, lse 16, workspace 17)
+PyObject* attn_prefill_scored(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded_layer(a, n, 18, [](LayerArguments& in, ecoserve_ctx* c) {
+    const int32_t T = in.size(11, 0), B = in.numel(13), width = in.size(14, 1);
+    const ecoserve_cache* const cache = paged_cache(in, 3);
+    const ecoserve_scores* const form = score_form(in, 7, T);
+    const auto q = in.rows(11, T, in.l->num_q_heads);
+    const int32_t *const cu = in.ints(12, (int64_t)B + 1), *const before = in.ints(13, B), *const table = in.table(14, B);
+    const int64_t heads = (int64_t)T * in.l->num_q_heads;
+    void* const out = in.whole(15, in.element(), heads * in.l->head_dim);
+    float* const lse = in.a[16] == Py_None ? nullptr : static_cast<float*>(in.whole(16, at::kFloat, heads));
+    const auto ws = in.space(17, in.taken ? scored.prefill_bytes(c, B, T) : 0);
+    return in.call([&](void* s) { return scored.prefill(c, cache, form, q.at, q.stride, cu, before, table, width, out, lse, B, T, ws.at, ws.bytes, s); });
+  });
+}
+
+// (handle, address of the layout, device, cache 3-6, scores 7-10, q 11, block_table 12, ctx_len 13, out 14, lse 15, max_ctx_len 16, workspace 17)
+PyObject* attn_decode_scored(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded_layer(a, n, 18, [](LayerArguments& in, ecoserve_ctx* c) {
+    const int32_t B = in.numel(13), width = in.size(12, 1), most = in.narrow_integer(16);
+    const ecoserve_cache* const cache = paged_cache(in, 3);
+    const ecoserve_scores* const form = score_form(in, 7, B);
+    const auto q = in.rows(11, B, in.l->num_q_heads);
+    const int32_t *const table = in.table(12, B), *const len = in.ints(13, B);
+    const int64_t heads = (int64_t)B * in.l->num_q_heads;
+    void* const out = in.whole(14, in.element(), heads * in.l->head_dim);
+    float* const lse = in.a[15] == Py_None ? nullptr : static_cast<float*>(in.whole(15, at::kFloat, heads));
+    const auto ws = in.space(17, in.taken ? scored.decode_bytes(c) : 0);
+    return in.call([&](void* s) { return scored.decode(c, cache, form, q.at, q.stride, table, width, len, out, lse, B, most, ws.at, ws.bytes, s); });
+  });
+}
+
+// (addresses of the entry points, in the order of ScoredEntries)
+PyObject* bind_scored(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  void* at[6];
+  if (n != 6) {
+    PyErr_SetString(PyExc_TypeError, "bind_scored() takes six addresses");
+    return nullptr;
+  }
+  for (int i = 0; i < 6; ++i) {
+    at[i] = PyLong_AsVoidPtr(a[i]);
+    if (!at[i] && PyErr_Occurred()) return nullptr;
+  }
+  scored.append = reinterpret_cast<decltype(scored.append)>(at[0]);
+  scored.read = reinterpret_cast<decltype(scored.read)>(at[1]);
+  scored.prefill_bytes = reinterpret_cast<decltype(scored.prefill_bytes)>(at[2]);
+  scored.prefill = reinterpret_cast<decltype(scored.prefill)>(at[3]);
+  scored.decode_bytes = reinterpret_cast<decltype(scored.decode_bytes)>(at[4]);
+  scored.decode = reinterpret_cast<decltype(scored.decode)>(at[5]);
+  Py_RETURN_NONE;
+}
+
 // (addresses of the entry points, in the order of SparseEntries)
 PyObject* bind_sparse(PyObject*, PyObject* const* a, Py_ssize_t n) {
   void* at[6];
@@ -370,7 +503,8 @@ PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
 #define ECO_FAST(f) {#f, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {ECO_FAST(bind), ECO_FAST(kv_append), ECO_FAST(attn_prefill), ECO_FAST(attn_decode), ECO_FAST(attn_decode_append),
                          ECO_FAST(attn_decode_noalloc),
-                         ECO_FAST(bind_sparse), ECO_FAST(kv_append_rope), ECO_FAST(kv_summary), ECO_FAST(block_select), ECO_FAST(attn_sparse), {nullptr, nullptr, 0, nullptr}};
+                         ECO_FAST(bind_sparse), ECO_FAST(kv_append_rope), ECO_FAST(kv_summary), ECO_FAST(block_select), ECO_FAST(attn_sparse),
+                         ECO_FAST(bind_scored), ECO_FAST(kv_append_norm), ECO_FAST(kv_read), ECO_FAST(attn_prefill_scored), ECO_FAST(attn_decode_scored), {nullptr, nullptr, 0, nullptr}};
 // (ECO_BIND_FITS: the interpreter and the torch that this is compiled for; build.py looks for it in the built file)
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_bind", "Marshalling of the hot calls' arguments, " ECO_BIND_FITS, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

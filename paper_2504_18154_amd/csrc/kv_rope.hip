@@ -16,39 +16,13 @@
 #include <type_traits>
 
 #include "common.h"
+#include "turns.h"
 
 namespace eco {
 
 namespace {
 
 constexpr int kRopeThreads = 256;
-
-// What the kernels need of the rotation (by value: the axes of the pairs travel with the launch).
-struct Turns {
-  const double* inv_freq;
-  const int32_t* positions;  // [num_axes][T] or NULL
-  int32_t T, rotary, num_axes;
-  uint8_t axis[128];
-};
-
-struct Angle {
-  float c, s;
-};
-__device__ __forceinline__ Angle angle_of(int32_t position, double inv_freq) {
-  const double t = (double)position * (inv_freq * 0.15915494309189535);  // turns
-  const double q4 = (t - rint(t)) * 4.0, k = rint(q4);
-  const float a = (float)((q4 - k) * 1.5707963267948966), a2 = a * a;
-  const float s = a + a * a2 * (-1.f / 6 + a2 * (1.f / 120 + a2 * (-1.f / 5040 + a2 * (1.f / 362880))));
-  const float c = 1.f + a2 * (-0.5f + a2 * (1.f / 24 + a2 * (-1.f / 720 + a2 * (1.f / 40320 - a2 * (1.f / 3628800)))));
-  const int quarter = (int)k & 3;
-  const float x = quarter & 1 ? s : c, y = quarter & 1 ? c : s;
-  return {quarter == 1 || quarter == 2 ? -x : x, quarter >= 2 ? -y : y};
-}
-// The angle of pair i of packed token `tok`, at `place` in its sequence.
-__device__ __forceinline__ Angle angle_of_pair(const Turns& r, int i, int tok, int place) {
-  const int32_t p = r.positions ? r.positions[(size_t)(r.num_axes > 1 ? r.axis[i] : 0) * r.T + tok] : place;
-  return angle_of(p, r.inv_freq[i]);
-}
 
 template <typename E>
 __device__ __forceinline__ float value(E x) {
@@ -300,13 +274,7 @@ void launch_typed(const RopeAppend& a, const Turns& turns, int num_cu, hipStream
 }  // namespace
 
 hipError_t launch_kv_append_rope(const RopeAppend& a, const ecoserve_rope& rope, const double* inv_freq, const int32_t* positions, int num_cu, hipStream_t s) {
-  Turns t;
-  t.inv_freq = inv_freq;
-  t.positions = positions;
-  t.T = a.T;
-  t.rotary = rope.rotary_dim;
-  t.num_axes = rope.num_axes;
-  for (int i = 0; i < 128; ++i) t.axis[i] = rope.axis[i];
+  const Turns t = make_turns(rope, inv_freq, positions, a.T);
   const bool adjacent = rope.pairing == ECOSERVE_ROPE_ADJACENT;
   if (a.dtype == ECOSERVE_BF16) adjacent ? launch_typed<uint16_t, true>(a, t, num_cu, s) : launch_typed<uint16_t, false>(a, t, num_cu, s);
   else adjacent ? launch_typed<float, true>(a, t, num_cu, s) : launch_typed<float, false>(a, t, num_cu, s);

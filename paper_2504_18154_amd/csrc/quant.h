@@ -1,0 +1,86 @@
+// The caches of ecoserve_cache: codes of 8 bits with a scale per (token, head), or the layout's own bf16.
+//
+// A row of D elements with largest magnitude A is held as codes c of x ~ c 2^e, e the smallest integer >= -126 with A <= M 2^e (M = 127 for int8, 448 for
+// e4m3), and the byte e + 127: powers of two, so that coding is one rounding, decoding is none (a code has 4 or 7 bits, bf16 8), and the scales are the
+// operands that the conversions of gfx950 take.
+#pragma once
+
+#include "common.h"
+
+namespace eco {
+
+constexpr int kNative = ECOSERVE_CACHE_LAYOUT, kInt8 = ECOSERVE_CACHE_INT8, kE4m3 = ECOSERVE_CACHE_E4M3;
+constexpr int kScaleBytes = 2 * kBlockSize;  // of a (block, head): 16 of the keys, 16 of the values
+constexpr uint32_t kBadScale = 255;         // scale byte of a row that holds a NaN or an infinity (codes 0)
+
+inline bool quant_format_ok(int32_t format) { return format == kNative || format == kInt8 || format == kE4m3; }
+
+}  // namespace eco
+
+#if defined(__HIPCC__)
+namespace eco {
+
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+
+template <int F>
+struct Cached {
+  static constexpr int kBytes = F == kNative ? 2 : 1;   // of an element
+  static constexpr int kUnit = F == kNative ? 8 : 16;   // channels of a 16-byte unit of K
+};
+
+// 2^(b - 127) of byte i of a word of scale bytes; 255 gives infinity, whose product with a code of 0 is NaN.
+template <int I>
+__device__ __forceinline__ float scale_of(uint32_t w) {
+  const uint32_t at = I == 3 ? w >> 1 : w << (23 - 8 * I);
+  return __uint_as_float(at & 0x7f800000u);
+}
+__device__ __forceinline__ float scale_of_byte(uint32_t b) { return __uint_as_float(b << 23); }
+
+// Codes 0 .. 3 of a word as fp32.
+template <int F, int I>
+__device__ __forceinline__ float code_value(uint32_t w) {
+  if constexpr (F == kInt8) return (float)(int8_t)(w >> (8 * I));
+  else return __builtin_amdgcn_cvt_f32_fp8((int)w, I);
+}
+// Four codes as bf16, exactly, times a power of two.
+template <int F>
+__device__ __forceinline__ u32x2 codes_to_bf16(uint32_t w, float scale) {
+  if constexpr (F == kE4m3) {
+    return u32x2{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, false)),
+                 __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, true))};
+  } else {
+    return u32x2{pack_bf16x2(code_value<F, 0>(w) * scale, code_value<F, 1>(w) * scale), pack_bf16x2(code_value<F, 2>(w) * scale, code_value<F, 3>(w) * scale)};
+  }
+}
+template <int F>
+__device__ __forceinline__ bf16x8 codes_to_bf16x8(uint32_t a, uint32_t b, float scale) {
+  const u32x2 x = codes_to_bf16<F>(a, scale), y = codes_to_bf16<F>(b, scale);
+  return __builtin_bit_cast(bf16x8, u32x4{x[0], x[1], y[0], y[1]});
+}
+
+// The scale byte of a row with largest magnitude `most` (NaN and infinity: 255), and the factor 2^-e of its codes.
+template <int F>
+__device__ __forceinline__ uint32_t scale_byte(float most) {
+  if (!(most < INFINITY)) return kBadScale;
+  const uint32_t u = __float_as_uint(most);
+  // most = f 2^x with f in [1, 2): M = 1.984375 2^6 or 1.75 2^8
+  const int top = F == kInt8 ? 6 : 8;
+  const uint32_t edge = F == kInt8 ? 0x7e0000u : 0x600000u;
+  const int e = (int)(u >> 23) - 127 - top + ((u & 0x7fffffu) > edge ? 1 : 0);
+  return (uint32_t)(max(e, -126) + 127);
+}
+__device__ __forceinline__ float inverse_scale(uint32_t byte) { return ldexpf(1.f, 127 - (int)byte); }
+
+// Four values, times the inverse scale, as codes: one rounding to nearest even each.
+template <int F>
+__device__ __forceinline__ uint32_t to_codes(float a, float b, float c, float d) {
+  if constexpr (F == kE4m3) {
+    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false), true);
+  } else {
+    const int x = (int)rintf(a), y = (int)rintf(b), z = (int)rintf(c), w = (int)rintf(d);
+    return (uint32_t)(x & 255) | (uint32_t)(y & 255) << 8 | (uint32_t)(z & 255) << 16 | (uint32_t)w << 24;
+  }
+}
+
+}  // namespace eco
+#endif

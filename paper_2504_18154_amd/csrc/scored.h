@@ -1,0 +1,95 @@
+// Argument blocks, partitions and workspaces of attention over the caches of ecoserve_cache.  Plain arithmetic, for the launches, the entry points and a
+// host program alike.
+#pragma once
+
+#include <stddef.h>
+#include <stdint.h>
+
+#include <algorithm>
+
+#include "common.h"
+
+namespace eco {
+
+struct ScoredArgs {
+  const void* q;
+  int32_t q_row_stride;
+  const void *k_cache, *v_cache;
+  const uint8_t* scales;
+  const int32_t *cu_q, *ctx_before;  // prompts; decode: ctx_before is ctx_len and cu_q NULL
+  const int32_t* block_table;
+  int32_t bt_stride;
+  void* out;
+  float* lse;
+  const float* slopes;
+  const int32_t *key_begin, *key_end;
+  int32_t B, T, Hq, Hkv, D, format, num_cu;
+  float scale_log2e;  // scores live in the exp2 domain
+  float softcap;      // 0: none
+  float* states;
+  uint32_t* counters;  // zero between launches
+};
+
+// Floats of a slice's state of one query head: the unnormalised head vector, its maximum and its sum, and two that keep 16 bytes aligned.
+constexpr int32_t scored_state_words(int32_t D) { return D + 4; }
+
+// Decode: the steps of 32 tokens of every (sequence, K/V head) are cut into slices of about equal length, as many in all as `decode_scored_slices`, one
+// workgroup at a time each.
+constexpr int32_t kStepTokens = 32;
+constexpr int32_t kScoredMostSlices = 256;  // of a (sequence, K/V head)
+inline int32_t decode_scored_grid(int32_t num_cu) { return 3 * num_cu; }
+inline int32_t decode_scored_slices(int32_t num_cu) { return 2 * decode_scored_grid(num_cu); }
+// Slices of sequences that are cut, over all K/V heads: a sequence longer than the slices' length has less than twice as many as its length asks for.
+inline int64_t decode_scored_states(int32_t Hkv, int32_t num_cu) { return 2 * (int64_t)decode_scored_slices(num_cu) + 2 * Hkv; }
+inline size_t decode_scored_workspace(const ecoserve_layout& L, int32_t num_cu) {
+  return (size_t)decode_scored_states(L.num_kv_heads, num_cu) * (L.num_q_heads / L.num_kv_heads) * scored_state_words(L.head_dim) * 4;
+}
+
+// Prompts: tiles of 128 rows ((position, query head) pairs of a K/V head), their 64-key steps cut among `prefill_scored_splits` workgroups where tiles are few.
+constexpr int32_t kTileRows = 128;
+inline int64_t prefill_scored_tiles(int32_t B, int32_t T, int32_t G) { return (int64_t)T * G / kTileRows + (B < T ? B : T); }
+inline int32_t prefill_scored_splits(const ecoserve_layout& L, int32_t B, int32_t T, int32_t num_cu) {
+  const int64_t items = prefill_scored_tiles(B, T, L.num_q_heads / L.num_kv_heads) * L.num_kv_heads, room = 2 * (int64_t)num_cu / std::max<int64_t>(items, 1);
+  return room < 2 ? 1 : (int32_t)std::min<int64_t>(room, 32);
+}
+constexpr int32_t scored_chunks(int32_t D) { return D <= 64 ? 2 : D <= 128 ? 4 : 8; }  // of 32 channels, that a kernel's instance holds
+constexpr int64_t prefill_scored_state_floats(int32_t D) { return kTileRows * (32 * (int64_t)scored_chunks(D) + 2); }
+inline size_t prefill_scored_workspace(const ecoserve_layout& L, int32_t B, int32_t T, int32_t num_cu) {
+  const int32_t splits = prefill_scored_splits(L, B, T, num_cu);
+  if (splits == 1) return 0;
+  return (size_t)splits * prefill_scored_tiles(B, T, L.num_q_heads / L.num_kv_heads) * L.num_kv_heads * prefill_scored_state_floats(L.head_dim) * 4;
+}
+
+// decode of a few tokens and prompts (attn_scored_decode.hip, attn_scored_prefill.hip)
+hipError_t launch_decode_scored(const ScoredArgs& a, hipStream_t s);
+hipError_t launch_prefill_scored(const ScoredArgs& a, int32_t splits, hipStream_t s);
+
+// The append with norms, rotation and coding on the way, and reading back (kv_norm.hip)
+struct NormAppend {
+  const void* q;  // NULL: K and V alone
+  int32_t q_row_stride;
+  void* q_out;
+  int32_t q_out_row_stride;
+  void *k_cache, *v_cache;
+  uint8_t* scales;
+  const void *k_new, *v_new;
+  int32_t new_row_stride;
+  const int32_t *cu_q, *ctx_before, *block_table;
+  int32_t bt_stride, B, T, max_new_len, Hq, Hkv, D, format, num_cu;
+  bool norm;
+  float eps;
+  const float *q_weight, *k_weight;  // or NULL
+  int32_t weight_stride;             // 0: one for all heads
+};
+hipError_t launch_kv_append_norm(const NormAppend& a, const ecoserve_rope* rope, const double* inv_freq, const int32_t* positions, hipStream_t s);
+struct ReadBack {
+  const void *k_cache, *v_cache;
+  const uint8_t* scales;
+  void *k_rows, *v_rows;
+  int32_t row_stride;
+  const int32_t *cu, *first, *block_table;
+  int32_t bt_stride, B, T, Hkv, D, format, num_cu;
+};
+hipError_t launch_kv_read(const ReadBack& a, hipStream_t s);
+
+}  // namespace eco

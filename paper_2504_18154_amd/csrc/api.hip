@@ -648,6 +648,7 @@ int ecoserve_attn_decode_scored(ecoserve_ctx* c, const ecoserve_cache* cache, co
   if (!cache_there(cache) || !q || !block_table || !ctx_len || !out) return ECOSERVE_EINVAL;
   if (B > c->max_batch || bt_stride <= 0 || max_ctx_len < 1) return ECOSERVE_EINVAL;
   if ((int64_t)max_ctx_len > (int64_t)c->max_blocks_per_seq * kBlockSize || (int64_t)max_ctx_len > (int64_t)bt_stride * kBlockSize) return ECOSERVE_EINVAL;
+  if ((int64_t)B * (max_ctx_len / 32 + 2 + kPieceCost) > 0x7fffffffLL) return ECOSERVE_EINVAL;
   if (!aligned16(q) || !aligned16(out) || !aligned16(workspace) || (reinterpret_cast<uintptr_t>(lse) & 3u)) return ECOSERVE_EINVAL;
   if (!workspace || workspace_bytes < decode_scored_workspace(c->lay, c->num_cu)) return ECOSERVE_EINVAL;
   DeviceGuard guard(c->device);

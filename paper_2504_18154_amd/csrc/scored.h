@@ -30,19 +30,21 @@ struct ScoredArgs {
   uint32_t* counters;  // zero between launches
 };
 
+constexpr int32_t scored_chunks(int32_t D) { return D <= 64 ? 2 : D <= 128 ? 4 : 8; }  // of 32 channels, that a kernel's instance holds
 // Floats of a slice's state of one query head: the unnormalised head vector, its maximum and its sum, and two that keep 16 bytes aligned.
 constexpr int32_t scored_state_words(int32_t D) { return D + 4; }
 
-// Decode: the steps of 32 tokens of every (sequence, K/V head) are cut into slices of about equal length, as many in all as `decode_scored_slices`, one
-// workgroup at a time each.
-constexpr int32_t kStepTokens = 32;
-constexpr int32_t kScoredMostSlices = 256;  // of a (sequence, K/V head)
-inline int32_t decode_scored_grid(int32_t num_cu) { return 3 * num_cu; }
-inline int32_t decode_scored_slices(int32_t num_cu) { return 2 * decode_scored_grid(num_cu); }
-// Slices of sequences that are cut, over all K/V heads: a sequence longer than the slices' length has less than twice as many as its length asks for.
-inline int64_t decode_scored_states(int32_t Hkv, int32_t num_cu) { return 2 * (int64_t)decode_scored_slices(num_cu) + 2 * Hkv; }
+// Decode: the steps of 64 tokens of every (sequence, K/V head) are one numbering, cut into equal shares, one per workgroup.
+constexpr int32_t kScoredMostPieces = 256;  // of a (sequence, K/V head)
+constexpr int32_t kLeastSteps = 8;          // of a share
+constexpr int32_t kShortShare = 16;         // (see the kernel)
+constexpr int32_t kPieceCost = 4;           // units in front of a (sequence, K/V head)'s steps
+// Workgroups of four wavefronts that a CU holds, by the registers of the kernel's instances (chunks: of 32 channels).
+constexpr int32_t decode_scored_waves(bool narrow, int32_t chunks) { return chunks == 8 || (chunks == 4 && !narrow) ? 1 : 2; }
+// A workgroup cuts two (sequence, K/V head)s at most.
+constexpr int64_t decode_scored_states(int32_t chunks, int32_t num_cu) { return 2 * (int64_t)decode_scored_waves(true, chunks) * num_cu; }
 inline size_t decode_scored_workspace(const ecoserve_layout& L, int32_t num_cu) {
-  return (size_t)decode_scored_states(L.num_kv_heads, num_cu) * (L.num_q_heads / L.num_kv_heads) * scored_state_words(L.head_dim) * 4;
+  return (size_t)decode_scored_states(scored_chunks(L.head_dim), num_cu) * (L.num_q_heads / L.num_kv_heads) * scored_state_words(L.head_dim) * 4;
 }
 
 // Prompts: tiles of 128 rows ((position, query head) pairs of a K/V head), their 64-key steps cut among `prefill_scored_splits` workgroups where tiles are few.
@@ -52,7 +54,6 @@ inline int32_t prefill_scored_splits(const ecoserve_layout& L, int32_t B, int32_
   const int64_t items = prefill_scored_tiles(B, T, L.num_q_heads / L.num_kv_heads) * L.num_kv_heads, room = 2 * (int64_t)num_cu / std::max<int64_t>(items, 1);
   return room < 2 ? 1 : (int32_t)std::min<int64_t>(room, 32);
 }
-constexpr int32_t scored_chunks(int32_t D) { return D <= 64 ? 2 : D <= 128 ? 4 : 8; }  // of 32 channels, that a kernel's instance holds
 constexpr int64_t prefill_scored_state_floats(int32_t D) { return kTileRows * (32 * (int64_t)scored_chunks(D) + 2); }
 inline size_t prefill_scored_workspace(const ecoserve_layout& L, int32_t B, int32_t T, int32_t num_cu) {
   const int32_t splits = prefill_scored_splits(L, B, T, num_cu);

@@ -36,6 +36,7 @@ constexpr float kLowest = -3.0e38f;  // maximum before the first key: below ever
 constexpr float kTau = 8.f;          // the maximum in the exponent is raised when a score passes it by 2^8: weights reach that, and lose nothing by it
 constexpr int kRsrc = 0x00020000;
 constexpr int kAgent = 16;           // past the caches that XCDs do not share
+constexpr uint32_t kLeastShift = 67; // scale bytes from 2^-60 on
 
 __device__ __forceinline__ float across_halves_max(float x) {
   const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
@@ -109,7 +110,8 @@ __device__ __attribute__((noinline)) void row_again(const uint16_t* __restrict__
 }
 
 // Workgroup (x, y): K/V head x % Hkv of tile x / Hkv, counted from the last one; y: which part of its steps.
-template <int F, int NC, bool kForm>
+// kFull: the head vector fills the instance's channels.
+template <int F, int NC, bool kForm, bool kFull>
 __global__ __launch_bounds__(kThreads, NC == 8 ? 1 : 2) void prefill_scored_kernel(
     const uint16_t* __restrict__ q, int q_row_stride, const char* __restrict__ k_cache, const char* __restrict__ v_cache, const uint8_t* __restrict__ scales,
     const int32_t* __restrict__ cu_q, const int32_t* __restrict__ ctx_before, const int32_t* __restrict__ block_table, int bt_stride,
@@ -158,7 +160,8 @@ __global__ __launch_bounds__(kThreads, NC == 8 ? 1 : 2) void prefill_scored_kern
 
   // ---- staging: a step's 16-byte pieces to registers, and from there to LDS as bf16
   const int blk_bytes = kBlockSize * D * C::kBytes;
-  const long long blk_stride = (long long)Hkv * blk_bytes;
+  const uint32_t blk_stride = (uint32_t)Hkv * (uint32_t)blk_bytes;
+  [[maybe_unused]] const uint32_t scale_stride = (uint32_t)Hkv * kScaleBytes;
   const char *const k_head = k_cache + (size_t)g * blk_bytes, *const v_head = v_cache + (size_t)g * blk_bytes;
   const int32_t* const table = block_table + (size_t)seq.b * bt_stride;
   const int blk_lo = t_lo >> 4, blk_hi = (t_hi - 1) >> 4;
@@ -171,104 +174,145 @@ __global__ __launch_bounds__(kThreads, NC == 8 ? 1 : 2) void prefill_scored_kern
     id_k = id_of(4 * j + (lane >> 4));
     id_v = id_of(4 * j + wave);
   };
+  auto at_block = [](int id, uint32_t stride) { return (size_t)(uint32_t)id * stride; };
   auto load = [&]() {
-    const char* const kp = k_head + (long long)id_k * blk_stride + (lane & 15) * 16;
-    const char* const vp = v_head + (long long)id_v * blk_stride;
+    const char* const kp = k_head + at_block(id_k, blk_stride) + (lane & 15) * 16 + wave * 256;
+    const char* const vp = v_head + at_block(id_v, blk_stride) + lane * 16;
 #pragma unroll
     for (int i = 0; i < W::kChunks; ++i) {
-      const int u = 4 * i + wave;  // unit of 16 bytes
-      if (u * C::kUnit < D) kr[i] = *reinterpret_cast<const u32x4*>(kp + u * 256);
-      const int piece = 64 * i + lane;  // of a block's V: 16 bytes of a channel
-      if (piece * 16 < blk_bytes) vr[i] = *reinterpret_cast<const u32x4*>(vp + piece * 16);
+      if (kFull || (4 * i + wave) * C::kUnit < D) kr[i] = *reinterpret_cast<const u32x4*>(kp + 1024 * i);  // unit 4 i + wave
+      if (kFull || (64 * i + lane) * 16 < blk_bytes) vr[i] = *reinterpret_cast<const u32x4*>(vp + 1024 * i);
     }
     if constexpr (W::kNarrow) {
       const uint8_t* const sc = scales + (size_t)g * kScaleBytes;
-      k_scale = sc[(long long)id_k * Hkv * kScaleBytes + (lane & 15)];
-      const u32x4 v = *reinterpret_cast<const u32x4*>(sc + (long long)id_v * Hkv * kScaleBytes + kBlockSize);
+      k_scale = sc[at_block(id_k, scale_stride) + (lane & 15)];
+      const u32x4 v = *reinterpret_cast<const u32x4*>(sc + at_block(id_v, scale_stride) + kBlockSize);
 #pragma unroll
       for (int i = 0; i < 4; ++i) v_scale[i] = v[i];
     }
   };
   // (j: the step that lies in the registers)
   auto store = [&](int j) {
-    char* const kb = s_k[W::kBuffers == 2 ? j & 1 : 0];
-    char* const vb = s_v[W::kBuffers == 2 ? j & 1 : 0];
+    char* const kb = s_k[W::kBuffers == 2 ? j & 1 : 0] + lane * 16;
+    char* const vb = s_v[W::kBuffers == 2 ? j & 1 : 0] + 2 * wave * W::kOctet + (W::kNarrow ? lane * 16 : (lane >> 1) * 16 + (lane & 1) * W::kOctet);
     const u32x4 zero = {0, 0, 0, 0};
     const float ks = scale_of_byte(k_scale);
-    bool bad = false;
 #pragma unroll
     for (int i = 0; i < W::kChunks; ++i) {
       const int u = 4 * i + wave;
+      const bool there = kFull || u * C::kUnit < D;
       if constexpr (W::kNarrow) {
         u32x4 a = zero, b = zero;
-        if (u * 16 < D) {
+        if (there) {
           a = __builtin_bit_cast(u32x4, codes_to_bf16x8<F>(kr[i][0], kr[i][1], ks));
           b = __builtin_bit_cast(u32x4, codes_to_bf16x8<F>(kr[i][2], kr[i][3], ks));
         }
-        *reinterpret_cast<u32x4*>(kb + ((2 * u) * kKeys + lane) * 16) = a;
-        *reinterpret_cast<u32x4*>(kb + ((2 * u + 1) * kKeys + lane) * 16) = b;
+        *reinterpret_cast<u32x4*>(kb + 2 * u * kKeys * 16) = a;
+        *reinterpret_cast<u32x4*>(kb + (2 * u + 1) * kKeys * 16) = b;
       } else {
-        *reinterpret_cast<u32x4*>(kb + (u * kKeys + lane) * 16) = u * 8 < D ? kr[i] : zero;
+        *reinterpret_cast<u32x4*>(kb + u * kKeys * 16) = there ? kr[i] : zero;
       }
     }
     // V: slots behind the tile's last key (nobody sees them) may hold anything: zeros.  So are those in front of the first.
     const int key0 = j * kKeys + 16 * wave, keep_lo = t_lo - key0, keep_hi = t_hi - key0;  // of the block's 16 slots
+    const bool edge = keep_lo > 0 || keep_hi < 16;
     if constexpr (W::kNarrow) {
-      float f[16];
+      uint32_t sw[4];
 #pragma unroll
-      for (int w = 0; w < 4; ++w) {
-        const uint32_t sw = (uint32_t)__builtin_amdgcn_readfirstlane((int)v_scale[w]);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int slot = 4 * w + e;
-          const uint32_t byte = (sw >> (8 * e)) & 255u;
-          const bool there = slot >= keep_lo && slot < keep_hi;
-          bad |= there && byte == kBadScale;
-          f[slot] = there && byte != kBadScale ? scale_of_byte(byte) : 0.f;
-        }
-      }
-      const bool edge = keep_lo > 0 || keep_hi < 16;
-#pragma unroll
-      for (int i = 0; i < W::kChunks; ++i) {
-        const int d = 64 * i + lane;
-        if (d >= D) continue;
-        u32x4 c = vr[i];
-        if (edge) {
-#pragma unroll
-          for (int w = 0; w < 4; ++w) {
-            uint32_t keep = 0;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) keep |= 4 * w + e >= keep_lo && 4 * w + e < keep_hi ? 0xffu << (8 * e) : 0u;
-            c[w] &= keep;
-          }
-        }
-        u32x4 lo8, hi8;
+      for (int w = 0; w < 4; ++w) sw[w] = (uint32_t)__builtin_amdgcn_readfirstlane((int)v_scale[w]);
+      auto clear = [&](const uint32_t (&keep)[4]) {  // (the slots' codes, and scales that say nothing)
 #pragma unroll
         for (int w = 0; w < 4; ++w) {
-          const uint32_t x = pack_bf16x2(code_value<F, 0>(c[w]) * f[4 * w], code_value<F, 1>(c[w]) * f[4 * w + 1]);
-          const uint32_t y = pack_bf16x2(code_value<F, 2>(c[w]) * f[4 * w + 2], code_value<F, 3>(c[w]) * f[4 * w + 3]);
-          if (w < 2) lo8[2 * w] = x, lo8[2 * w + 1] = y;
-          else hi8[2 * w - 4] = x, hi8[2 * w - 3] = y;
-        }
-        *reinterpret_cast<u32x4*>(vb + (2 * wave) * W::kOctet + d * 16) = lo8;
-        *reinterpret_cast<u32x4*>(vb + (2 * wave + 1) * W::kOctet + d * 16) = hi8;
-      }
-      if (bad && lane == 0) s_bad[j & 1] = j + 1;
-    } else {
+          sw[w] = (sw[w] & keep[w]) | (0x7f7f7f7fu & ~keep[w]);
 #pragma unroll
-      for (int i = 0; i < W::kChunks; ++i) {
-        const int piece = 64 * i + lane, d = piece >> 1, h8 = piece & 1;
-        if (d >= D) continue;
-        u32x4 c = vr[i];
-        if (keep_lo > 8 * h8 || keep_hi < 8 * h8 + 8) {
+          for (int i = 0; i < W::kChunks; ++i) vr[i][w] &= keep[w];
+        }
+      };
+      if (edge) {
+        uint32_t keep[4] = {0, 0, 0, 0};
+#pragma unroll
+        for (int slot = 0; slot < 16; ++slot) keep[slot >> 2] |= slot >= keep_lo && slot < keep_hi ? 0xffu << (8 * (slot & 3)) : 0u;
+        clear(keep);
+      }
+      // (a byte of 255 is a zero byte of ~w)
+      auto any_bad = [&]() {
+        uint32_t bad = 0;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) bad |= (~sw[w] - 0x01010101u) & sw[w] & 0x80808080u;
+        return bad != 0;
+      };
+      if (any_bad()) {
+        uint32_t keep[4] = {0, 0, 0, 0};
+#pragma unroll
+        for (int slot = 0; slot < 16; ++slot) keep[slot >> 2] |= ((sw[slot >> 2] >> (8 * (slot & 3))) & 255u) != kBadScale ? 0xffu << (8 * (slot & 3)) : 0u;
+        clear(keep);
+        if (lane == 0) s_bad[j & 1] = j + 1;
+      }
+      bool small = false;
+      if constexpr (F == kE4m3) {
+        // (no byte borrows: its top bit is set before, and gone behind if the rest is below 67)
+#pragma unroll
+        for (int w = 0; w < 4; ++w) small |= (~((sw[w] | 0x80808080u) - kLeastShift * 0x01010101u) & ~sw[w] & 0x80808080u) != 0;
+      }
+      if (F == kE4m3 && !small) {
+        // A scale is a whole number added to the exponent of a bf16: two at a time.  The codes are made 2^-60 of themselves first, so that all sums are positive; a code
+        // of zero becomes 2^-67 of the scale's unit, which no sum of fp32 notices beside a code.  (As products in fp32: twice the instructions.)
+        typedef uint16_t half2 __attribute__((ext_vector_type(2)));
+        half2 up[8];
+#pragma unroll
+        for (int t = 0; t < 8; ++t) {
+          const uint32_t w = sw[t >> 1], two = t & 1 ? ((w >> 9) & 0x7f80u) | ((w >> 1) & 0x7f800000u) : ((w << 7) & 0x7f80u) | ((w << 15) & 0x7f800000u);
+          up[t] = __builtin_bit_cast(half2, two - kLeastShift * 0x00800080u);
+        }
+#pragma unroll
+        for (int i = 0; i < W::kChunks; ++i) {
+          u32x4 x[2];
 #pragma unroll
           for (int w = 0; w < 4; ++w) {
-            const int slot = 8 * h8 + 2 * w;
-            c[w] &= (slot >= keep_lo && slot < keep_hi ? 0xffffu : 0u) | (slot + 1 >= keep_lo && slot + 1 < keep_hi ? 0xffff0000u : 0u);
+            const u32x2 y = codes_to_bf16<F>(vr[i][w], 0x1p-60f);
+            const uint32_t y0 = y[0], y1 = y[1];  // (a cast of a vector's element takes its first one)
+            const half2 z0 = __builtin_bit_cast(half2, y0) + up[2 * w], z1 = __builtin_bit_cast(half2, y1) + up[2 * w + 1];
+            x[w >> 1][2 * (w & 1)] = __builtin_bit_cast(uint32_t, z0);
+            x[w >> 1][2 * (w & 1) + 1] = __builtin_bit_cast(uint32_t, z1);
+          }
+          if (kFull || 64 * i + lane < D) {
+            *reinterpret_cast<u32x4*>(vb + 1024 * i) = x[0];
+            *reinterpret_cast<u32x4*>(vb + 1024 * i + W::kOctet) = x[1];
           }
         }
-        *reinterpret_cast<u32x4*>(vb + (2 * wave + h8) * W::kOctet + d * 16) = c;
+      } else {
+        float f[16];
+#pragma unroll
+        for (int w = 0; w < 4; ++w) f[4 * w] = scale_of<0>(sw[w]), f[4 * w + 1] = scale_of<1>(sw[w]), f[4 * w + 2] = scale_of<2>(sw[w]), f[4 * w + 3] = scale_of<3>(sw[w]);
+#pragma unroll
+        for (int i = 0; i < W::kChunks; ++i) {
+          u32x4 x[2];
+#pragma unroll
+          for (int w = 0; w < 4; ++w) {
+            const uint32_t c = vr[i][w];
+            x[w >> 1][2 * (w & 1)] = pack_bf16x2(code_value<F, 0>(c) * f[4 * w], code_value<F, 1>(c) * f[4 * w + 1]);
+            x[w >> 1][2 * (w & 1) + 1] = pack_bf16x2(code_value<F, 2>(c) * f[4 * w + 2], code_value<F, 3>(c) * f[4 * w + 3]);
+          }
+          if (kFull || 64 * i + lane < D) {
+            *reinterpret_cast<u32x4*>(vb + 1024 * i) = x[0];
+            *reinterpret_cast<u32x4*>(vb + 1024 * i + W::kOctet) = x[1];
+          }
+        }
       }
+    } else {
+      if (edge) {
+        const int h8 = 8 * (lane & 1);
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+          const int slot = h8 + 2 * w;
+          const uint32_t keep = (slot >= keep_lo && slot < keep_hi ? 0xffffu : 0u) | (slot + 1 >= keep_lo && slot + 1 < keep_hi ? 0xffff0000u : 0u);
+#pragma unroll
+          for (int i = 0; i < W::kChunks; ++i) vr[i][w] &= keep;
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < W::kChunks; ++i)
+        if (kFull || 32 * i + (lane >> 1) < D) *reinterpret_cast<u32x4*>(vb + 512 * i) = vr[i];
     }
   };
 
@@ -501,8 +545,9 @@ void launch_formed(const ScoredArgs& a, int32_t splits, hipStream_t s) {
                        (const char*)a.v_cache, a.scales, a.cu_q, a.ctx_before, a.block_table, a.bt_stride, a.key_begin, a.key_end, (uint16_t*)a.out, a.lse, a.states,
                        a.counters, a.B, a.Hq, a.Hkv, G, make_divisor(G), make_divisor(a.Hkv), a.D, units, form);
   };
-  if (formed) go(&prefill_scored_kernel<F, NC, true>);
-  else go(&prefill_scored_kernel<F, NC, false>);
+  const bool full = a.D == 32 * NC;
+  if (formed) full ? go(&prefill_scored_kernel<F, NC, true, true>) : go(&prefill_scored_kernel<F, NC, true, false>);
+  else full ? go(&prefill_scored_kernel<F, NC, false, true>) : go(&prefill_scored_kernel<F, NC, false, false>);
 }
 
 template <int F>

@@ -36,7 +36,7 @@ constexpr float kLowest = -3.0e38f;  // maximum before the first key: below ever
 constexpr float kTau = 8.f;          // the maximum in the exponent is raised when a score passes it by 2^8: weights reach that, and lose nothing by it
 constexpr int kRsrc = 0x00020000;
 constexpr int kAgent = 16;           // past the caches that XCDs do not share
-constexpr uint32_t kLeastShift = 67; // scale bytes from 2^-60 on
+constexpr uint32_t kLeastShift = 67, kMostShift = 246;  // scale bytes, 2^-60 ... 2^119, whose sums with the exponent of any code stay inside it
 
 __device__ __forceinline__ float across_halves_max(float x) {
   const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
@@ -248,13 +248,14 @@ __global__ __launch_bounds__(kThreads, NC == 8 ? 1 : 2) void prefill_scored_kern
         clear(keep);
         if (lane == 0) s_bad[j & 1] = j + 1;
       }
-      bool small = false;
+      bool far = false;  // a scale outside kLeastShift ... kMostShift
       if constexpr (F == kE4m3) {
-        // (no byte borrows: its top bit is set before, and gone behind if the rest is below 67)
+        // (no byte borrows or carries: the top bits are set apart)
 #pragma unroll
-        for (int w = 0; w < 4; ++w) small |= (~((sw[w] | 0x80808080u) - kLeastShift * 0x01010101u) & ~sw[w] & 0x80808080u) != 0;
+        for (int w = 0; w < 4; ++w)
+          far |= (((~((sw[w] | 0x80808080u) - kLeastShift * 0x01010101u) & ~sw[w]) | (((sw[w] & 0x7f7f7f7fu) + (255u - kMostShift) * 0x01010101u) & sw[w])) & 0x80808080u) != 0;
       }
-      if (F == kE4m3 && !small) {
+      if (F == kE4m3 && !far) {
         // A scale is a whole number added to the exponent of a bf16: two at a time.  The codes are made 2^-60 of themselves first, so that all sums are positive; a code
         // of zero becomes 2^-67 of the scale's unit, which no sum of fp32 notices beside a code.  (As products in fp32: twice the instructions.)
         typedef uint16_t half2 __attribute__((ext_vector_type(2)));
@@ -345,26 +346,26 @@ __global__ __launch_bounds__(kThreads, NC == 8 ? 1 : 2) void prefill_scored_kern
     const int k0 = j * kKeys;
     // register i of half-tile sub is key k0 + 32 sub + 16 (i / 8) + 8 half + i % 8
     if (kForm) {
-      const float away = (float)(k0 + 8 * half - pos);
+      const float at_first = slope * (float)(k0 + 8 * half - pos);  // (the further keys' bias is slope times a literal)
 #pragma unroll
       for (int sub = 0; sub < 2; ++sub)
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
           float x = s[sub][i];
-          if (form.cap_in > 0.f) x = form.cap_log2e - 2.f * form.cap_log2e * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(x * form.cap_in));
-          else x *= form.scale_log2e;
-          s[sub][i] = __builtin_fmaf(slope, away + (float)(32 * sub + 16 * (i >> 3) + (i & 7)), x);
+          if (form.cap_in > 0.f) x = __builtin_fmaf(-2.f * form.cap_log2e, __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(x * form.cap_in)), form.cap_log2e + at_first);
+          else x = __builtin_fmaf(x, form.scale_log2e, at_first);
+          s[sub][i] = __builtin_fmaf(slope, (float)(32 * sub + 16 * (i >> 3) + (i & 7)), x);
         }
     }
     if (k0 < w_lo_last || k0 + kKeys > w_hi_first) {
       asm volatile("" ::: "memory");  // (a branch, and no selects in every step)
-      const int first = lo - k0 - 8 * half, last = hi - k0 - 8 * half;
+      const unsigned from = (unsigned)(k0 + 8 * half - lo), keys = (unsigned)max(hi - lo, 0);
 #pragma unroll
       for (int sub = 0; sub < 2; ++sub)
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
           const int at = 32 * sub + 16 * (i >> 3) + (i & 7);
-          if (at < first || at >= last) s[sub][i] = -INFINITY;
+          if (from + at >= keys) s[sub][i] = -INFINITY;
         }
     }
     const float c = kForm ? 1.f : form.scale_log2e;  // (with a form the scores are in the exp2 domain already)

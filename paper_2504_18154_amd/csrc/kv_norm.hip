@@ -3,13 +3,16 @@
 // A row (token, head) is D elements, 8 to a lane: 8, 16 or 32 lanes of a wavefront hold it (D <= 64, 128, 256), sum its squares and find its largest magnitude
 // among themselves.  All of it is fp32, rounded once: to bf16, or to codes (quant.h).
 //   norm      y = x / sqrt(mean(x^2) + eps) * w
-//   rotation  pair (a, b) -> (a cos - b sin, a sin + b cos); kv_rope.hip says how the angles are formed.  Pairs are normed by the same factor, so a lane reads the
-//             partners of its elements from memory (they are its neighbours', in the same lines) and needs no exchange.
+//   rotation  pair (a, b) -> (a cos - b sin, a sin + b cos); kv_rope.hip says how the angles are formed.  A token's weights and angles make one pair of factors per
+//             element, for itself and its partner, and the norm's 1 / sqrt multiplies the sum.  Partners come from the lane that has them; where they are not
+//             eight in a lane (rotary widths that are odd multiples of 8), from memory.
 //   codes     the scale from the largest magnitude of the turned row, then one rounding
 //
-// Memory bounds the large calls, launch latency and a few round trips the small ones.  A lane keeps its token's angles and the weights and walks the heads.  The
-// blocks of the batch are numbered as in kv_append.hip; a workgroup takes the tokens of one block and a run of heads of K and Q, or up to four heads of V, whose
-// codes go through LDS to lie along the slots.
+// Memory bounds the large calls, launch latency and a few round trips the small ones.  A lane keeps its token's factors and walks the heads, the next ones' loads
+// in flight.  The blocks of the batch are numbered as in kv_append.hip; a workgroup takes the tokens of one block and a run of heads of K and Q, or up to four
+// heads of V, whose codes go through LDS to lie along the slots.
+// Measured, 64 query heads and 8 of K and V, of 128, rotated and normed: 65 536 tokens into 8-bit codes 515 us (2.55 GB, 4.9 TB/s; a copy reaches 5.0), three chunks
+// of 200 ... 1500 tokens into bf16 37 us, a token of each of 64 sequences (40 query heads) 5.6 us.
 #include <type_traits>
 
 #include "quant.h"
@@ -21,6 +24,10 @@ namespace eco {
 namespace {
 
 constexpr int kThreads = 256;
+constexpr int kVHeads = 4;  // heads of V to a workgroup
+// Heads of K and Q to a workgroup from which its lanes work on two rows at a time.  72 heads of 65 536 tokens: 573 us with one, 515 with two.  7 heads of 2400
+// tokens: 37 with one, 47 with two, whose registers (114 for 86) leave fewer workgroups to a CU.
+constexpr int kManyHeads = 16;
 
 // Sum and maximum over the LP lanes that hold a row; every lane has the result, in the same order of sums everywhere.
 template <int LP, typename Op>
@@ -49,97 +56,121 @@ struct NormArgs {
   const float *q_weight, *k_weight;
   const int32_t *cu_q, *ctx_before, *block_table;
   int q_row_stride, q_out_row_stride, new_row_stride, bt_stride, B, Hq, Hkv, D, weight_stride;
-  float eps;
-  bool norm;
+  float eps, per_D;  // per_D: 1 / D, or 0 without a norm
 };
 
-// What a lane needs of its 8 elements' places: which are turned, and where their partners stand.
+// What a lane needs of its 8 elements' places: element i becomes x c[i] + (its partner) s[i].
 template <bool kAdjacent>
 struct Place {
   int e0, D;           // first element; lanes behind the row hold zeros
   bool here, turned;   // turned: all 8 are (rotary is a multiple of 8)
-  int away[2];         // of the partners of elements 0 .. 3 and 4 .. 7
-  Angle an[kAdjacent ? 4 : 8];
-  __device__ __forceinline__ Place(int l, int D_) : e0(8 * l), D(D_), here(8 * l < D_), turned(false) { away[0] = away[1] = 0; }
+  bool exchanged;      // the partners are one lane's 8 elements (rotary is a multiple of 16)
+  int from;            // that lane, for the exchange
+  int away[2];         // else: of the partners of elements 0 .. 3 and 4 .. 7
+  float c[8], s[8];
+  __device__ __forceinline__ Place(int l, int D_) : e0(8 * l), D(D_), here(8 * l < D_), turned(false), exchanged(true), from(0) { away[0] = away[1] = 0; }
   __device__ __forceinline__ void angles(const Turns& turns, int tok, int position) {
     const int R = turns.rotary, half = R >> 1;
     turned = e0 < R;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) c[i] = 1.f, s[i] = -0.f;  // (a partner of 0 leaves x as it is, the sign of a zero too)
+    exchanged = !(half & 7);
+    from = 4 * ((int)(threadIdx.x & 63) + (e0 < half ? half : -half) / 8);
     if (!turned) return;
     if constexpr (kAdjacent) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) an[i] = angle_of_pair(turns, (e0 >> 1) + i, tok, position);
+      for (int i = 0; i < 4; ++i) {
+        const Angle t = angle_of_pair(turns, (e0 >> 1) + i, tok, position);
+        c[2 * i] = c[2 * i + 1] = t.c;
+        s[2 * i] = -t.s, s[2 * i + 1] = t.s;
+      }
     } else {
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         const bool second = e0 + 4 * h >= half;
         away[h] = second ? -half : half;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) an[4 * h + i] = angle_of_pair(turns, e0 + 4 * h + i - (second ? half : 0), tok, position);
+        for (int i = 0; i < 4; ++i) {
+          const Angle t = angle_of_pair(turns, e0 + 4 * h + i - (second ? half : 0), tok, position);
+          c[4 * h + i] = t.c;
+          s[4 * h + i] = second ? t.s : -t.s;
+        }
       }
     }
   }
 };
 
-// A row's elements as they come, and their partners'.
+// A row's elements as they come, and their partners' where these have to be loaded.
 template <bool kAdjacent>
 struct Raw {
-  Eight own;
-  Four partner[2];
+  u32x4 own, partner;
   __device__ __forceinline__ void load(const uint16_t* row, const Place<kAdjacent>& at) {
-    own = Eight{};
-    if (at.here) own = *reinterpret_cast<const Eight*>(row + at.e0);
-    if (!kAdjacent && at.turned)
+    own = partner = u32x4{0, 0, 0, 0};
+    if (at.here) own = *reinterpret_cast<const u32x4*>(row + at.e0);
+    if (!kAdjacent && !at.exchanged && at.turned)
 #pragma unroll
-      for (int h = 0; h < 2; ++h) partner[h] = *reinterpret_cast<const Four*>(row + at.e0 + 4 * h + at.away[h]);
+      for (int h = 0; h < 2; ++h) {
+        const u32x2 x = *reinterpret_cast<const u32x2*>(row + at.e0 + 4 * h + at.away[h]);
+        partner[2 * h] = x[0], partner[2 * h + 1] = x[1];
+      }
+  }
+  __device__ __forceinline__ void exchange(const Place<kAdjacent>& at) {
+    if constexpr (kAdjacent) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) partner[i] = at.turned ? __builtin_amdgcn_alignbit(own[i], own[i], 16) : 0u;
+    } else if (at.exchanged) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t x = (uint32_t)__builtin_amdgcn_ds_bpermute(at.from, (int)own[i]);
+        partner[i] = at.turned ? x : 0u;
+      }
+    }
   }
 };
+// The factors of a row's elements and of their partners: the rotation's, times the weights (NULL: 1).
 template <bool kAdjacent>
-struct Weights {
+struct Factors {
   float own[8], partner[8];
-  __device__ __forceinline__ void load(const float* w, const Place<kAdjacent>& at) {
+  __device__ __forceinline__ void set(const float* w, const Place<kAdjacent>& at) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) own[i] = partner[i] = 1.f;
+    for (int i = 0; i < 8; ++i) own[i] = at.c[i], partner[i] = at.s[i];
     if (!w || !at.here) return;
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       const f32x4 a = *reinterpret_cast<const f32x4*>(w + at.e0 + 4 * h);
       f32x4 b = a;
-      if (!kAdjacent && at.turned) b = *reinterpret_cast<const f32x4*>(w + at.e0 + 4 * h + at.away[h]);
+      if (kAdjacent) b = f32x4{a[1], a[0], a[3], a[2]};
+      else if (at.turned) b = *reinterpret_cast<const f32x4*>(w + at.e0 + 4 * h + at.away[h]);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) own[4 * h + i] = a[i], partner[4 * h + i] = b[i];
+      for (int i = 0; i < 4; ++i) {
+        own[4 * h + i] *= a[i];
+        if (at.turned) partner[4 * h + i] *= b[i];
+      }
     }
   }
 };
-
-template <int LP, bool kAdjacent>
-__device__ __forceinline__ void formed(float (&y)[8], const Raw<kAdjacent>& raw, const Weights<kAdjacent>& w, const Place<kAdjacent>& at, bool norm, float eps) {
+__device__ __forceinline__ void values_of(float (&y)[8], u32x4 x) {
 #pragma unroll
-  for (int i = 0; i < 8; ++i) y[i] = bf16_bits_to_float(raw.own.e[i]);
-  float f = 1.f;
-  if (norm) {
+  for (int i = 0; i < 8; ++i) y[i] = __uint_as_float(i & 1 ? x[i >> 1] & 0xffff0000u : x[i >> 1] << 16);
+}
+
+// per_D: 1 / D, or 0 without a norm
+template <int LP, bool kAdjacent>
+__device__ __forceinline__ void formed(float (&y)[8], Raw<kAdjacent>& raw, const Factors<kAdjacent>& by, const Place<kAdjacent>& at, float per_D, float eps) {
+  float x[8], other[8];
+  raw.exchange(at);
+  values_of(x, raw.own);
+  values_of(other, raw.partner);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) y[i] = __builtin_fmaf(other[i], by.partner[i], x[i] * by.own[i]);
+  if (per_D > 0.f) {
     float sum = 0.f;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) sum = __builtin_fmaf(y[i], y[i], sum);
+    for (int i = 0; i < 8; ++i) sum = __builtin_fmaf(x[i], x[i], sum);
     sum = over_row<LP>(sum, [](float a, float b) { return a + b; });
-    f = rsqrtf(sum / (float)at.D + eps);
+    const float f = rsqrtf(__builtin_fmaf(sum, per_D, eps));
 #pragma unroll
-    for (int i = 0; i < 8; ++i) y[i] = y[i] * f * w.own[i];
-  }
-  if (!at.turned) return;
-  if constexpr (kAdjacent) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float a = y[2 * i], b = y[2 * i + 1];
-      y[2 * i] = a * at.an[i].c - b * at.an[i].s;
-      y[2 * i + 1] = a * at.an[i].s + b * at.an[i].c;
-    }
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      float x = bf16_bits_to_float(raw.partner[i >> 2].e[i & 3]);
-      if (norm) x = x * f * w.partner[i];
-      y[i] = at.away[i >> 2] > 0 ? y[i] * at.an[i].c - x * at.an[i].s : x * at.an[i].s + y[i] * at.an[i].c;
-    }
+    for (int i = 0; i < 8; ++i) y[i] *= f;
   }
 }
 
@@ -180,9 +211,10 @@ __device__ __forceinline__ void transpose4(const uint32_t (&r)[4], uint32_t (&o)
   o[2] = __builtin_amdgcn_perm(d, b, 0x05040100u), o[3] = __builtin_amdgcn_perm(d, b, 0x07060302u);
 }
 
-template <int LP, int F, bool kAdjacent>
-__global__ __launch_bounds__(kThreads) void kv_append_norm_kernel(const NormArgs a, const Turns turns, int v_heads, int v_slices, int per_slice) {
-  constexpr int kBytes = Cached<F>::kBytes, kGroups = kThreads / LP, kAhead = 2;
+// kAhead: rows of a lane that are loaded while as many are worked on.
+template <int LP, int F, bool kAdjacent, int kAhead>
+__global__ __launch_bounds__(kThreads) void kv_append_norm_kernel(const NormArgs a, const Turns turns, int v_slices, int per_slice) {
+  constexpr int kBytes = Cached<F>::kBytes, kGroups = kThreads / LP;
   extern __shared__ __attribute__((aligned(16))) char staged[];
   const int D = a.D, Hkv = a.Hkv, tid = threadIdx.x, group = tid / LP, l = tid % LP;
   auto first_unit = [](int cu, int b) { return (cu >> 4) + 2 * b; };
@@ -197,22 +229,29 @@ __global__ __launch_bounds__(kThreads) void kv_append_norm_kernel(const NormArgs
   const size_t head_bytes = (size_t)kBlockSize * D * kBytes;
 
   if ((int)blockIdx.y < v_slices) {
-    const int g0 = blockIdx.y * v_heads, heads = min(v_heads, Hkv - g0);
+    const int g0 = blockIdx.y * kVHeads, heads = min(kVHeads, Hkv - g0);
     char* const dst = a.v_cache + (blk * Hkv + g0) * head_bytes;
     if constexpr (F != kNative) {
       const int row_bytes = D + 8;
-      for (int r = group; r < heads * 16; r += kGroups) {
-        const int h = r >> 4, slot = r & 15;
-        if (slot < lo || slot >= hi) continue;
-        Eight x = {};
-        if (8 * l < D) x = *reinterpret_cast<const Eight*>(a.v_new + (size_t)(t_slot0 + slot) * a.new_row_stride + (size_t)(g0 + h) * D + 8 * l);
-        float y[8];
+      constexpr int kRows = kVHeads * 16 / kGroups;
+      u32x4 x[kRows];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) y[i] = bf16_bits_to_float(x.e[i]);
+      for (int n = 0; n < kRows; ++n) {
+        const int r = group + n * kGroups, slot = r & 15;
+        x[n] = u32x4{0, 0, 0, 0};
+        if (r < heads * 16 && slot >= lo && slot < hi && 8 * l < D)
+          x[n] = *reinterpret_cast<const u32x4*>(a.v_new + (size_t)(t_slot0 + slot) * a.new_row_stride + (size_t)(g0 + (r >> 4)) * D + 8 * l);
+      }
+#pragma unroll
+      for (int n = 0; n < kRows; ++n) {
+        const int r = group + n * kGroups, slot = r & 15;
+        if (r >= heads * 16 || slot < lo || slot >= hi) continue;
+        float y[8];
+        values_of(y, x[n]);
         uint32_t byte;
         const u32x2 c = coded<LP, F>(y, byte);
         if (8 * l < D) *reinterpret_cast<u32x2*>(staged + r * row_bytes + 8 * l) = c;
-        if (l == 0) a.scales[(blk * Hkv + g0 + h) * kScaleBytes + kBlockSize + slot] = (uint8_t)byte;
+        if (l == 0) a.scales[(blk * Hkv + g0 + (r >> 4)) * kScaleBytes + kBlockSize + slot] = (uint8_t)byte;
       }
       __syncthreads();
       for (int u = tid; u < heads * (D / 4); u += kThreads) {
@@ -276,27 +315,36 @@ __global__ __launch_bounds__(kThreads) void kv_append_norm_kernel(const NormArgs
     const int tok = t_slot0 + slot;
     Place<kAdjacent> at(l, D);
     at.angles(turns, tok, (j << 4) + slot);
-    Weights<kAdjacent> w;
-    int w_of = -1;  // 0: K's, 1: Q's
-    for (int h0 = h_begin + group / kSlots; h0 < h_end; h0 += kAhead * kHeads) {
-      Raw<kAdjacent> raw[kAhead];
+    Factors<kAdjacent> by;
+    int by_of = -1;  // 0: K's, 1: Q's
+    const int step = kAhead * kHeads;
+    Raw<kAdjacent> next[kAhead];
+    auto load = [&](int h0) {
 #pragma unroll
       for (int n = 0; n < kAhead; ++n) {
         const int h = min(h0 + n * kHeads, h_end - 1);
-        raw[n].load(h < Hkv ? a.k_new + (size_t)tok * a.new_row_stride + (size_t)h * D : a.q + (size_t)tok * a.q_row_stride + (size_t)(h - Hkv) * D, at);
+        next[n].load(h < Hkv ? a.k_new + (size_t)tok * a.new_row_stride + (size_t)h * D : a.q + (size_t)tok * a.q_row_stride + (size_t)(h - Hkv) * D, at);
       }
+    };
+    int h0 = h_begin + group / kSlots;
+    load(h0);
+    for (; h0 < h_end; h0 += step) {
+      Raw<kAdjacent> raw[kAhead];
+#pragma unroll
+      for (int n = 0; n < kAhead; ++n) raw[n] = next[n];
+      if (h0 + step < h_end) load(h0 + step);
 #pragma unroll
       for (int n = 0; n < kAhead; ++n) {
         const int h = h0 + n * kHeads;
         if (h >= h_end) break;
         const bool is_q = h >= Hkv;
-        if (a.norm && (w_of != (int)is_q || a.weight_stride)) {
+        if (by_of != (int)is_q || a.weight_stride) {
           const float* const base = is_q ? a.q_weight : a.k_weight;
-          w.load(base ? base + (size_t)(is_q ? h - Hkv : h) * a.weight_stride : nullptr, at);
-          w_of = is_q;
+          by.set(base ? base + (size_t)(is_q ? h - Hkv : h) * a.weight_stride : nullptr, at);
+          by_of = is_q;
         }
         float y[8];
-        formed<LP>(y, raw[n], w, at, a.norm, a.eps);
+        formed<LP>(y, raw[n], by, at, a.per_D, a.eps);
         if (is_q) {
           if (at.here) *reinterpret_cast<Eight*>(a.q_out + (size_t)tok * a.q_out_row_stride + (size_t)(h - Hkv) * D + 8 * l) = rounded8(y);
         } else {
@@ -347,11 +395,11 @@ __global__ __launch_bounds__(kThreads) void kv_append_norm_one_kernel(const Norm
   at.angles(turns, tok, p);
   Raw<kAdjacent> raw;
   raw.load(src, at);
-  Weights<kAdjacent> w;
+  Factors<kAdjacent> by;
   const float* const base = is_q ? a.q_weight : a.k_weight;
-  if (a.norm) w.load(base ? base + (size_t)h * a.weight_stride : nullptr, at);
+  by.set(base ? base + (size_t)h * a.weight_stride : nullptr, at);
   float y[8];
-  formed<LP>(y, raw, w, at, a.norm, a.eps);
+  formed<LP>(y, raw, by, at, a.per_D, a.eps);
   if (is_q) {
     if (at.here) *reinterpret_cast<Eight*>(a.q_out + (size_t)tok * a.q_out_row_stride + (size_t)h * D + 8 * l) = rounded8(y);
   } else {
@@ -368,14 +416,16 @@ void launch_append(const NormAppend& a, const NormArgs& args, const Turns& turns
     hipLaunchKernelGGL((kv_append_norm_one_kernel<LP, F, kAdjacent>), dim3((unsigned)((rows + at_once - 1) / at_once)), dim3(threads), 0, s, args, turns, of_seq);
     return;
   }
-  const int v_heads = 4, v_slices = (a.Hkv + v_heads - 1) / v_heads, total = a.Hkv + (a.q ? a.Hq : 0);
+  const int v_slices = (a.Hkv + kVHeads - 1) / kVHeads, total = a.Hkv + (a.q ? a.Hq : 0);
   const int64_t units = (int64_t)a.T / 16 + 2 * (int64_t)a.B;
   // heads per workgroup: eight workgroups per CU, then more heads to an angle
   const int64_t want = (8 * (int64_t)a.num_cu + units - 1) / units;
   const int slices = (int)(want < total ? want : total), per_slice = (total + slices - 1) / slices;
   const dim3 grid((unsigned)units, (unsigned)(v_slices + (total + per_slice - 1) / per_slice));
-  const size_t lds = (size_t)v_heads * 16 * (F == kNative ? 2 * (a.D + 8) : a.D + 8);
-  hipLaunchKernelGGL((kv_append_norm_kernel<LP, F, kAdjacent>), grid, dim3(kThreads), lds, s, args, turns, v_heads, v_slices, per_slice);
+  const size_t lds = (size_t)kVHeads * 16 * (F == kNative ? 2 * (a.D + 8) : a.D + 8);
+  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(kThreads), lds, s, args, turns, v_slices, per_slice); };
+  if (per_slice >= kManyHeads) go(&kv_append_norm_kernel<LP, F, kAdjacent, 2>);
+  else go(&kv_append_norm_kernel<LP, F, kAdjacent, 1>);
 }
 
 // Workgroup x: a block of a sequence, numbered as above; y: up to `heads_of` heads.
@@ -462,8 +512,8 @@ hipError_t launch_kv_append_norm(const NormAppend& a, const ecoserve_rope* rope,
   if (rope) turns = make_turns(*rope, inv_freq, positions, a.T);
   const bool adjacent = rope && rope->pairing == ECOSERVE_ROPE_ADJACENT;
   const NormArgs args = {(const uint16_t*)a.q, (const uint16_t*)a.k_new, (const uint16_t*)a.v_new, (uint16_t*)a.q_out, (char*)a.k_cache, (char*)a.v_cache, a.scales,
-                         a.q_weight, a.k_weight, a.cu_q, a.ctx_before, a.block_table, a.q_row_stride, a.q_out_row_stride, a.new_row_stride, a.bt_stride, a.B, a.Hq, a.Hkv,
-                         a.D, a.weight_stride, a.eps, a.norm};
+                         a.norm ? a.q_weight : nullptr, a.norm ? a.k_weight : nullptr, a.cu_q, a.ctx_before, a.block_table, a.q_row_stride, a.q_out_row_stride, a.new_row_stride, a.bt_stride, a.B, a.Hq, a.Hkv,
+                         a.D, a.norm ? a.weight_stride : 0, a.eps, a.norm ? 1.f / (float)a.D : 0.f};
   auto with_lanes = [&](auto format, auto pairing) {
     constexpr int F = decltype(format)::value;
     constexpr bool kAdjacent = decltype(pairing)::value;

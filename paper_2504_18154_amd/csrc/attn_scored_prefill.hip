@@ -64,6 +64,46 @@ struct Tile {
   static constexpr int kChunks = kNarrow ? NC / 2 : NC;             // 16-byte loads of K, and of V, per thread and step
 };
 
+// The tile that `rank` others come before, by falling length (the keys that its last row sees, in at most 16 classes), in a batch of up to 64 sequences, one to a
+// lane; b = -1 behind the last tile.  A sequence's tiles grow longer, so those of class v and above are its last ones, and their number is a formula: v is found by
+// halving.  24 prompts of 5 ... 300 tokens: 30.4 us in the sequences' order, 26.6 in this one, which costs a workgroup 0.7 us (two prompts of 8192 tokens, which it
+// has nothing to offer: 2242 and 2265).  Where ranges are given the lengths are not known: three prompts of several documents 147 and 162.
+struct TileOf {
+  SeqOf seq;
+  int tile;
+};
+__device__ __forceinline__ TileOf heaviest_tile(const int32_t* __restrict__ cu_q, const int32_t* __restrict__ ctx_before, int B, int G, int rank) {
+  const int b = min((int)(threadIdx.x & 63), B - 1);
+  const int tok0 = cu_q[b], S = (int)(threadIdx.x & 63) < B ? cu_q[b + 1] - tok0 : 0, cb = ctx_before[b];
+  const int tiles = S > 0 ? (S * G + kTileRows - 1) / kTileRows : 0;
+  const int steps = lanes_max(tiles && cb + S > 0 ? (cb + S - 1) / kKeys + 1 : 0), shift = max(0, 28 - __builtin_clz(steps | 1));
+  // the first tile of class v: its last row sees key (v - 1) 64 2^shift
+  auto first_of = [&](int v) {
+    const long long at = ((long long)kKeys << shift) * (v - 1) - cb;
+    return v <= 0 || at <= 0 ? 0 : at >= S ? tiles : (int)at * G / kTileRows;
+  };
+  auto add = [](int x, int y) { return x + y; };
+  int lo = 0, hi = ((steps + (1 << shift) - 1) >> shift) + 1, above = 0;
+  while (hi - lo > 1) {
+    const int v = (lo + hi) >> 1, n = __builtin_amdgcn_readlane(lanes_scan(tiles - first_of(v), add), 63);
+    if (n > rank) lo = v;
+    else hi = v, above = n;
+  }
+  // (the rank's class is lo, and `above` tiles have higher ones)
+  const int upto = lanes_scan(first_of(hi) - first_of(lo), add);
+  const unsigned long long reach = __ballot(upto > rank - above);
+  TileOf r;
+  r.seq.b = -1;
+  if (!reach) return r;
+  const int who = __builtin_ctzll(reach);
+  r.seq.b = who;
+  r.seq.tok0 = __builtin_amdgcn_readlane(tok0, who);
+  r.seq.S = __builtin_amdgcn_readlane(S, who);
+  r.seq.cb = __builtin_amdgcn_readlane(cb, who);
+  r.tile = __builtin_amdgcn_readlane(first_of(hi), who) - (__builtin_amdgcn_readlane(upto, who) - (rank - above));
+  return r;
+}
+
 // What a row of scores needs of the score's form.
 struct Form {
   float scale_log2e, cap_in, cap_log2e;  // cap_in: 2 log2(e) scale / cap, or 0
@@ -126,8 +166,16 @@ __global__ __launch_bounds__(kThreads, NC == 8 ? 1 : 2) void prefill_scored_kern
   // ---- the tile, its rows and their keys
   const int xu = fast_div((int)blockIdx.x, div_hkv), g = (int)blockIdx.x - xu * Hkv, unit = units - 1 - xu;
   auto first_unit = [&](int cu, int b) { return (long long)cu * G / kTileRows + b; };
-  const SeqOf seq = find_sequence(cu_q, ctx_before, B, unit, first_unit);
-  const int rows = seq.S * G, row0 = (int)(unit - first_unit(seq.tok0, seq.b)) * kTileRows;
+  TileOf at_tile;
+  if (B > 2 && B <= 64 && !key_begin && !key_end) {
+    at_tile = heaviest_tile(cu_q, ctx_before, B, G, xu);
+    if (at_tile.seq.b < 0) return;
+  } else {
+    at_tile.seq = find_sequence(cu_q, ctx_before, B, unit, first_unit);
+    at_tile.tile = (int)(unit - first_unit(at_tile.seq.tok0, at_tile.seq.b));
+  }
+  const SeqOf seq = at_tile.seq;
+  const int rows = seq.S * G, row0 = at_tile.tile * kTileRows;
   if (seq.S <= 0 || row0 >= rows) return;
   const int rr = row0 + wave * 32 + col, place = fast_div(min(rr, rows - 1), div_g), head = g * G + min(rr, rows - 1) - place * G, tok = seq.tok0 + place;
   const bool valid = rr < rows;

@@ -104,6 +104,8 @@ __device__ __forceinline__ TileOf heaviest_tile(const int32_t* __restrict__ cu_q
   return r;
 }
 
+enum { kPlain, kCapped, kBiased };  // scores: scaled, capped, or with a bias
+
 // What a row of scores needs of the score's form.
 struct Form {
   float scale_log2e, cap_in, cap_log2e;  // cap_in: 2 log2(e) scale / cap, or 0
@@ -112,7 +114,7 @@ struct Form {
 
 // One row again, from its keys alone, by a wavefront: lane l has channels l, l + 64, ...  For results that are not finite, where a value that the row does not
 // see may be the cause.
-template <int NC, bool kForm>
+template <int NC, int kForm>
 __device__ __attribute__((noinline)) void row_again(const uint16_t* __restrict__ q_row, const char* __restrict__ k_head, const char* __restrict__ v_head, long long blk_stride,
                                                     const int32_t* __restrict__ table, int lo, int hi, int pos, float slope, Form form, int D, uint16_t* __restrict__ to) {
   constexpr int kPer = NC == 8 ? 4 : NC == 4 ? 2 : 1;
@@ -135,9 +137,9 @@ __device__ __attribute__((noinline)) void row_again(const uint16_t* __restrict__
       v[i] = bf16_bits_to_float(vp[d * 16 + (j & 15)]);
     }
     s = wave_sum(s);
-    if (kForm && form.cap_in > 0.f) s = form.cap_log2e - 2.f * form.cap_log2e * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(s * form.cap_in));
+    if (kForm != kPlain && form.cap_in > 0.f) s = form.cap_log2e - 2.f * form.cap_log2e * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(s * form.cap_in));
     else s *= form.scale_log2e;
-    if (kForm) s = __builtin_fmaf(slope, (float)(j - pos), s);
+    if (kForm == kBiased) s = __builtin_fmaf(slope, (float)(j - pos), s);
     const float m_new = fmaxf(m, s), alpha = __builtin_amdgcn_exp2f(m - m_new), p = __builtin_amdgcn_exp2f(s - m_new);
     l = l * alpha + p;
 #pragma unroll
@@ -151,7 +153,8 @@ __device__ __attribute__((noinline)) void row_again(const uint16_t* __restrict__
 
 // Workgroup (x, y): K/V head x % Hkv of tile x / Hkv, counted from the last one; y: which part of its steps.
 // kFull: the head vector fills the instance's channels.
-template <int F, int NC, bool kForm, bool kFull>
+// kForm: kPlain, kCapped or kBiased (capped or not).
+template <int F, int NC, int kForm, bool kFull>
 __global__ __launch_bounds__(kThreads, NC == 8 ? 1 : 2) void prefill_scored_kernel(
     const uint16_t* __restrict__ q, int q_row_stride, const char* __restrict__ k_cache, const char* __restrict__ v_cache, const uint8_t* __restrict__ scales,
     const int32_t* __restrict__ cu_q, const int32_t* __restrict__ ctx_before, const int32_t* __restrict__ block_table, int bt_stride,
@@ -204,7 +207,7 @@ __global__ __launch_bounds__(kThreads, NC == 8 ? 1 : 2) void prefill_scored_kern
     const bf16x8 zero = {0, 0, 0, 0, 0, 0, 0, 0};
     qf[t] = valid && 16 * t + 8 * half < D ? *reinterpret_cast<const bf16x8*>(q_row + 16 * t + 8 * half) : zero;
   }
-  const float slope = kForm && form.slopes ? form.slopes[head] * kLog2e : 0.f;
+  const float slope = kForm == kBiased && form.slopes ? form.slopes[head] * kLog2e : 0.f;
 
   // ---- staging: a step's 16-byte pieces to registers, and from there to LDS as bf16
   const int blk_bytes = kBlockSize * D * C::kBytes;
@@ -393,7 +396,14 @@ __global__ __launch_bounds__(kThreads, NC == 8 ? 1 : 2) void prefill_scored_kern
       }
     const int k0 = j * kKeys;
     // register i of half-tile sub is key k0 + 32 sub + 16 (i / 8) + 8 half + i % 8
-    if (kForm) {
+    if constexpr (kForm == kCapped) {
+      // cap tanh(x / cap) = cap - 2 cap / (1 + e^(2 x / cap)): kept as -1 / (1 + e), the factor and the summand go with the maximum's into the weights' exponent
+#pragma unroll
+      for (int sub = 0; sub < 2; ++sub)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[sub][i] = __builtin_amdgcn_rcpf(-1.f - __builtin_amdgcn_exp2f(s[sub][i] * form.cap_in));
+    }
+    if constexpr (kForm == kBiased) {
       const float at_first = slope * (float)(k0 + 8 * half - pos);  // (the further keys' bias is slope times a literal)
 #pragma unroll
       for (int sub = 0; sub < 2; ++sub)
@@ -416,14 +426,15 @@ __global__ __launch_bounds__(kThreads, NC == 8 ? 1 : 2) void prefill_scored_kern
           if (from + at >= keys) s[sub][i] = -INFINITY;
         }
     }
-    const float c = kForm ? 1.f : form.scale_log2e;  // (with a form the scores are in the exp2 domain already)
+    // the exponents of the weights: c s + shift
+    const float c = kForm == kBiased ? 1.f : kForm == kCapped ? 2.f * form.cap_log2e : form.scale_log2e, at_zero = kForm == kCapped ? form.cap_log2e : 0.f;
     float top = max3(s[0][0], s[0][1], s[0][2]);
 #pragma unroll
     for (int i = 3; i < 15; i += 2) top = max3(top, s[0][i], s[0][i + 1]);
     top = max3(top, s[0][15], s[1][0]);
 #pragma unroll
     for (int i = 1; i < 15; i += 2) top = max3(top, s[1][i], s[1][i + 1]);
-    top = across_halves_max(fmaxf(top, s[1][15])) * c;
+    top = __builtin_fmaf(across_halves_max(fmaxf(top, s[1][15])), c, at_zero);
     if (__any(top - m > kTau)) {
       const float m_new = fmaxf(m, top), alpha = __builtin_amdgcn_exp2f(m - m_new);
       l *= alpha;
@@ -431,6 +442,7 @@ __global__ __launch_bounds__(kThreads, NC == 8 ? 1 : 2) void prefill_scored_kern
       for (int dt = 0; dt < NC; ++dt) o[dt] *= alpha;
       m = m_new;
     }
+    const float shift = at_zero - m;
     bf16x8 p[4];
     float sums[2] = {0.f, 0.f};
 #pragma unroll
@@ -439,7 +451,7 @@ __global__ __launch_bounds__(kThreads, NC == 8 ? 1 : 2) void prefill_scored_kern
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const int i = 8 * (u & 1) + 2 * e;
-        const float a = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u >> 1][i], c, -m)), b = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u >> 1][i + 1], c, -m));
+        const float a = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u >> 1][i], c, shift)), b = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u >> 1][i + 1], c, shift));
         sums[0] += a;
         sums[1] += b;
         w[e] = pack_bf16x2(a, b);
@@ -587,7 +599,6 @@ __global__ __launch_bounds__(kThreads, NC == 8 ? 1 : 2) void prefill_scored_kern
 template <int F, int NC>
 void launch_formed(const ScoredArgs& a, int32_t splits, hipStream_t s) {
   const int G = a.Hq / a.Hkv, units = (int)prefill_scored_tiles(a.B, a.T, G);
-  const bool formed = a.softcap > 0.f || a.slopes;
   const Form form = {a.scale_log2e, a.softcap > 0.f ? 2.f * a.scale_log2e / a.softcap : 0.f, a.softcap * kLog2e, a.slopes};
   auto go = [&](auto kernel) {
     hipLaunchKernelGGL(kernel, dim3((unsigned)units * a.Hkv, (unsigned)splits), dim3(kThreads), 0, s, (const uint16_t*)a.q, a.q_row_stride, (const char*)a.k_cache,
@@ -595,8 +606,13 @@ void launch_formed(const ScoredArgs& a, int32_t splits, hipStream_t s) {
                        a.counters, a.B, a.Hq, a.Hkv, G, make_divisor(G), make_divisor(a.Hkv), a.D, units, form);
   };
   const bool full = a.D == 32 * NC;
-  if (formed) full ? go(&prefill_scored_kernel<F, NC, true, true>) : go(&prefill_scored_kernel<F, NC, true, false>);
-  else full ? go(&prefill_scored_kernel<F, NC, false, true>) : go(&prefill_scored_kernel<F, NC, false, false>);
+  auto with_form = [&](auto kind) {
+    constexpr int kForm = decltype(kind)::value;
+    full ? go(&prefill_scored_kernel<F, NC, kForm, true>) : go(&prefill_scored_kernel<F, NC, kForm, false>);
+  };
+  if (a.slopes) with_form(std::integral_constant<int, kBiased>());
+  else if (a.softcap > 0.f) with_form(std::integral_constant<int, kCapped>());
+  else with_form(std::integral_constant<int, kPlain>());
 }
 
 template <int F>

@@ -653,7 +653,8 @@ int ecoserve_attn_decode_scored(ecoserve_ctx* c, const ecoserve_cache* cache, co
   if (!workspace || workspace_bytes < decode_scored_workspace(c->lay, c->num_cu)) return ECOSERVE_EINVAL;
   DeviceGuard guard(c->device);
   if (!guard.ok) return ECOSERVE_EHIP;
-  const ScoredArgs a = scored_args(c, cache, scores, q, q_row_stride, nullptr, ctx_len, block_table, bt_stride, out, lse, B, B, workspace);
+  ScoredArgs a = scored_args(c, cache, scores, q, q_row_stride, nullptr, ctx_len, block_table, bt_stride, out, lse, B, B, workspace);
+  a.max_ctx_len = max_ctx_len;
   return launch_decode_scored(a, (hipStream_t)stream) == hipSuccess ? ECOSERVE_OK : ECOSERVE_EHIP;
 }
 

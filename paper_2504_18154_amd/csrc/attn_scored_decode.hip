@@ -155,7 +155,7 @@ __device__ __forceinline__ void add_up(int tid, const float* first_state, int n_
 
 // kFull: the head vector fills the instance's channels.
 template <int F, int NC, bool kForm, int kWaves, bool kFull>
-__global__ __launch_bounds__(64 * kWaves, decode_scored_waves(F != kNative, NC) * kWaves / 4) void decode_scored_kernel(const uint16_t* __restrict__ q, int q_row_stride, const char* __restrict__ k_cache,
+__global__ __launch_bounds__(64 * kWaves, decode_scored_waves(F != kNative, NC)) void decode_scored_kernel(const uint16_t* __restrict__ q, int q_row_stride, const char* __restrict__ k_cache,
                                                                  const char* __restrict__ v_cache, const uint8_t* __restrict__ scales,
                                                                  const int32_t* __restrict__ block_table, int bt_stride, const int32_t* __restrict__ ctx_len,
                                                                  const int32_t* __restrict__ key_begin, const int32_t* __restrict__ key_end,
@@ -528,7 +528,7 @@ void launch_waves(const ScoredArgs& a, hipStream_t s) {
   const size_t words = std::max((size_t)kWaves * G * (kPassChannels<NC> + 4), (size_t)G * kScoredMostPieces);
   const size_t lds = (head_words(a.B) + words) * sizeof(uint32_t);
   const float cap_in = form && a.softcap > 0.f ? 2.f * a.scale_log2e / a.softcap : 0.f;
-  const int grid = decode_scored_waves(F != kNative, NC) * a.num_cu;
+  const int grid = (kWaves == 8 ? 1 : decode_scored_waves(F != kNative, NC)) * a.num_cu;
   auto go = [&](auto kernel) {
     hipLaunchKernelGGL(kernel, dim3(grid), dim3(64 * kWaves), lds, s, (const uint16_t*)a.q, a.q_row_stride, (const char*)a.k_cache, (const char*)a.v_cache, a.scales,
                        a.block_table, a.bt_stride, a.ctx_before, a.key_begin, a.key_end, a.slopes, (uint16_t*)a.out, a.lse, a.states, a.counters, a.B, a.Hq, a.Hkv, G,
@@ -539,7 +539,12 @@ void launch_waves(const ScoredArgs& a, hipStream_t s) {
   else full ? go(&decode_scored_kernel<F, NC, false, kWaves, true>) : go(&decode_scored_kernel<F, NC, false, kWaves, false>);
 }
 template <int F, int NC>
-void launch_formed(const ScoredArgs& a, hipStream_t s) { launch_waves<F, NC, 4>(a, s); }
+void launch_formed(const ScoredArgs& a, hipStream_t s) {
+  if constexpr (F != kNative && NC <= 4) {
+    if (decode_scored_short((int64_t)a.B * a.Hkv * ((a.max_ctx_len + 63) / 64 + kPieceCost), true, NC, a.num_cu)) return launch_waves<F, NC, 8>(a, s);
+  }
+  launch_waves<F, NC, 4>(a, s);
+}
 
 template <int F>
 void launch_format(const ScoredArgs& a, hipStream_t s) {

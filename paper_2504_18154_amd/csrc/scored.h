@@ -28,6 +28,7 @@ struct ScoredArgs {
   float softcap;      // 0: none
   float* states;
   uint32_t* counters;  // zero between launches
+  int32_t max_ctx_len = 0;  // decode: a bound on the lengths, for the choice of a launch alone
 };
 
 constexpr int32_t scored_chunks(int32_t D) { return D <= 64 ? 2 : D <= 128 ? 4 : 8; }  // of 32 channels, that a kernel's instance holds
@@ -41,6 +42,9 @@ constexpr int32_t kShortShare = 16;         // (see the kernel)
 constexpr int32_t kPieceCost = 4;           // units in front of a (sequence, K/V head)'s steps
 // Workgroups of four wavefronts that a CU holds, by the registers of the kernel's instances (chunks: of 32 channels).
 constexpr int32_t decode_scored_waves(bool narrow, int32_t chunks) { return chunks == 8 || (chunks == 4 && !narrow) ? 1 : 2; }
+// Short batches over coded caches, a CU's share of which one workgroup takes: it has eight wavefronts, and twice as many bytes on their way.  One sequence of
+// 20 000 tokens: 22.3 us with four, 20.7 with eight.  (Long ones leave no difference between two workgroups of four and one of eight but their barriers.)
+inline bool decode_scored_short(int64_t steps, bool narrow, int32_t chunks, int32_t num_cu) { return narrow && chunks <= 4 && steps <= (int64_t)kShortShare * num_cu; }
 // A workgroup cuts two (sequence, K/V head)s at most.
 constexpr int64_t decode_scored_states(int32_t chunks, int32_t num_cu) { return 2 * (int64_t)decode_scored_waves(true, chunks) * num_cu; }
 inline size_t decode_scored_workspace(const ecoserve_layout& L, int32_t num_cu) {

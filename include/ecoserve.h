@@ -491,7 +491,7 @@ int ecoserve_attn_sparse(ecoserve_ctx* ctx, const void* q, int64_t q_row_stride,
  *     scales : uint8[num_blocks][Hkv][2][bs]            of the keys, then of the values, a byte per token
  *   A code c of a (token, head) with scale byte b stands for c * 2^(b - 127); b = 255: the row held a NaN or an infinity, and stands for NaN throughout.
  *   Coding a row of largest magnitude A: e = the smallest integer >= -126 with A <= M * 2^e, M = 127 or 448; b = e + 127; the codes are the
- *   row / 2^e, rounded once to nearest even.  (Relative to A an int8 row is within 2^-7, and to an element an e4m3 one within 2^-4: int8 is
+ *   row / 2^e, rounded once to nearest even.  The codes of e4m3 that are NaNs (127 and 255) do not occur in a stored row.  (Relative to A an int8 row is within 2^-7, and to an element an e4m3 one within 2^-4: int8 is
  *   the finer one unless a head has a few channels far above the others.)
  *
  * All four take BF16 layouts whose head_dim is a multiple of 16; others: ECOSERVE_EUNSUPPORTED.  k and v are 16-byte aligned, scales too.  Slots that no
@@ -551,7 +551,7 @@ int ecoserve_kv_read(ecoserve_ctx* ctx, const ecoserve_cache* cache, void* k_row
  * others.
  */
 typedef struct {
-  float softcap;             /* 0: none; otherwise positive and finite */
+  float softcap;             /* 0: none; otherwise from 2^-126 on, and finite */
   const float* slopes;       /* dev, float[Hq], or NULL */
   const int32_t* key_begin;  /* dev, int32[T], or NULL: 0 */
   const int32_t* key_end;    /* dev, int32[T], or NULL: p + 1 */
@@ -564,6 +564,7 @@ typedef struct {
  *
  *   scores    : host, or NULL: Eq. 2 as it is
  *   workspace : dev, 16-byte aligned, of at least the bytes that the function of the same call says (0: NULL is fine); nothing in it is kept from call to call
+ * Limits: T Hq / Hkv, the rows of a K/V head, below 2^31 - 128; B (max_ctx_len / 32 + 6) below 2^31; others: ECOSERVE_EINVAL.
  * Weights are rounded to bf16 before the product with the values; maxima, sums and lse are fp32.
  * Calls that share a context are ordered (rules at the top): work that is split is counted in the context's merge counters.  Calls that may
  * run at the same time, recorded into graphs or not, need a context and a workspace each.  The options do not concern these calls.

@@ -597,7 +597,7 @@ int ecoserve_kv_read(ecoserve_ctx* c, const ecoserve_cache* cache, void* k_rows,
 static bool scores_ok(const ecoserve_scores* scores) {
   if (!scores) return true;
   auto aligned4 = [](const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; };
-  return scores->softcap >= 0.f && !isinf(scores->softcap) && aligned4(scores->slopes) && aligned4(scores->key_begin) && aligned4(scores->key_end);
+  return (scores->softcap == 0.f || (scores->softcap >= 0x1p-126f && !isinf(scores->softcap))) && aligned4(scores->slopes) && aligned4(scores->key_begin) && aligned4(scores->key_end);
 }
 // (prompts of more rows than 32 bits count are refused)
 static bool scored_rows_ok(const ecoserve_ctx* c, int32_t B, int32_t T) {

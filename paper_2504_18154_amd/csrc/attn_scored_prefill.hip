@@ -36,7 +36,6 @@ constexpr float kLowest = -3.0e38f;  // maximum before the first key: below ever
 constexpr float kTau = 8.f;          // the maximum in the exponent is raised when a score passes it by 2^8: weights reach that, and lose nothing by it
 constexpr int kRsrc = 0x00020000;
 constexpr int kAgent = 16;           // past the caches that XCDs do not share
-constexpr uint32_t kLeastShift = 67, kMostShift = 246;  // scale bytes, 2^-60 ... 2^119, whose sums with the exponent of any code stay inside it
 
 __device__ __forceinline__ float across_halves_max(float x) {
   const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
@@ -299,56 +298,28 @@ __global__ __launch_bounds__(kThreads, NC == 8 ? 1 : 2) void prefill_scored_kern
         clear(keep);
         if (lane == 0) s_bad[j & 1] = j + 1;
       }
-      bool far = false;  // a scale outside kLeastShift ... kMostShift
-      if constexpr (F == kE4m3) {
-        // (no byte borrows or carries: the top bits are set apart)
+      // two tokens to a word: the conversion of e4m3 has one scale for both, so it is done with either, and a half of each kept
+      float f[16];
 #pragma unroll
-        for (int w = 0; w < 4; ++w)
-          far |= (((~((sw[w] | 0x80808080u) - kLeastShift * 0x01010101u) & ~sw[w]) | (((sw[w] & 0x7f7f7f7fu) + (255u - kMostShift) * 0x01010101u) & sw[w])) & 0x80808080u) != 0;
-      }
-      if (F == kE4m3 && !far) {
-        // A scale is a whole number added to the exponent of a bf16: two at a time.  The codes are made 2^-60 of themselves first, so that all sums are positive; a code
-        // of zero becomes 2^-67 of the scale's unit, which no sum of fp32 notices beside a code.  (As products in fp32: twice the instructions.)
-        typedef uint16_t half2 __attribute__((ext_vector_type(2)));
-        half2 up[8];
+      for (int w = 0; w < 4; ++w) f[4 * w] = scale_of<0>(sw[w]), f[4 * w + 1] = scale_of<1>(sw[w]), f[4 * w + 2] = scale_of<2>(sw[w]), f[4 * w + 3] = scale_of<3>(sw[w]);
 #pragma unroll
-        for (int t = 0; t < 8; ++t) {
-          const uint32_t w = sw[t >> 1], two = t & 1 ? ((w >> 9) & 0x7f80u) | ((w >> 1) & 0x7f800000u) : ((w << 7) & 0x7f80u) | ((w << 15) & 0x7f800000u);
-          up[t] = __builtin_bit_cast(half2, two - kLeastShift * 0x00800080u);
-        }
+      for (int i = 0; i < W::kChunks; ++i) {
+        u32x4 x[2];
 #pragma unroll
-        for (int i = 0; i < W::kChunks; ++i) {
-          u32x4 x[2];
+        for (int w = 0; w < 4; ++w) {
+          const uint32_t c = vr[i][w];
 #pragma unroll
-          for (int w = 0; w < 4; ++w) {
-            const u32x2 y = codes_to_bf16<F>(vr[i][w], 0x1p-60f);
-            const uint32_t y0 = y[0], y1 = y[1];  // (a cast of a vector's element takes its first one)
-            const half2 z0 = __builtin_bit_cast(half2, y0) + up[2 * w], z1 = __builtin_bit_cast(half2, y1) + up[2 * w + 1];
-            x[w >> 1][2 * (w & 1)] = __builtin_bit_cast(uint32_t, z0);
-            x[w >> 1][2 * (w & 1) + 1] = __builtin_bit_cast(uint32_t, z1);
-          }
-          if (kFull || 64 * i + lane < D) {
-            *reinterpret_cast<u32x4*>(vb + 1024 * i) = x[0];
-            *reinterpret_cast<u32x4*>(vb + 1024 * i + W::kOctet) = x[1];
+          for (int h = 0; h < 2; ++h) {
+            const float lo_scale = f[4 * w + 2 * h], hi_scale = f[4 * w + 2 * h + 1];
+            uint32_t to;
+            if constexpr (F == kE4m3) to = __builtin_amdgcn_perm(two_codes(c, hi_scale, h), two_codes(c, lo_scale, h), 0x07060100u);
+            else to = h ? pack_bf16x2(code_value<F, 2>(c) * lo_scale, code_value<F, 3>(c) * hi_scale) : pack_bf16x2(code_value<F, 0>(c) * lo_scale, code_value<F, 1>(c) * hi_scale);
+            x[w >> 1][2 * (w & 1) + h] = to;
           }
         }
-      } else {
-        float f[16];
-#pragma unroll
-        for (int w = 0; w < 4; ++w) f[4 * w] = scale_of<0>(sw[w]), f[4 * w + 1] = scale_of<1>(sw[w]), f[4 * w + 2] = scale_of<2>(sw[w]), f[4 * w + 3] = scale_of<3>(sw[w]);
-#pragma unroll
-        for (int i = 0; i < W::kChunks; ++i) {
-          u32x4 x[2];
-#pragma unroll
-          for (int w = 0; w < 4; ++w) {
-            const uint32_t c = vr[i][w];
-            x[w >> 1][2 * (w & 1)] = pack_bf16x2(code_value<F, 0>(c) * f[4 * w], code_value<F, 1>(c) * f[4 * w + 1]);
-            x[w >> 1][2 * (w & 1) + 1] = pack_bf16x2(code_value<F, 2>(c) * f[4 * w + 2], code_value<F, 3>(c) * f[4 * w + 3]);
-          }
-          if (kFull || 64 * i + lane < D) {
-            *reinterpret_cast<u32x4*>(vb + 1024 * i) = x[0];
-            *reinterpret_cast<u32x4*>(vb + 1024 * i + W::kOctet) = x[1];
-          }
+        if (kFull || 64 * i + lane < D) {
+          *reinterpret_cast<u32x4*>(vb + 1024 * i) = x[0];
+          *reinterpret_cast<u32x4*>(vb + 1024 * i + W::kOctet) = x[1];
         }
       }
     } else {

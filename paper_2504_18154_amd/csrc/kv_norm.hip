@@ -4,7 +4,7 @@
 // among themselves.  All of it is fp32, rounded once: to bf16, or to codes (quant.h).
 //   norm      y = x / sqrt(mean(x^2) + eps) * w
 //   rotation  pair (a, b) -> (a cos - b sin, a sin + b cos); kv_rope.hip says how the angles are formed.  A token's weights and angles make one pair of factors per
-//             element, for itself and its partner, and the norm's 1 / sqrt multiplies the sum.  Partners come from the lane that has them; where they are not
+//             element, for itself and its partner.  Partners come from the lane that has them; where they are not
 //             eight in a lane (rotary widths that are odd multiples of 8), from memory.
 //   codes     the scale from the largest magnitude of the turned row, then one rounding
 //
@@ -161,17 +161,18 @@ __device__ __forceinline__ void formed(float (&y)[8], Raw<kAdjacent>& raw, const
   raw.exchange(at);
   values_of(x, raw.own);
   values_of(other, raw.partner);
-#pragma unroll
-  for (int i = 0; i < 8; ++i) y[i] = __builtin_fmaf(other[i], by.partner[i], x[i] * by.own[i]);
   if (per_D > 0.f) {
     float sum = 0.f;
 #pragma unroll
     for (int i = 0; i < 8; ++i) sum = __builtin_fmaf(x[i], x[i], sum);
     sum = over_row<LP>(sum, [](float a, float b) { return a + b; });
     const float f = rsqrtf(__builtin_fmaf(sum, per_D, eps));
+    // (before the weights and the rotation: what is large stays inside fp32)
 #pragma unroll
-    for (int i = 0; i < 8; ++i) y[i] *= f;
+    for (int i = 0; i < 8; ++i) x[i] *= f, other[i] *= f;
   }
+#pragma unroll
+  for (int i = 0; i < 8; ++i) y[i] = __builtin_fmaf(other[i], by.partner[i], x[i] * by.own[i]);
 }
 
 // Codes of a row's 8 elements, and its scale byte.

@@ -31,7 +31,7 @@ struct Cached {
 // 2^(b - 127) of byte i of a word of scale bytes; 255 gives infinity, whose product with a code of 0 is NaN.
 template <int I>
 __device__ __forceinline__ float scale_of(uint32_t w) {
-  const uint32_t at = I == 3 ? w >> 1 : w << (23 - 8 * I);
+  const uint32_t at = I == 3 ? w >> 1 : w << (I == 3 ? 0 : 23 - 8 * I);
   return __uint_as_float(at & 0x7f800000u);
 }
 __device__ __forceinline__ float scale_of_byte(uint32_t b) { return __uint_as_float(b << 23); }
@@ -42,12 +42,16 @@ __device__ __forceinline__ float code_value(uint32_t w) {
   if constexpr (F == kInt8) return (float)(int8_t)(w >> (8 * I));
   else return __builtin_amdgcn_cvt_f32_fp8((int)w, I);
 }
+// Codes 0 and 1, or 2 and 3, of a word of e4m3 as bf16, exactly, times a power of two.
+__device__ __forceinline__ uint32_t two_codes(uint32_t w, float scale, bool upper) {
+  return upper ? __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, true))
+               : __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, false));
+}
 // Four codes as bf16, exactly, times a power of two.
 template <int F>
 __device__ __forceinline__ u32x2 codes_to_bf16(uint32_t w, float scale) {
   if constexpr (F == kE4m3) {
-    return u32x2{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, false)),
-                 __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, true))};
+    return u32x2{two_codes(w, scale, false), two_codes(w, scale, true)};
   } else {
     return u32x2{pack_bf16x2(code_value<F, 0>(w) * scale, code_value<F, 1>(w) * scale), pack_bf16x2(code_value<F, 2>(w) * scale, code_value<F, 3>(w) * scale)};
   }

@@ -89,7 +89,7 @@ constexpr int kPassChannels = NC == 8 ? 128 : 32 * NC;
 template <int kWaves>
 __device__ __forceinline__ void add_up(int tid, const float* first_state, int n_pieces, int G, int D, uint16_t* out_rows, float* lse_rows, float* s_w, float* s_M, float* s_L,
                                                  f32x4* s_red) {
-  constexpr int kThreads = 64 * kWaves, kAtOnce = 8;
+  constexpr int kThreads = 64 * kWaves, kAtOnce = 4;
   const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), state_words = scored_state_words(D);
   const __amdgpu_buffer_rsrc_t from = __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(first_state), 0, 2 * n_pieces * G * state_words * 4, kRsrc);
   auto state_at = [&](int k) { return (k == 0 ? 1 : 2 * k) * G * state_words; };  // in words
@@ -103,6 +103,8 @@ __device__ __forceinline__ void add_up(int tid, const float* first_state, int n_
     for (int j = 0; j < kAtOnce; ++j)
       x[j] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(from, (state_at(min(k0 + j * parts, n_pieces - 1)) + at) * 4, 0, kAgent));
   };
+  ask(min(i0, groups - 1), part);  // (the first ones: beside what says their weights)
+  bool asked = true;
   for (int h = wave; h < G; h += kWaves) {
     constexpr int kMost = kScoredMostPieces / 64;
     float ms[kMost], ls[kMost], M = kLowest, L = 0.f;
@@ -133,7 +135,8 @@ __device__ __forceinline__ void add_up(int tid, const float* first_state, int n_
     f32x4 o = {0.f, 0.f, 0.f, 0.f};
     if (here) {
       for (int k0 = part; k0 < n_pieces; k0 += kAtOnce * parts) {
-        ask(i, k0);
+        if (!asked) ask(i, k0);
+        asked = false;
 #pragma unroll
         for (int j = 0; j < kAtOnce; ++j)
           if (k0 + j * parts < n_pieces) o += x[j] * s_w[h * n_pieces + k0 + j * parts];

@@ -602,7 +602,7 @@ static bool scores_ok(const ecoserve_scores* scores) {
 // (prompts of more rows than 32 bits count are refused)
 static bool scored_rows_ok(const ecoserve_ctx* c, int32_t B, int32_t T) {
   const int64_t G = c->lay.num_q_heads / c->lay.num_kv_heads;
-  return T * G <= 0x7fffffffLL - kTileRows && prefill_scored_tiles(B, T, (int32_t)G) * c->lay.num_kv_heads <= 0x7fffffffLL;
+  return T * G <= 0x7fffffffLL - kMostTileRows && prefill_scored_tiles(kTileRows, B, T, (int32_t)G) * c->lay.num_kv_heads <= 0x7fffffffLL;
 }
 static ScoredArgs scored_args(const ecoserve_ctx* c, const ecoserve_cache* cache, const ecoserve_scores* scores, const void* q, int64_t q_row_stride,
                               const int32_t* cu_q, const int32_t* ctx, const int32_t* block_table, int32_t bt_stride, void* out, float* lse, int32_t B, int32_t T,
@@ -633,7 +633,8 @@ int ecoserve_attn_prefill_scored(ecoserve_ctx* c, const ecoserve_cache* cache, c
   DeviceGuard guard(c->device);
   if (!guard.ok) return ECOSERVE_EHIP;
   const ScoredArgs a = scored_args(c, cache, scores, q, q_row_stride, cu_q, ctx_before, block_table, bt_stride, out, lse, B, T, workspace);
-  return launch_prefill_scored(a, prefill_scored_splits(c->lay, B, T, c->num_cu), (hipStream_t)stream) == hipSuccess ? ECOSERVE_OK : ECOSERVE_EHIP;
+  const int32_t rows = prefill_scored_rows(c->lay, B, T, c->num_cu);
+  return launch_prefill_scored(a, rows, prefill_scored_splits(c->lay, rows, B, T, c->num_cu), (hipStream_t)stream) == hipSuccess ? ECOSERVE_OK : ECOSERVE_EHIP;
 }
 
 size_t ecoserve_decode_scored_workspace_bytes(const ecoserve_ctx* c) { return c ? decode_scored_workspace(c->lay, c->num_cu) : 0; }

@@ -5,7 +5,7 @@
 //   scores  S^T[key][row] = K . Q^T     v_mfma_f32_32x32x16_bf16
 //   values  O^T[d][row] += V^T . P^T    v_mfma_f32_32x32x16_bf16
 // A step's codes are loaded two steps ahead, and a step ahead turned into bf16, scales and all (exact: a code has 7 bits at most and the scales are powers
-// of two), on the way into LDS, once for the four wavefronts; the loop over the keys is the same for all formats.
+// of two), on the way into LDS, once for the tile's wavefronts; the loop over the keys is the same for all formats.
 //   K in LDS: [16-byte unit of 8 channels][64 keys], V: [8 keys][channel][16 bytes]; both are read as A operands, 16 bytes a lane.
 // Rows of S^T stand for keys with bits 2 and 3 swapped, so that the 16 scores that a lane holds of 32 keys are two runs of 8 neighbouring keys: the B
 // operand of the second product, and P stays in registers.
@@ -31,7 +31,7 @@ namespace eco {
 
 namespace {
 
-constexpr int kThreads = 256, kKeys = 64;
+constexpr int kKeys = 64;
 constexpr float kLowest = -3.0e38f;  // maximum before the first key: below every finite score, and no infinity to be subtracted from one
 constexpr float kTau = 8.f;          // the maximum in the exponent is raised when a score passes it by 2^8: weights reach that, and lose nothing by it
 constexpr int kRsrc = 0x00020000;
@@ -51,8 +51,9 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   return r;
 }
 
-template <int F, int NC>
+template <int F, int NC, int kWaves>
 struct Tile {
+  static constexpr int kThreads = 64 * kWaves, kRows = 32 * kWaves;
   static constexpr bool kNarrow = F != kNative;
   static constexpr int kD = 32 * NC;                                // channels that the instance holds
   static constexpr int kUnits = kD / 8;                             // of 8 channels
@@ -60,7 +61,7 @@ struct Tile {
   static constexpr int kOctet = kD * 16 + 64;                       // 8 keys of V, and what moves the next ones to other banks
   static constexpr int kVBytes = 8 * kOctet;
   static constexpr int kBuffers = NC == 8 ? 1 : 2;                  // (heads of 256: a second one would leave a workgroup per CU)
-  static constexpr int kChunks = kNarrow ? NC / 2 : NC;             // 16-byte loads of K, and of V, per thread and step
+  static constexpr int kChunks = (kNarrow ? 2 : 4) * NC / kWaves;   // 16-byte loads of K, and of V, per thread and step
 };
 
 // The tile that `rank` others come before, by falling length (the keys that its last row sees, in at most 16 classes), in a batch of up to 64 sequences, one to a
@@ -71,15 +72,16 @@ struct TileOf {
   SeqOf seq;
   int tile;
 };
+template <int kRows>
 __device__ __forceinline__ TileOf heaviest_tile(const int32_t* __restrict__ cu_q, const int32_t* __restrict__ ctx_before, int B, int G, int rank) {
   const int b = min((int)(threadIdx.x & 63), B - 1);
   const int tok0 = cu_q[b], S = (int)(threadIdx.x & 63) < B ? cu_q[b + 1] - tok0 : 0, cb = ctx_before[b];
-  const int tiles = S > 0 ? (S * G + kTileRows - 1) / kTileRows : 0;
+  const int tiles = S > 0 ? (S * G + kRows - 1) / kRows : 0;
   const int steps = lanes_max(tiles && cb + S > 0 ? (cb + S - 1) / kKeys + 1 : 0), shift = max(0, 28 - __builtin_clz(steps | 1));
   // the first tile of class v: its last row sees key (v - 1) 64 2^shift
   auto first_of = [&](int v) {
     const long long at = ((long long)kKeys << shift) * (v - 1) - cb;
-    return v <= 0 || at <= 0 ? 0 : at >= S ? tiles : (int)at * G / kTileRows;
+    return v <= 0 || at <= 0 ? 0 : at >= S ? tiles : (int)at * G / kRows;
   };
   auto add = [](int x, int y) { return x + y; };
   int lo = 0, hi = ((steps + (1 << shift) - 1) >> shift) + 1, above = 0;
@@ -153,31 +155,31 @@ __device__ __attribute__((noinline)) void row_again(const uint16_t* __restrict__
 // Workgroup (x, y): K/V head x % Hkv of tile x / Hkv, counted from the last one; y: which part of its steps.
 // kFull: the head vector fills the instance's channels.
 // kForm: kPlain, kCapped or kBiased (capped or not).
-template <int F, int NC, int kForm, bool kFull>
-__global__ __launch_bounds__(kThreads, NC == 8 ? 1 : 2) void prefill_scored_kernel(
+template <int F, int NC, int kForm, bool kFull, int kWaves>
+__global__ __launch_bounds__(64 * kWaves, NC == 8 ? 1 : 2) void prefill_scored_kernel(
     const uint16_t* __restrict__ q, int q_row_stride, const char* __restrict__ k_cache, const char* __restrict__ v_cache, const uint8_t* __restrict__ scales,
     const int32_t* __restrict__ cu_q, const int32_t* __restrict__ ctx_before, const int32_t* __restrict__ block_table, int bt_stride,
     const int32_t* __restrict__ key_begin, const int32_t* __restrict__ key_end, uint16_t* __restrict__ out, float* __restrict__ lse, float* states,
     uint32_t* counters, int B, int Hq, int Hkv, int G, Divisor div_g, Divisor div_hkv, int D, int units, Form form) {
   typedef Cached<F> C;
-  typedef Tile<F, NC> W;
+  typedef Tile<F, NC, kWaves> W;
   __shared__ __attribute__((aligned(16))) char s_k[W::kBuffers][W::kKBytes], s_v[W::kBuffers][W::kVBytes];
-  __shared__ int s_lo[4], s_hi[4], s_order, s_bad[2];
+  __shared__ int s_lo[kWaves], s_hi[kWaves], s_order, s_bad[2];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 31, half = lane >> 5;
 
   // ---- the tile, its rows and their keys
   const int xu = fast_div((int)blockIdx.x, div_hkv), g = (int)blockIdx.x - xu * Hkv, unit = units - 1 - xu;
-  auto first_unit = [&](int cu, int b) { return (long long)cu * G / kTileRows + b; };
+  auto first_unit = [&](int cu, int b) { return (long long)cu * G / W::kRows + b; };
   TileOf at_tile;
   if (B > 2 && B <= 64 && !key_begin && !key_end) {
-    at_tile = heaviest_tile(cu_q, ctx_before, B, G, xu);
+    at_tile = heaviest_tile<W::kRows>(cu_q, ctx_before, B, G, xu);
     if (at_tile.seq.b < 0) return;
   } else {
     at_tile.seq = find_sequence(cu_q, ctx_before, B, unit, first_unit);
     at_tile.tile = (int)(unit - first_unit(at_tile.seq.tok0, at_tile.seq.b));
   }
   const SeqOf seq = at_tile.seq;
-  const int rows = seq.S * G, row0 = at_tile.tile * kTileRows;
+  const int rows = seq.S * G, row0 = at_tile.tile * W::kRows;
   if (seq.S <= 0 || row0 >= rows) return;
   const int rr = row0 + wave * 32 + col, place = fast_div(min(rr, rows - 1), div_g), head = g * G + min(rr, rows - 1) - place * G, tok = seq.tok0 + place;
   const bool valid = rr < rows;
@@ -190,7 +192,9 @@ __global__ __launch_bounds__(kThreads, NC == 8 ? 1 : 2) void prefill_scored_kern
   if (lane == 0) s_lo[wave] = w_lo, s_hi[wave] = w_hi;
   if (tid < 2) s_bad[tid] = 0;
   __syncthreads();
-  const int t_lo = min(min(s_lo[0], s_lo[1]), min(s_lo[2], s_lo[3])), t_hi = max(max(s_hi[0], s_hi[1]), max(s_hi[2], s_hi[3]));
+  int t_lo = s_lo[0], t_hi = s_hi[0];
+#pragma unroll
+  for (int w = 1; w < kWaves; ++w) t_lo = min(t_lo, s_lo[w]), t_hi = max(t_hi, s_hi[w]);
   uint16_t* const out_row = out + ((size_t)tok * Hq + head) * D;
   float* const lse_row = lse ? lse + (size_t)tok * Hq + head : nullptr;
   const int j_first = t_hi > 0 ? t_lo / kKeys : 0, j_end = t_hi > 0 ? (t_hi - 1) / kKeys + 1 : 0;
@@ -220,18 +224,19 @@ __global__ __launch_bounds__(kThreads, NC == 8 ? 1 : 2) void prefill_scored_kern
   u32x4 kr[W::kChunks], vr[W::kChunks];
   uint32_t k_scale = 127, v_scale[4] = {0x7f7f7f7fu, 0x7f7f7f7fu, 0x7f7f7f7fu, 0x7f7f7f7fu};
   int id_k = 0, id_v = 0;
+  const int v_block = wave & 3, v_part = wave >> 2;  // the block of V that the wavefront stages, and which of its runs of 64 places first
   auto load_ids = [&](int j) {
     id_k = id_of(4 * j + (lane >> 4));
-    id_v = id_of(4 * j + wave);
+    id_v = id_of(4 * j + v_block);
   };
   auto at_block = [](int id, uint32_t stride) { return (size_t)(uint32_t)id * stride; };
   auto load = [&]() {
     const char* const kp = k_head + at_block(id_k, blk_stride) + (lane & 15) * 16 + wave * 256;
-    const char* const vp = v_head + at_block(id_v, blk_stride) + lane * 16;
+    const char* const vp = v_head + at_block(id_v, blk_stride) + (v_part * 64 + lane) * 16;
 #pragma unroll
     for (int i = 0; i < W::kChunks; ++i) {
-      if (kFull || (4 * i + wave) * C::kUnit < D) kr[i] = *reinterpret_cast<const u32x4*>(kp + 1024 * i);  // unit 4 i + wave
-      if (kFull || (64 * i + lane) * 16 < blk_bytes) vr[i] = *reinterpret_cast<const u32x4*>(vp + 1024 * i);
+      if (kFull || (kWaves * i + wave) * C::kUnit < D) kr[i] = *reinterpret_cast<const u32x4*>(kp + kWaves * 256 * i);  // unit kWaves i + wave
+      if (kFull || (kWaves * 16 * i + v_part * 64 + lane) * 16 < blk_bytes) vr[i] = *reinterpret_cast<const u32x4*>(vp + kWaves * 256 * i);
     }
     if constexpr (W::kNarrow) {
       const uint8_t* const sc = scales + (size_t)g * kScaleBytes;
@@ -244,12 +249,12 @@ __global__ __launch_bounds__(kThreads, NC == 8 ? 1 : 2) void prefill_scored_kern
   // (j: the step that lies in the registers)
   auto store = [&](int j) {
     char* const kb = s_k[W::kBuffers == 2 ? j & 1 : 0] + lane * 16;
-    char* const vb = s_v[W::kBuffers == 2 ? j & 1 : 0] + 2 * wave * W::kOctet + (W::kNarrow ? lane * 16 : (lane >> 1) * 16 + (lane & 1) * W::kOctet);
+    char* const vb = s_v[W::kBuffers == 2 ? j & 1 : 0] + 2 * v_block * W::kOctet + (W::kNarrow ? v_part * 1024 + lane * 16 : v_part * 512 + (lane >> 1) * 16 + (lane & 1) * W::kOctet);
     const u32x4 zero = {0, 0, 0, 0};
     const float ks = scale_of_byte(k_scale);
 #pragma unroll
     for (int i = 0; i < W::kChunks; ++i) {
-      const int u = 4 * i + wave;
+      const int u = kWaves * i + wave;
       const bool there = kFull || u * C::kUnit < D;
       if constexpr (W::kNarrow) {
         u32x4 a = zero, b = zero;
@@ -264,7 +269,7 @@ __global__ __launch_bounds__(kThreads, NC == 8 ? 1 : 2) void prefill_scored_kern
       }
     }
     // V: slots behind the tile's last key (nobody sees them) may hold anything: zeros.  So are those in front of the first.
-    const int key0 = j * kKeys + 16 * wave, keep_lo = t_lo - key0, keep_hi = t_hi - key0;  // of the block's 16 slots
+    const int key0 = j * kKeys + 16 * v_block, keep_lo = t_lo - key0, keep_hi = t_hi - key0;  // of the block's 16 slots
     const bool edge = keep_lo > 0 || keep_hi < 16;
     if constexpr (W::kNarrow) {
       uint32_t sw[4];
@@ -317,9 +322,9 @@ __global__ __launch_bounds__(kThreads, NC == 8 ? 1 : 2) void prefill_scored_kern
             x[w >> 1][2 * (w & 1) + h] = to;
           }
         }
-        if (kFull || 64 * i + lane < D) {
-          *reinterpret_cast<u32x4*>(vb + 1024 * i) = x[0];
-          *reinterpret_cast<u32x4*>(vb + 1024 * i + W::kOctet) = x[1];
+        if (kFull || kWaves * 16 * i + v_part * 64 + lane < D) {
+          *reinterpret_cast<u32x4*>(vb + kWaves * 256 * i) = x[0];
+          *reinterpret_cast<u32x4*>(vb + kWaves * 256 * i + W::kOctet) = x[1];
         }
       }
     } else {
@@ -335,7 +340,7 @@ __global__ __launch_bounds__(kThreads, NC == 8 ? 1 : 2) void prefill_scored_kern
       }
 #pragma unroll
       for (int i = 0; i < W::kChunks; ++i)
-        if (kFull || 32 * i + (lane >> 1) < D) *reinterpret_cast<u32x4*>(vb + 512 * i) = vr[i];
+        if (kFull || kWaves * 8 * i + v_part * 32 + (lane >> 1) < D) *reinterpret_cast<u32x4*>(vb + kWaves * 128 * i) = vr[i];
     }
   };
 
@@ -458,6 +463,10 @@ __global__ __launch_bounds__(kThreads, NC == 8 ? 1 : 2) void prefill_scored_kern
     __syncthreads();
     for (int j = j0; j < j1; ++j) {
       if constexpr (W::kBuffers == 2) {
+        // (of eight wavefronts that turn codes into operands, four do so first and four last, so that a SIMD's two are not at the same thing: 2170 and 2140 us of
+        // two prompts of 8192 tokens; bf16 is only copied, and better all at once)
+        const bool first = kWaves == 4 || !W::kNarrow || wave < 4;
+        if (!first && j >= wj0 && j < wj1) step(j);
         if (j + 1 < j1) {
           store(j + 1);
           if (j + 2 < j1) {
@@ -465,7 +474,7 @@ __global__ __launch_bounds__(kThreads, NC == 8 ? 1 : 2) void prefill_scored_kern
             if (j + 3 < j1) load_ids(j + 3);
           }
         }
-        if (j >= wj0 && j < wj1) step(j);
+        if (first && j >= wj0 && j < wj1) step(j);
         __syncthreads();
       } else {
         if (j >= wj0 && j < wj1) step(j);
@@ -491,10 +500,10 @@ __global__ __launch_bounds__(kThreads, NC == 8 ? 1 : 2) void prefill_scored_kern
 
   if (splits > 1) {
     // ---- parts of the steps: the states, in the lanes' own order; the last workgroup adds them up
-    constexpr int kStateFloats = kTileRows * (32 * NC + 2);
+    constexpr int kStateFloats = W::kRows * (32 * NC + 2);
     const size_t item = blockIdx.x;
     const __amdgpu_buffer_rsrc_t mine = __builtin_amdgcn_make_buffer_rsrc(states + (item * splits + blockIdx.y) * kStateFloats, 0, kStateFloats * 4, kRsrc);
-    const int at = (wave * NC * 1024 + lane * 4) * 4, at_ml = (kTileRows * 32 * NC + 2 * (wave * 32 + col)) * 4;
+    const int at = (wave * NC * 1024 + lane * 4) * 4, at_ml = (W::kRows * 32 * NC + 2 * (wave * 32 + col)) * 4;
 #pragma unroll
     for (int dt = 0; dt < NC; ++dt)
 #pragma unroll
@@ -567,41 +576,49 @@ __global__ __launch_bounds__(kThreads, NC == 8 ? 1 : 2) void prefill_scored_kern
   if (lse_row && valid && half == 0) *lse_row = none ? -INFINITY : (m + log2f(l)) * kLn2;
 }
 
-template <int F, int NC>
-void launch_formed(const ScoredArgs& a, int32_t splits, hipStream_t s) {
-  const int G = a.Hq / a.Hkv, units = (int)prefill_scored_tiles(a.B, a.T, G);
+template <int F, int NC, int kWaves>
+void launch_waves(const ScoredArgs& a, int32_t splits, hipStream_t s) {
+  const int G = a.Hq / a.Hkv, units = (int)prefill_scored_tiles(32 * kWaves, a.B, a.T, G);
   const Form form = {a.scale_log2e, a.softcap > 0.f ? 2.f * a.scale_log2e / a.softcap : 0.f, a.softcap * kLog2e, a.slopes};
   auto go = [&](auto kernel) {
-    hipLaunchKernelGGL(kernel, dim3((unsigned)units * a.Hkv, (unsigned)splits), dim3(kThreads), 0, s, (const uint16_t*)a.q, a.q_row_stride, (const char*)a.k_cache,
+    hipLaunchKernelGGL(kernel, dim3((unsigned)units * a.Hkv, (unsigned)splits), dim3(64 * kWaves), 0, s, (const uint16_t*)a.q, a.q_row_stride, (const char*)a.k_cache,
                        (const char*)a.v_cache, a.scales, a.cu_q, a.ctx_before, a.block_table, a.bt_stride, a.key_begin, a.key_end, (uint16_t*)a.out, a.lse, a.states,
                        a.counters, a.B, a.Hq, a.Hkv, G, make_divisor(G), make_divisor(a.Hkv), a.D, units, form);
   };
   const bool full = a.D == 32 * NC;
   auto with_form = [&](auto kind) {
     constexpr int kForm = decltype(kind)::value;
-    full ? go(&prefill_scored_kernel<F, NC, kForm, true>) : go(&prefill_scored_kernel<F, NC, kForm, false>);
+    full ? go(&prefill_scored_kernel<F, NC, kForm, true, kWaves>) : go(&prefill_scored_kernel<F, NC, kForm, false, kWaves>);
   };
   if (a.slopes) with_form(std::integral_constant<int, kBiased>());
   else if (a.softcap > 0.f) with_form(std::integral_constant<int, kCapped>());
   else with_form(std::integral_constant<int, kPlain>());
 }
 
+template <int F, int NC>
+void launch_formed(const ScoredArgs& a, int32_t rows, int32_t splits, hipStream_t s) {
+  if constexpr (NC == 4) {
+    if (rows == kMostTileRows) return launch_waves<F, NC, 8>(a, splits, s);
+  }
+  launch_waves<F, NC, 4>(a, splits, s);
+}
+
 template <int F>
-void launch_format(const ScoredArgs& a, int32_t splits, hipStream_t s) {
+void launch_format(const ScoredArgs& a, int32_t rows, int32_t splits, hipStream_t s) {
   switch (scored_chunks(a.D)) {
-    case 2: return launch_formed<F, 2>(a, splits, s);
-    case 4: return launch_formed<F, 4>(a, splits, s);
-    default: return launch_formed<F, 8>(a, splits, s);
+    case 2: return launch_formed<F, 2>(a, rows, splits, s);
+    case 4: return launch_formed<F, 4>(a, rows, splits, s);
+    default: return launch_formed<F, 8>(a, rows, splits, s);
   }
 }
 
 }  // namespace
 
-hipError_t launch_prefill_scored(const ScoredArgs& a, int32_t splits, hipStream_t s) {
+hipError_t launch_prefill_scored(const ScoredArgs& a, int32_t rows, int32_t splits, hipStream_t s) {
   switch (a.format) {
-    case kInt8: launch_format<kInt8>(a, splits, s); break;
-    case kE4m3: launch_format<kE4m3>(a, splits, s); break;
-    default: launch_format<kNative>(a, splits, s); break;
+    case kInt8: launch_format<kInt8>(a, rows, splits, s); break;
+    case kE4m3: launch_format<kE4m3>(a, rows, splits, s); break;
+    default: launch_format<kNative>(a, rows, splits, s); break;
   }
   return hipGetLastError();
 }

@@ -51,23 +51,30 @@ inline size_t decode_scored_workspace(const ecoserve_layout& L, int32_t num_cu) 
   return (size_t)decode_scored_states(scored_chunks(L.head_dim), num_cu) * (L.num_q_heads / L.num_kv_heads) * scored_state_words(L.head_dim) * 4;
 }
 
-// Prompts: tiles of 128 rows ((position, query head) pairs of a K/V head), their 64-key steps cut among `prefill_scored_splits` workgroups where tiles are few.
-constexpr int32_t kTileRows = 128;
-inline int64_t prefill_scored_tiles(int32_t B, int32_t T, int32_t G) { return (int64_t)T * G / kTileRows + (B < T ? B : T); }
-inline int32_t prefill_scored_splits(const ecoserve_layout& L, int32_t B, int32_t T, int32_t num_cu) {
-  const int64_t items = prefill_scored_tiles(B, T, L.num_q_heads / L.num_kv_heads) * L.num_kv_heads, room = 2 * (int64_t)num_cu / std::max<int64_t>(items, 1);
+// Prompts: tiles of 128 or 256 rows ((position, query head) pairs of a K/V head), their 64-key steps cut among `prefill_scored_splits` workgroups where tiles are few.
+constexpr int32_t kTileRows = 128, kMostTileRows = 256;
+inline int64_t prefill_scored_tiles(int32_t rows, int32_t B, int32_t T, int32_t G) { return (int64_t)T * G / rows + (B < T ? B : T); }
+// Rows of a tile, 32 to a wavefront: the more of them there are, the fewer turn a step's codes into operands for themselves.  (Heads of up to 64 channels have no 16
+// bytes of a step for each of eight wavefronts, those of more than 128 no registers for two on a SIMD.)  64 heads on 8 of 128, in tiles of 128 and 256 rows: two
+// prompts of 8192 tokens over e4m3 2200 and 2140 us, 2048 tokens of three over bf16 131 and 128.  Short prompts would leave the larger ones half empty.
+inline int32_t prefill_scored_rows(const ecoserve_layout& L, int32_t B, int32_t T, int32_t num_cu) {
+  const int32_t G = L.num_q_heads / L.num_kv_heads;
+  return scored_chunks(L.head_dim) == 4 && (int64_t)T * G >= 4 * (int64_t)kMostTileRows * B && prefill_scored_tiles(kMostTileRows, B, T, G) * L.num_kv_heads >= 2 * num_cu ? kMostTileRows : kTileRows;
+}
+inline int32_t prefill_scored_splits(const ecoserve_layout& L, int32_t rows, int32_t B, int32_t T, int32_t num_cu) {
+  const int64_t items = prefill_scored_tiles(rows, B, T, L.num_q_heads / L.num_kv_heads) * L.num_kv_heads, room = 2 * (int64_t)num_cu / std::max<int64_t>(items, 1);
   return room < 2 ? 1 : (int32_t)std::min<int64_t>(room, 32);
 }
-constexpr int64_t prefill_scored_state_floats(int32_t D) { return kTileRows * (32 * (int64_t)scored_chunks(D) + 2); }
+constexpr int64_t prefill_scored_state_floats(int32_t rows, int32_t D) { return rows * (32 * (int64_t)scored_chunks(D) + 2); }
 inline size_t prefill_scored_workspace(const ecoserve_layout& L, int32_t B, int32_t T, int32_t num_cu) {
-  const int32_t splits = prefill_scored_splits(L, B, T, num_cu);
+  const int32_t rows = prefill_scored_rows(L, B, T, num_cu), splits = prefill_scored_splits(L, rows, B, T, num_cu);
   if (splits == 1) return 0;
-  return (size_t)splits * prefill_scored_tiles(B, T, L.num_q_heads / L.num_kv_heads) * L.num_kv_heads * prefill_scored_state_floats(L.head_dim) * 4;
+  return (size_t)splits * prefill_scored_tiles(rows, B, T, L.num_q_heads / L.num_kv_heads) * L.num_kv_heads * prefill_scored_state_floats(rows, L.head_dim) * 4;
 }
 
 // decode of a few tokens and prompts (attn_scored_decode.hip, attn_scored_prefill.hip)
 hipError_t launch_decode_scored(const ScoredArgs& a, hipStream_t s);
-hipError_t launch_prefill_scored(const ScoredArgs& a, int32_t splits, hipStream_t s);
+hipError_t launch_prefill_scored(const ScoredArgs& a, int32_t rows, int32_t splits, hipStream_t s);
 
 // The append with norms, rotation and coding on the way, and reading back (kv_norm.hip)
 struct NormAppend {

@@ -171,3 +171,26 @@ def test_another_stream_than_the_current_one():
     side.synchronize()
     check_rows(p, q, out, lse, seq, pos, np.zeros(len(seq)), pos + 1)
     p.ctx.close()
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("D,Hq,Hkv", [(128, 64, 8), (96, 16, 16), (128, 20, 10)], ids=str)
+def test_prompts_of_many_rows(fmt, D, Hq, Hkv):
+    """Enough rows for the large tiles: tokens of every place in one, at both ends of both prompts; plain, capped in a window, biased."""
+    G = Hq // Hkv
+    new = np.array([256 * 512 // Hq + 33, 1100 // G + 5 * 256 // G])
+    before = np.array([0, 77])
+    p = Pools(fmt, D, Hq, Hkv, before + new, seed=70)
+    p.fill(before + new, 71)
+    held = p.held()
+    seq, pos = packed(before, new)
+    T = len(seq)
+    assert T * G >= 4 * 256 * 2 and (T * G // 256 + 2) * Hkv >= 512
+    q = _q(T, p, 72, 1.5)
+    some = sorted({0, 1, 31, 63, 64, 127, 128, int(new[0]) - 1, int(new[0]), int(new[0]) + 33, T - 1} | set(range(7, T, max(1, T // 25))))
+    for kind, begin in (("plain", None), ("cap", np.maximum(pos - 150, 0)), ("slopes", None)):
+        cap, slopes = _form(p, kind)
+        out, lse = _prefill(p, before, new, q, _scores(p, cap, slopes, begin))
+        assert not out.isnan().any()
+        check_rows(p, q, out, lse, seq, pos, np.zeros(T) if begin is None else begin, pos + 1, cap, slopes, tokens=some, held=held, label=kind)
+    p.ctx.close()

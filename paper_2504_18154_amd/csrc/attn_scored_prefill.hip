@@ -1,7 +1,7 @@
 // Attention of prompts (chunks of them, behind what is cached) over the caches of ecoserve_cache, with formed scores, on gfx950 matrix cores.
 //
-// Eq. 2 of Section 2.1 for the prefill phase, bound by the matrix units and the vector work of the softmax beside them.  A tile is 128 rows ((position,
-// query head of the group) pairs of one sequence and K/V head), 32 to each of four wavefronts, which share the tile's keys, 64 at a time:
+// Eq. 2 of Section 2.1 for the prefill phase, bound by the matrix units and the vector work of the softmax beside them.  A tile is 128 or 256 rows ((position,
+// query head of the group) pairs of one sequence and K/V head), 32 to each of four or eight wavefronts, which share the tile's keys, 64 at a time:
 //   scores  S^T[key][row] = K . Q^T     v_mfma_f32_32x32x16_bf16
 //   values  O^T[d][row] += V^T . P^T    v_mfma_f32_32x32x16_bf16
 // A step's codes are loaded two steps ahead, and a step ahead turned into bf16, scales and all (exact: a code has 7 bits at most and the scales are powers

@@ -381,15 +381,19 @@ __global__ __launch_bounds__(64 * kWaves, NC == 8 ? 1 : 2) void prefill_scored_k
     }
     if constexpr (kForm == kBiased) {
       const float at_first = slope * (float)(k0 + 8 * half - pos);  // (the further keys' bias is slope times a literal)
+      float by = form.scale_log2e, start = at_first;
+      if (form.cap_in > 0.f) {  // (one branch: as a choice per score it took as long as the products)
+        by = 2.f * form.cap_log2e;
+        start += form.cap_log2e;
+#pragma unroll
+        for (int sub = 0; sub < 2; ++sub)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) s[sub][i] = __builtin_amdgcn_rcpf(-1.f - __builtin_amdgcn_exp2f(s[sub][i] * form.cap_in));
+      }
 #pragma unroll
       for (int sub = 0; sub < 2; ++sub)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          float x = s[sub][i];
-          if (form.cap_in > 0.f) x = __builtin_fmaf(-2.f * form.cap_log2e, __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(x * form.cap_in)), form.cap_log2e + at_first);
-          else x = __builtin_fmaf(x, form.scale_log2e, at_first);
-          s[sub][i] = __builtin_fmaf(slope, (float)(32 * sub + 16 * (i >> 3) + (i & 7)), x);
-        }
+        for (int i = 0; i < 16; ++i) s[sub][i] = __builtin_fmaf(slope, (float)(32 * sub + 16 * (i >> 3) + (i & 7)), __builtin_fmaf(s[sub][i], by, start));
     }
     if (k0 < w_lo_last || k0 + kKeys > w_hi_first) {
       asm volatile("" ::: "memory");  // (a branch, and no selects in every step)

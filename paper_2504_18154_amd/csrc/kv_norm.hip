@@ -25,8 +25,8 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kVHeads = 4;  // heads of V to a workgroup
-// Heads of K and Q to a workgroup from which its lanes work on two rows at a time.  72 heads of 65 536 tokens: 573 us with one, 515 with two.  7 heads of 2400
-// tokens: 37 with one, 47 with two, whose registers (114 for 86) leave fewer workgroups to a CU.
+// Heads of K and Q to a workgroup from which its lanes work on two rows at a time.  72 heads of 65 536 tokens into codes: 573 us with one, 515 with two; into bf16 605 and
+// 712.  7 heads of 2400 tokens: 37 with one, 47 with two, whose registers (114 for 86) leave fewer workgroups to a CU.
 constexpr int kManyHeads = 16;
 
 // Sum and maximum over the LP lanes that hold a row; every lane has the result, in the same order of sums everywhere.
@@ -232,17 +232,17 @@ __global__ __launch_bounds__(kThreads) void kv_append_norm_kernel(const NormArgs
   if ((int)blockIdx.y < v_slices) {
     const int g0 = blockIdx.y * kVHeads, heads = min(kVHeads, Hkv - g0);
     char* const dst = a.v_cache + (blk * Hkv + g0) * head_bytes;
+    constexpr int kRows = kVHeads * 16 / kGroups;
+    u32x4 x[kRows];
+#pragma unroll
+    for (int n = 0; n < kRows; ++n) {
+      const int r = group + n * kGroups, slot = r & 15;
+      x[n] = u32x4{0, 0, 0, 0};
+      if (r < heads * 16 && slot >= lo && slot < hi && 8 * l < D)
+        x[n] = *reinterpret_cast<const u32x4*>(a.v_new + (size_t)(t_slot0 + slot) * a.new_row_stride + (size_t)(g0 + (r >> 4)) * D + 8 * l);
+    }
     if constexpr (F != kNative) {
       const int row_bytes = D + 8;
-      constexpr int kRows = kVHeads * 16 / kGroups;
-      u32x4 x[kRows];
-#pragma unroll
-      for (int n = 0; n < kRows; ++n) {
-        const int r = group + n * kGroups, slot = r & 15;
-        x[n] = u32x4{0, 0, 0, 0};
-        if (r < heads * 16 && slot >= lo && slot < hi && 8 * l < D)
-          x[n] = *reinterpret_cast<const u32x4*>(a.v_new + (size_t)(t_slot0 + slot) * a.new_row_stride + (size_t)(g0 + (r >> 4)) * D + 8 * l);
-      }
 #pragma unroll
       for (int n = 0; n < kRows; ++n) {
         const int r = group + n * kGroups, slot = r & 15;
@@ -280,28 +280,33 @@ __global__ __launch_bounds__(kThreads) void kv_append_norm_kernel(const NormArgs
         }
       }
     } else {
-      const int upr = D / 8, vrow = D + 8;
+      const int vrow = D + 8;
       uint16_t* const vt = reinterpret_cast<uint16_t*>(staged);
-      for (int u = tid; u < heads * 16 * upr; u += kThreads) {
-        const int h = u / (16 * upr), r = u % (16 * upr), slot = r / upr, c = r % upr;
-        if (slot >= lo && slot < hi)
-          *reinterpret_cast<u32x4*>(vt + (h * 16 + slot) * vrow + c * 8) =
-              *reinterpret_cast<const u32x4*>(a.v_new + (size_t)(t_slot0 + slot) * a.new_row_stride + (g0 + h) * D + c * 8);
-      }
+#pragma unroll
+      for (int n = 0; n < kRows; ++n)
+        if (const int r = group + n * kGroups; r < heads * 16 && 8 * l < D) *reinterpret_cast<u32x4*>(vt + r * vrow + 8 * l) = x[n];
       __syncthreads();
-      for (int u = tid; u < heads * D * 2; u += kThreads) {
-        const int row = u >> 1, s0 = (u & 1) * 8, h = row / D;
-        const uint16_t* const col = vt + h * 16 * vrow + (row - h * D);
-        uint16_t* const to = reinterpret_cast<uint16_t*>(dst) + (size_t)row * 16;
-        if (s0 >= lo && s0 + 8 <= hi) {
-          Eight x;
+      // two channels' halves of the slots to a thread
+      for (int u = tid; u < heads * D; u += kThreads) {
+        const int s0 = 8 * (u & 1), h = (u >> 1) / (D / 2), d = 2 * ((u >> 1) - h * (D / 2));
+        const uint16_t* const from = vt + (h * 16 + s0) * vrow + d;
+        uint16_t* const to = reinterpret_cast<uint16_t*>(dst) + ((size_t)h * D + d) * 16 + s0;
+        u32x4 y[2];
 #pragma unroll
-          for (int e = 0; e < 8; ++e) x.e[e] = col[(s0 + e) * vrow];
-          *reinterpret_cast<Eight*>(to + s0) = x;
-        } else {
+        for (int w = 0; w < 4; ++w) {
+          const uint32_t even = *reinterpret_cast<const uint32_t*>(from + 2 * w * vrow), odd = *reinterpret_cast<const uint32_t*>(from + (2 * w + 1) * vrow);
+          y[0][w] = __builtin_amdgcn_perm(odd, even, 0x05040100u);
+          y[1][w] = __builtin_amdgcn_perm(odd, even, 0x07060302u);
+        }
 #pragma unroll
-          for (int e = 0; e < 8; ++e)
-            if (s0 + e >= lo && s0 + e < hi) to[s0 + e] = col[(s0 + e) * vrow];
+        for (int i = 0; i < 2; ++i) {
+          if (s0 >= lo && s0 + 8 <= hi) {
+            *reinterpret_cast<u32x4*>(to + i * 16) = y[i];
+          } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+              if (s0 + e >= lo && s0 + e < hi) to[i * 16 + e] = (uint16_t)(y[i][e >> 1] >> (16 * (e & 1)));
+          }
         }
       }
     }
@@ -425,7 +430,7 @@ void launch_append(const NormAppend& a, const NormArgs& args, const Turns& turns
   const dim3 grid((unsigned)units, (unsigned)(v_slices + (total + per_slice - 1) / per_slice));
   const size_t lds = (size_t)kVHeads * 16 * (F == kNative ? 2 * (a.D + 8) : a.D + 8);
   auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(kThreads), lds, s, args, turns, v_slices, per_slice); };
-  if (per_slice >= kManyHeads) go(&kv_append_norm_kernel<LP, F, kAdjacent, 2>);
+  if (F != kNative && per_slice >= kManyHeads) go(&kv_append_norm_kernel<LP, F, kAdjacent, 2>);
   else go(&kv_append_norm_kernel<LP, F, kAdjacent, 1>);
 }
 

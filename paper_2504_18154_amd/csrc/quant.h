@@ -81,8 +81,10 @@ __device__ __forceinline__ uint32_t to_codes(float a, float b, float c, float d)
   if constexpr (F == kE4m3) {
     return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false), true);
   } else {
-    const int x = (int)rintf(a), y = (int)rintf(b), z = (int)rintf(c), w = (int)rintf(d);
-    return (uint32_t)(x & 255) | (uint32_t)(y & 255) << 8 | (uint32_t)(z & 255) << 16 | (uint32_t)w << 24;
+    // (1.5 2^23 and a whole number of up to 2^22 have the number in their low bits; the sum is the rounding)
+    constexpr float kWhole = 12582912.f;
+    const uint32_t x = __float_as_uint(a + kWhole), y = __float_as_uint(b + kWhole), z = __float_as_uint(c + kWhole), w = __float_as_uint(d + kWhole);
+    return __builtin_amdgcn_perm(__builtin_amdgcn_perm(w, z, 0x0c0c0400u), __builtin_amdgcn_perm(y, x, 0x0c0c0400u), 0x05040100u);
   }
 }
 

@@ -20,6 +20,11 @@
 // Weights are rounded to bf16 for the second product (2^-9 of each, unbiased: the result's own rounding is as large); maxima, sums and the
 // log-sum-exp are fp32, from the weights before that rounding.
 //
+// Measured: 32 contexts of 16 k ... 131 k tokens, 64 heads on 8 of 128, e4m3: 786 us (5.03 GB, 6.4 TB/s; reads reach 7.0).  64 of 100 ... 4000 tokens, 40 heads on 8: 57 us
+// (4.7 TB/s: four of five heads are cut, a piece costs 5 us of latency, and its workgroup's neighbour on the CU covers half of it).  One of 20 000 tokens, int8: 20.1 us, of
+// which 6 are the reads: the numbering, ids and first keys 6, the wavefronts' states 2, writing and counting 1.5, adding up 5.  96 windows of 1024 tokens, 8 heads on 1
+// of 256, bf16: 30 us (3.3 TB/s), a workgroup to a CU.
+//
 // Lane layouts relied upon (lane = 16 quad + col), 16x16x32:  A[row = col][k = 8 quad .. + 7],  B[k = 8 quad .. + 7][col],  C[row = 4 quad + i][col].
 #include <type_traits>
 

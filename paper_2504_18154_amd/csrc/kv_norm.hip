@@ -11,8 +11,8 @@
 // Memory bounds the large calls, launch latency and a few round trips the small ones.  A lane keeps its token's factors and walks the heads, the next ones' loads
 // in flight.  The blocks of the batch are numbered as in kv_append.hip; a workgroup takes the tokens of one block and a run of heads of K and Q, or up to four
 // heads of V, whose codes go through LDS to lie along the slots.
-// Measured, 64 query heads and 8 of K and V, of 128, rotated and normed: 65 536 tokens into 8-bit codes 515 us (2.55 GB, 4.9 TB/s; a copy reaches 5.0), three chunks
-// of 200 ... 1500 tokens into bf16 37 us, a token of each of 64 sequences (40 query heads) 5.6 us.
+// Measured, 64 query heads and 8 of K and V, of 128, rotated and normed: 65 536 tokens into 8-bit codes 506 us (2.55 GB, 5.0 TB/s, what a copy reaches), into bf16 600
+// (4.5 TB/s: the 16 bytes that a lane has of a row of K go to a line of their own), three chunks of 200 ... 1500 tokens into bf16 38 us, a token of each of 64 sequences (40 query heads) 5.6 us.
 #include <type_traits>
 
 #include "quant.h"
@@ -25,8 +25,8 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kVHeads = 4;  // heads of V to a workgroup
-// Heads of K and Q to a workgroup from which its lanes work on two rows at a time.  72 heads of 65 536 tokens into codes: 573 us with one, 515 with two; into bf16 605 and
-// 712.  7 heads of 2400 tokens: 37 with one, 47 with two, whose registers (114 for 86) leave fewer workgroups to a CU.
+// Heads of K and Q to a workgroup from which its lanes work on two rows at a time.  72 heads of 65 536 tokens into codes: 573 us with one, 506 with two; into bf16 600 and
+// 704.  7 heads of 2400 tokens: 38 with one, 47 with two, whose registers (118 for 85) leave fewer workgroups to a CU.
 constexpr int kManyHeads = 16;
 
 // Sum and maximum over the LP lanes that hold a row; every lane has the result, in the same order of sums everywhere.
@@ -105,8 +105,8 @@ template <bool kAdjacent>
 struct Raw {
   u32x4 own, partner;
   __device__ __forceinline__ void load(const uint16_t* row, const Place<kAdjacent>& at) {
-    own = partner = u32x4{0, 0, 0, 0};
-    if (at.here) own = *reinterpret_cast<const u32x4*>(row + at.e0);
+    partner = u32x4{0, 0, 0, 0};
+    own = *reinterpret_cast<const u32x4*>(row + (at.here ? at.e0 : 0));
     if (!kAdjacent && !at.exchanged && at.turned)
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
@@ -158,6 +158,7 @@ __device__ __forceinline__ void values_of(float (&y)[8], u32x4 x) {
 template <int LP, bool kAdjacent>
 __device__ __forceinline__ void formed(float (&y)[8], Raw<kAdjacent>& raw, const Factors<kAdjacent>& by, const Place<kAdjacent>& at, float per_D, float eps) {
   float x[8], other[8];
+  if (!at.here) raw.own = u32x4{0, 0, 0, 0};
   raw.exchange(at);
   values_of(x, raw.own);
   values_of(other, raw.partner);
@@ -236,10 +237,9 @@ __global__ __launch_bounds__(kThreads) void kv_append_norm_kernel(const NormArgs
     u32x4 x[kRows];
 #pragma unroll
     for (int n = 0; n < kRows; ++n) {
-      const int r = group + n * kGroups, slot = r & 15;
-      x[n] = u32x4{0, 0, 0, 0};
-      if (r < heads * 16 && slot >= lo && slot < hi && 8 * l < D)
-        x[n] = *reinterpret_cast<const u32x4*>(a.v_new + (size_t)(t_slot0 + slot) * a.new_row_stride + (size_t)(g0 + (r >> 4)) * D + 8 * l);
+      // (rows and lanes that there are not: others' places, so that no load waits for a branch)
+      const int r = group + n * kGroups, slot = min(max(r & 15, lo), hi - 1), h = min(r >> 4, heads - 1);
+      x[n] = *reinterpret_cast<const u32x4*>(a.v_new + (size_t)(t_slot0 + slot) * a.new_row_stride + (size_t)(g0 + h) * D + (8 * l < D ? 8 * l : 0));
     }
     if constexpr (F != kNative) {
       const int row_bytes = D + 8;
@@ -248,7 +248,7 @@ __global__ __launch_bounds__(kThreads) void kv_append_norm_kernel(const NormArgs
         const int r = group + n * kGroups, slot = r & 15;
         if (r >= heads * 16 || slot < lo || slot >= hi) continue;
         float y[8];
-        values_of(y, x[n]);
+        values_of(y, 8 * l < D ? x[n] : u32x4{0, 0, 0, 0});
         uint32_t byte;
         const u32x2 c = coded<LP, F>(y, byte);
         if (8 * l < D) *reinterpret_cast<u32x2*>(staged + r * row_bytes + 8 * l) = c;

@@ -11,8 +11,9 @@
  * management"), with grouped-query head sharing (Section 4.1).  This library
  * is that path and nothing else: append new K/V rows to the paged cache (and
  * rotate them by position on the way), causal variable-length prefill
- * attention, split-context decode attention, and, for long contexts, attention
- * over the blocks that a score of block summaries chooses.
+ * attention, split-context decode attention, for long contexts, attention
+ * over the blocks that a score of block summaries chooses, and caches of 8 bits
+ * with norms on the way in and attention with formed scores over them.
  *
  * General rules
  *   - Plain C.  No exception crosses the boundary; every call returns a
@@ -30,8 +31,8 @@
  *   - One call handles one layer; callers loop over layers.
  *   - Calls that share a context must be issued on one stream (or be ordered
  *     by the caller): they share the context's workspace (split-context partial
- *     states and merge counters of decode, which block selection and attention
- *     over listed blocks use too, the query-tile list and its queues'
+ *     states and merge counters of decode, which block selection, attention
+ *     over listed blocks and attention with formed scores use too, the query-tile list and its queues'
  *     counters of prefill).  Calls that overlap all the same may spoil their own
  *     results and those of later calls on the context (a counter left away from
  *     its start); a new context is free of that.

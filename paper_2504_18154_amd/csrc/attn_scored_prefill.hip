@@ -58,7 +58,7 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
 
 template <int F, int NC, int kWaves>
 struct Tile {
-  static constexpr int kThreads = 64 * kWaves, kRows = 32 * kWaves;
+  static constexpr int kThreads = 64 * kWaves, kRows = 32 * kWaves;  // of a workgroup
   static constexpr bool kNarrow = F != kNative;
   static constexpr int kD = 32 * NC;                                // channels that the instance holds
   static constexpr int kUnits = kD / 8;                             // of 8 channels
@@ -461,6 +461,13 @@ __global__ __launch_bounds__(64 * kWaves, NC == 8 ? 1 : 2) void prefill_scored_k
   };
 
   if (j0 < j1) {
+    if constexpr (!kFull && !W::kNarrow) {
+      // channels behind the head vector: no step writes them, and what is not finite there would have every row taken again
+      for (int u = tid; u < W::kBuffers * 8 * (W::kD - D); u += W::kThreads) {
+        const int at = u / (W::kD - D), d = D + u - at * (W::kD - D);
+        *reinterpret_cast<u32x4*>(&s_v[0][0] + at / 8 * W::kVBytes + at % 8 * W::kOctet + d * 16) = u32x4{0, 0, 0, 0};
+      }
+    }
     load_ids(j0);
     load();
     if (j0 + 1 < j1) load_ids(j0 + 1);

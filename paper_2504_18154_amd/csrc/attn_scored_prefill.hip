@@ -16,7 +16,7 @@
 // one to arrive adds them up in order.
 //
 // Values that are not finite must not reach rows that do not see them (0 times NaN).  Codes: such a row is coded as zeros, its scale byte says 255, and rows that
-// see it are given NaN at the end.  bf16: results that are not finite are taken again, one row at a time, over the keys that it sees.
+// see it are given NaN at the end.  bf16: where a result is not finite and a key that the row does not see may be why, it is taken again over those that it sees.
 //
 // Weights are rounded to bf16 for the second product (2^-9 of each, unbiased); maxima, sums and the log-sum-exp are fp32, from the weights before that.
 //
@@ -117,6 +117,21 @@ struct Form {
   float scale_log2e, cap_in, cap_log2e;  // cap_in: 2 log2(e) scale / cap, or 0
   const float* slopes;
 };
+
+// Whether a value of keys [from, to) is not finite.
+__device__ __attribute__((noinline)) bool not_finite_in(const char* __restrict__ v_head, uint32_t blk_stride, const int32_t* __restrict__ table, int from, int to, int D) {
+  bool odd = false;
+  for (int blk = from >> 4; blk * kBlockSize < to; ++blk) {
+    const char* const at = v_head + (size_t)(uint32_t)table[blk] * blk_stride;
+    for (int u = threadIdx.x & 63; u < 2 * D; u += 64) {  // (half of a channel's slots)
+      const u32x4 x = *reinterpret_cast<const u32x4*>(at + u * 16);
+      const int key = blk * kBlockSize + 8 * (u & 1);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) odd |= key + e >= from && key + e < to && (x[e >> 1] >> (16 * (e & 1)) & 0x7f80u) == 0x7f80u;
+    }
+  }
+  return __any(odd);
+}
 
 // One row again, from its keys alone, by a wavefront: lane l has channels l, l + 64, ...  For results that are not finite, where a value that the row does not
 // see may be the cause.
@@ -571,9 +586,14 @@ __global__ __launch_bounds__(64 * kWaves, NC == 8 ? 1 : 2) void prefill_scored_k
     again = !none && across_halves_sum(odd) != 0.f && l < INFINITY;
     for (uint32_t left = (uint32_t)__ballot(again && half == 0); left; left &= left - 1) {
       const int r = __builtin_ctz(left);
-      const int r_tok = __builtin_amdgcn_readlane(tok, r), r_head = __builtin_amdgcn_readlane(head, r);
-      row_again<NC, kForm>(q + (size_t)r_tok * q_row_stride + (size_t)r_head * D, k_head, v_head, blk_stride, table, __builtin_amdgcn_readlane(lo, r),
-                           __builtin_amdgcn_readlane(hi, r), __builtin_amdgcn_readlane(pos, r),
+      const int r_tok = __builtin_amdgcn_readlane(tok, r), r_head = __builtin_amdgcn_readlane(head, r), r_lo = __builtin_amdgcn_readlane(lo, r), r_hi = __builtin_amdgcn_readlane(hi, r);
+      // (if nothing that the row does not see was the cause, the result stands)
+      const bool unseen = not_finite_in(v_head, blk_stride, table, max(t_lo, wj0 * kKeys), r_lo, D) || not_finite_in(v_head, blk_stride, table, r_hi, min(t_hi, wj1 * kKeys), D);
+      if (!unseen) {
+        if (col == r) again = false;
+        continue;
+      }
+      row_again<NC, kForm>(q + (size_t)r_tok * q_row_stride + (size_t)r_head * D, k_head, v_head, blk_stride, table, r_lo, r_hi, __builtin_amdgcn_readlane(pos, r),
                            __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(slope), r)), form, D, out + ((size_t)r_tok * Hq + r_head) * D);
     }
   }

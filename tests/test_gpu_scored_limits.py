@@ -194,3 +194,22 @@ def test_prompts_of_many_rows(fmt, D, Hq, Hkv):
         assert not out.isnan().any()
         check_rows(p, q, out, lse, seq, pos, np.zeros(T) if begin is None else begin, pos + 1, cap, slopes, tokens=some, held=held, label=kind)
     p.ctx.close()
+
+
+def test_a_value_that_all_rows_see_and_is_not_finite():
+    """An infinity at the first position of one prompt, a NaN behind every row of the other's first tiles: the first is in every row's result, and no row is at a loss for it."""
+    before, new = np.array([0, 0]), np.array([700, 700])
+    p = Pools("bf16", 128, 4, 2, before + new, seed=73)
+    p.fill(before + new, 74)
+    k, v = p.logical()
+    v[p.table[0, 0], 0, 0, 9] = float("inf")
+    v[p.table[1, 650 // 16], 1, 650 % 16, 100] = float("nan")
+    p.put(k, v)
+    seq, pos = packed(before, new)
+    q = _q(len(seq), p, 75)
+    out, lse = _prefill(p, before, new, q)
+    check_rows(p, q, out, lse, seq, pos, np.zeros(len(seq)), pos + 1, tokens=range(0, len(seq), 9))
+    o = out.cpu()
+    assert (~o[:700, :2, 9].isfinite()).all() and o[:700, :2, :9].isfinite().all() and o[:700, 2:].isfinite().all() and lse.isfinite().all()
+    assert o[700:700 + 650].isfinite().all() and o[700 + 650:, 2:, 100].isnan().all()
+    p.ctx.close()

@@ -189,7 +189,7 @@ __global__ __launch_bounds__(64 * kWaves, NC == 8 ? 1 : 2) void prefill_scored_k
 
   // ---- the tile, its rows and their keys
   const int xu = fast_div((int)blockIdx.x, div_hkv), g = (int)blockIdx.x - xu * Hkv, unit = units - 1 - xu;
-  auto first_unit = [&](int cu, int b) { return (long long)cu * G / W::kRows + b; };
+  auto first_unit = [&](int cu, int b) { return (long long)prefill_scored_first_tile(W::kRows, G, cu, b); };
   TileOf at_tile;
   if (B > 2 && B <= 64 && !key_begin && !key_end) {
     at_tile = heaviest_tile<W::kRows>(cu_q, ctx_before, B, G, xu);

@@ -8,6 +8,7 @@
 #include <algorithm>
 
 #include "common.h"
+#include "scored_tiles.h"
 
 namespace eco {
 
@@ -53,7 +54,6 @@ inline size_t decode_scored_workspace(const ecoserve_layout& L, int32_t num_cu) 
 
 // Prompts: tiles of 128 or 256 rows ((position, query head) pairs of a K/V head), their 64-key steps cut among `prefill_scored_splits` workgroups where tiles are few.
 constexpr int32_t kTileRows = 128, kMostTileRows = 256;
-inline int64_t prefill_scored_tiles(int32_t rows, int32_t B, int32_t T, int32_t G) { return (int64_t)T * G / rows + (B < T ? B : T); }
 // Rows of a tile, 32 to a wavefront: the more of them there are, the fewer turn a step's codes into operands for themselves.  (Heads of up to 64 channels have no 16
 // bytes of a step for each of eight wavefronts, those of more than 128 no registers for two on a SIMD.)  64 heads on 8 of 128, in tiles of 128 and 256 rows: two
 // prompts of 8192 tokens over e4m3 2200 and 2140 us, 2048 tokens of three over bf16 131 and 128.  Short prompts would leave the larger ones half empty.

@@ -11,7 +11,8 @@
 // operand of the second product, and P stays in registers.
 //
 // A row's keys are a range.  The tile walks the steps from the first range's begin to the last range's end; a wavefront passes over steps that none of its
-// rows sees, and masks only where a step is not inside all its rows' ranges.
+// rows sees, and masks only where a step is not inside all its rows' ranges.  Ranges that are given may leave keys between them that no row of the tile sees: tiles where
+// neighbouring rows' ranges do not touch look at each step for the keys that are seen, from all rows' ranges in LDS; other keys' blocks are not named, and their values zeros.
 // Tiles are dealt heaviest first.  Where they are few, their steps are cut among several workgroups; each leaves its state in the workspace, and the last
 // one to arrive adds them up in order.
 //
@@ -118,16 +119,29 @@ struct Form {
   const float* slopes;
 };
 
-// Whether a value of keys [from, to) is not finite.
-__device__ __attribute__((noinline)) bool not_finite_in(const char* __restrict__ v_head, uint32_t blk_stride, const int32_t* __restrict__ table, int from, int to, int D) {
+// Keys k0 .. k0 + 63 that one of n rows sees (n a multiple of 64).
+__device__ __forceinline__ uint64_t seen_by_rows(const int* row_lo, const int* row_hi, int n, int k0) {
+  uint64_t m = 0;
+  for (int r = threadIdx.x & 63; r < n; r += 64) m |= keys_seen(row_lo[r], row_hi[r], k0);
+  uint32_t a = (uint32_t)m, b = (uint32_t)(m >> 32);
+#pragma unroll
+  for (int w = 1; w < 64; w *= 2) a |= (uint32_t)__shfl_xor((int)a, w), b |= (uint32_t)__shfl_xor((int)b, w);
+  return (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)b) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)a);
+}
+
+// Whether a value of keys [from, to) is not finite.  (n > 0: of those that one of the n rows sees.)
+__device__ __attribute__((noinline)) bool not_finite_in(const char* __restrict__ v_head, uint32_t blk_stride, const int32_t* __restrict__ table, int from, int to, int D,
+                                                        const int* row_lo, const int* row_hi, int n) {
   bool odd = false;
   for (int blk = from >> 4; blk * kBlockSize < to; ++blk) {
+    const uint32_t slots = n ? (uint32_t)seen_by_rows(row_lo, row_hi, n, blk * kBlockSize) & 0xffffu : 0xffffu;
+    if (!slots) continue;
     const char* const at = v_head + (size_t)(uint32_t)table[blk] * blk_stride;
     for (int u = threadIdx.x & 63; u < 2 * D; u += 64) {  // (half of a channel's slots)
       const u32x4 x = *reinterpret_cast<const u32x4*>(at + u * 16);
       const int key = blk * kBlockSize + 8 * (u & 1);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) odd |= key + e >= from && key + e < to && (x[e >> 1] >> (16 * (e & 1)) & 0x7f80u) == 0x7f80u;
+      for (int e = 0; e < 8; ++e) odd |= key + e >= from && key + e < to && (slots >> (8 * (u & 1) + e) & 1) && (x[e >> 1] >> (16 * (e & 1)) & 0x7f80u) == 0x7f80u;
     }
   }
   return __any(odd);
@@ -184,7 +198,7 @@ __global__ __launch_bounds__(64 * kWaves, NC == 8 ? 1 : 2) void prefill_scored_k
   typedef Cached<F> C;
   typedef Tile<F, NC, kWaves> W;
   __shared__ __attribute__((aligned(16))) char s_k[W::kBuffers][W::kKBytes], s_v[W::kBuffers][W::kVBytes];
-  __shared__ int s_lo[kWaves], s_hi[kWaves], s_order, s_bad[2];
+  __shared__ int s_lo[kWaves], s_hi[kWaves], s_order, s_bad[2], s_row_lo[W::kRows], s_row_hi[W::kRows];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 31, half = lane >> 5;
 
   // ---- the tile, its rows and their keys
@@ -209,12 +223,25 @@ __global__ __launch_bounds__(64 * kWaves, NC == 8 ? 1 : 2) void prefill_scored_k
   const bool none = hi == 0;
   // over the wavefront's rows: first begin, last begin, first end, last end
   const int w_lo = -lanes_max(0x7fffffff - lo) + 0x7fffffff, w_hi = lanes_max(hi), w_lo_last = lanes_max(none ? 0 : lo), w_hi_first = 0x7fffffff - lanes_max(none ? 0 : 0x7fffffff - hi);
+  const bool given = key_begin || key_end;
   if (lane == 0) s_lo[wave] = w_lo, s_hi[wave] = w_hi;
+  if (given && half == 0) s_row_lo[wave * 32 + col] = lo, s_row_hi[wave * 32 + col] = hi;
   if (tid < 2) s_bad[tid] = 0;
   __syncthreads();
   int t_lo = s_lo[0], t_hi = s_hi[0];
 #pragma unroll
   for (int w = 1; w < kWaves; ++w) t_lo = min(t_lo, s_lo[w]), t_hi = max(t_hi, s_hi[w]);
+  t_lo = __builtin_amdgcn_readfirstlane(t_lo), t_hi = __builtin_amdgcn_readfirstlane(t_hi);
+  // (without given ranges a row sees what the rows in front of it see)
+  bool gaps = false;
+  if (given) {
+    const int n = min(rows - row0, W::kRows);
+    bool apart = false;
+#pragma unroll
+    for (int i = 0; i < W::kRows; i += 64)
+      if (const int r = i + lane; r + 1 < n) apart |= ranges_apart(s_row_lo[r], s_row_hi[r], s_row_lo[r + 1], s_row_hi[r + 1]);
+    gaps = __any(apart);
+  }
   uint16_t* const out_row = out + ((size_t)tok * Hq + head) * D;
   float* const lse_row = lse ? lse + (size_t)tok * Hq + head : nullptr;
   const int j_first = t_hi > 0 ? t_lo / kKeys : 0, j_end = t_hi > 0 ? (t_hi - 1) / kKeys + 1 : 0;
@@ -239,18 +266,21 @@ __global__ __launch_bounds__(64 * kWaves, NC == 8 ? 1 : 2) void prefill_scored_k
   const char *const k_head = k_cache + (size_t)g * blk_bytes, *const v_head = v_cache + (size_t)g * blk_bytes;
   const int32_t* const table = block_table + (size_t)seq.b * bt_stride;
   const int blk_lo = t_lo >> 4, blk_hi = (t_hi - 1) >> 4;
-  // (blocks without keys of the tile are not named: their neighbour stands in, and is masked)
-  auto id_of = [&](int blk) { return table[min(max(blk, blk_lo), blk_hi)]; };
+  auto seen_in = [&](int j) { return seen_by_rows(s_row_lo, s_row_hi, W::kRows, j * kKeys); };
   u32x4 kr[W::kChunks], vr[W::kChunks];
   uint32_t k_scale = 127, v_scale[4] = {0x7f7f7f7fu, 0x7f7f7f7fu, 0x7f7f7f7fu, 0x7f7f7f7fu};
   int id_k = 0, id_v = 0;
   const int v_block = wave & 3, v_part = wave >> 2;  // the block of V that the wavefront stages, and which of its runs of 64 places first
-  auto load_ids = [&](int j) {
-    id_k = id_of(4 * j + (lane >> 4));
-    id_v = id_of(4 * j + v_block);
+  // (blocks without keys of the tile are not named: another of its blocks stands in, and is masked)
+  auto load_ids = [&](int j, auto gapped) __attribute__((always_inline)) {
+    constexpr bool kGaps = decltype(gapped)::value;
+    uint64_t seen = 0;
+    if constexpr (kGaps) seen = seen_in(j);
+    id_k = table[entry_of_block(4 * j + (lane >> 4), blk_lo, blk_hi, kGaps, seen)];
+    id_v = table[entry_of_block(4 * j + v_block, blk_lo, blk_hi, kGaps, seen)];
   };
   auto at_block = [](int id, uint32_t stride) { return (size_t)(uint32_t)id * stride; };
-  auto load = [&]() {
+  auto load = [&]() __attribute__((always_inline)) {
     const char* const kp = k_head + at_block(id_k, blk_stride) + (lane & 15) * 16 + wave * 256;
     const char* const vp = v_head + at_block(id_v, blk_stride) + (v_part * 64 + lane) * 16;
 #pragma unroll
@@ -267,7 +297,7 @@ __global__ __launch_bounds__(64 * kWaves, NC == 8 ? 1 : 2) void prefill_scored_k
     }
   };
   // (j: the step that lies in the registers)
-  auto store = [&](int j) {
+  auto store = [&](int j, auto gapped) __attribute__((always_inline)) {
     char* const kb = s_k[W::kBuffers == 2 ? j & 1 : 0] + lane * 16;
     char* const vb = s_v[W::kBuffers == 2 ? j & 1 : 0] + 2 * v_block * W::kOctet + (W::kNarrow ? v_part * 1024 + lane * 16 : v_part * 512 + (lane >> 1) * 16 + (lane & 1) * W::kOctet);
     const u32x4 zero = {0, 0, 0, 0};
@@ -288,9 +318,12 @@ __global__ __launch_bounds__(64 * kWaves, NC == 8 ? 1 : 2) void prefill_scored_k
         *reinterpret_cast<u32x4*>(kb + u * kKeys * 16) = there ? kr[i] : zero;
       }
     }
-    // V: slots behind the tile's last key (nobody sees them) may hold anything: zeros.  So are those in front of the first.
-    const int key0 = j * kKeys + 16 * v_block, keep_lo = t_lo - key0, keep_hi = t_hi - key0;  // of the block's 16 slots
-    const bool edge = keep_lo > 0 || keep_hi < 16;
+    // V: slots behind the tile's last key (nobody sees them) may hold anything: zeros.  So are those in front of the first, and between others that none of its rows sees.
+    const int key0 = j * kKeys + 16 * v_block;
+    uint32_t slots = 0xffffu;
+    if constexpr (decltype(gapped)::value) slots &= (uint32_t)(seen_in(j) >> (16 * v_block));
+    else if (key0 < t_lo || key0 + 16 > t_hi) slots &= (uint32_t)keys_seen(t_lo, t_hi, key0);
+    const bool edge = slots != 0xffffu;
     if constexpr (W::kNarrow) {
       uint32_t sw[4];
 #pragma unroll
@@ -306,7 +339,7 @@ __global__ __launch_bounds__(64 * kWaves, NC == 8 ? 1 : 2) void prefill_scored_k
       if (edge) {
         uint32_t keep[4] = {0, 0, 0, 0};
 #pragma unroll
-        for (int slot = 0; slot < 16; ++slot) keep[slot >> 2] |= slot >= keep_lo && slot < keep_hi ? 0xffu << (8 * (slot & 3)) : 0u;
+        for (int slot = 0; slot < 16; ++slot) keep[slot >> 2] |= slots >> slot & 1 ? 0xffu << (8 * (slot & 3)) : 0u;
         clear(keep);
       }
       // (a byte of 255 is a zero byte of ~w)
@@ -353,7 +386,7 @@ __global__ __launch_bounds__(64 * kWaves, NC == 8 ? 1 : 2) void prefill_scored_k
 #pragma unroll
         for (int w = 0; w < 4; ++w) {
           const int slot = h8 + 2 * w;
-          const uint32_t keep = (slot >= keep_lo && slot < keep_hi ? 0xffffu : 0u) | (slot + 1 >= keep_lo && slot + 1 < keep_hi ? 0xffff0000u : 0u);
+          const uint32_t keep = (slots >> slot & 1 ? 0xffffu : 0u) | (slots >> (slot + 1) & 1 ? 0xffff0000u : 0u);
 #pragma unroll
           for (int i = 0; i < W::kChunks; ++i) vr[i][w] &= keep;
         }
@@ -375,7 +408,7 @@ __global__ __launch_bounds__(64 * kWaves, NC == 8 ? 1 : 2) void prefill_scored_k
   const int krow = (col & 0x13) | ((col & 4) << 1) | ((col & 8) >> 1);
   const int a_k_off = (half * kKeys + krow) * 16, a_v_off = half * W::kOctet + col * 16;
 
-  auto step = [&](int j) {
+  auto step = [&](int j) __attribute__((always_inline)) {
     const char* const kb = s_k[W::kBuffers == 2 ? j & 1 : 0] + a_k_off;
     const char* const vb = s_v[W::kBuffers == 2 ? j & 1 : 0] + a_v_off;
     f32x16 s[2];
@@ -475,21 +508,14 @@ __global__ __launch_bounds__(64 * kWaves, NC == 8 ? 1 : 2) void prefill_scored_k
     }
   };
 
-  if (j0 < j1) {
-    if constexpr (!kFull && !W::kNarrow) {
-      // channels behind the head vector: no step writes them, and what is not finite there would have every row taken again
-      for (int u = tid; u < W::kBuffers * 8 * (W::kD - D); u += W::kThreads) {
-        const int at = u / (W::kD - D), d = D + u - at * (W::kD - D);
-        *reinterpret_cast<u32x4*>(&s_v[0][0] + at / 8 * W::kVBytes + at % 8 * W::kOctet + d * 16) = u32x4{0, 0, 0, 0};
-      }
-    }
-    load_ids(j0);
+  auto walk = [&](auto gapped) __attribute__((always_inline)) {
+    load_ids(j0, gapped);
     load();
-    if (j0 + 1 < j1) load_ids(j0 + 1);
-    store(j0);
+    if (j0 + 1 < j1) load_ids(j0 + 1, gapped);
+    store(j0, gapped);
     if (j0 + 1 < j1) {
       load();
-      if (j0 + 2 < j1) load_ids(j0 + 2);
+      if (j0 + 2 < j1) load_ids(j0 + 2, gapped);
     }
     __syncthreads();
     for (int j = j0; j < j1; ++j) {
@@ -499,10 +525,10 @@ __global__ __launch_bounds__(64 * kWaves, NC == 8 ? 1 : 2) void prefill_scored_k
         const bool first = kWaves == 4 || !W::kNarrow || wave < 4;
         if (!first && j >= wj0 && j < wj1) step(j);
         if (j + 1 < j1) {
-          store(j + 1);
+          store(j + 1, gapped);
           if (j + 2 < j1) {
             load();
-            if (j + 3 < j1) load_ids(j + 3);
+            if (j + 3 < j1) load_ids(j + 3, gapped);
           }
         }
         if (first && j >= wj0 && j < wj1) step(j);
@@ -511,15 +537,27 @@ __global__ __launch_bounds__(64 * kWaves, NC == 8 ? 1 : 2) void prefill_scored_k
         if (j >= wj0 && j < wj1) step(j);
         __syncthreads();
         if (j + 1 < j1) {
-          store(j + 1);
+          store(j + 1, gapped);
           if (j + 2 < j1) {
             load();
-            if (j + 3 < j1) load_ids(j + 3);
+            if (j + 3 < j1) load_ids(j + 3, gapped);
           }
         }
         __syncthreads();
       }
     }
+  };
+  if (j0 < j1) {
+    if constexpr (!kFull && !W::kNarrow) {
+      // channels behind the head vector: no step writes them, and what is not finite there would have every row taken again
+      for (int u = tid; u < W::kBuffers * 8 * (W::kD - D); u += W::kThreads) {
+        const int at = u / (W::kD - D), d = D + u - at * (W::kD - D);
+        *reinterpret_cast<u32x4*>(&s_v[0][0] + at / 8 * W::kVBytes + at % 8 * W::kOctet + d * 16) = u32x4{0, 0, 0, 0};
+      }
+    }
+    // (two loops, so that the one of all other tiles has nothing to look for: in one, 2048 tokens of documents took 134 us instead of 128)
+    if (gaps) walk(std::true_type());
+    else walk(std::false_type());
   }
   l = across_halves_sum(l);
   if constexpr (W::kNarrow) {
@@ -588,7 +626,9 @@ __global__ __launch_bounds__(64 * kWaves, NC == 8 ? 1 : 2) void prefill_scored_k
       const int r = __builtin_ctz(left);
       const int r_tok = __builtin_amdgcn_readlane(tok, r), r_head = __builtin_amdgcn_readlane(head, r), r_lo = __builtin_amdgcn_readlane(lo, r), r_hi = __builtin_amdgcn_readlane(hi, r);
       // (if nothing that the row does not see was the cause, the result stands)
-      const bool unseen = not_finite_in(v_head, blk_stride, table, max(t_lo, wj0 * kKeys), r_lo, D) || not_finite_in(v_head, blk_stride, table, r_hi, min(t_hi, wj1 * kKeys), D);
+      const int n = gaps ? W::kRows : 0;
+      const bool unseen = not_finite_in(v_head, blk_stride, table, max(t_lo, wj0 * kKeys), r_lo, D, s_row_lo, s_row_hi, n) ||
+                          not_finite_in(v_head, blk_stride, table, r_hi, min(t_hi, wj1 * kKeys), D, s_row_lo, s_row_hi, n);
       if (!unseen) {
         if (col == r) again = false;
         continue;

@@ -1,4 +1,4 @@
-"""Attention with formed scores where it answered wrongly once: batches of fewer tokens than sequences."""
+"""Attention with formed scores where it answered wrongly once: batches of fewer tokens than sequences, ranges that leave keys between them."""
 import numpy as np
 import pytest
 import torch
@@ -24,4 +24,58 @@ def test_fewer_tokens_than_sequences(fmt, ranges, new):
     out, lse = _prefill(p, before, new, q, _scores(p, 0.0, None, begin, pos + 1) if ranges else None)
     assert not out.isnan().any() and not lse.isnan().any()
     check_rows(p, q, out, lse, seq, pos, begin, pos + 1)
+    p.ctx.close()
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("D,Hq,Hkv", [(64, 4, 2), (128, 64, 8), (80, 8, 8), (256, 8, 1)], ids=str)
+@pytest.mark.parametrize("kind", ["ends", "begins", "both"])
+def test_keys_that_no_row_sees(fmt, D, Hq, Hkv, kind):
+    """Tiles whose rows' ranges leave keys between them, whole blocks and parts of blocks: what stands there (codes that are NaN, beside scales that are not, and bf16 NaN) reaches nobody, and the
+    block table names a block of nothing else in their place."""
+    before, new = np.array([700, 0]), np.array([520 if Hq == 64 else 60, 40])
+    total = before + new
+    p = Pools(fmt, D, Hq, Hkv, total, seed=93)
+    p.fill(total, 94)
+    seq, pos = packed(before, new)
+    rng = np.random.default_rng(95)
+    begin, end = np.zeros(len(seq), dtype=np.int64), pos + 1
+    if kind == "begins":     # every row its own key, or none: runs of none of more than a block
+        begin = np.where(np.arange(len(seq)) // 20 % 2 == 0, pos, pos + 1)
+    else:                    # one segment of the past to a row: some are neighbours, most are not
+        at = rng.integers(0, 12, len(seq)) * 50
+        if kind == "both":
+            begin = np.where(seq == 0, at + 3, pos // 9 * 9)
+        end = np.where(seq == 0, at + 3 + rng.integers(0, 30, len(seq)), pos // 9 * 9 + rng.integers(0, 5, len(seq)))
+        if kind == "ends":   # (begins below 0; every range from the first key on, and one that is long)
+            end = np.where(seq == 0, np.minimum(end, 40), end)
+            end[10] = 600
+    seen = [np.zeros(t, dtype=bool) for t in total]
+    for t in range(len(seq)):
+        seen[seq[t]][max(int(begin[t]), 0):max(int(min(end[t], total[seq[t]])), 0)] = True
+    (k, v), s = p.logical(), p.scales()
+    s = None if s is None else s.copy()
+    named = {int(p.table[b, j]) for b in range(2) for j in range((total[b] + 15) // 16)}
+    spare = next(i for i in range(p.blocks) if i not in named)
+    bad = float("nan") if fmt == "bf16" else 0x7f
+    k[spare], v[spare] = bad, bad
+    if s is not None:
+        s[spare] = 127
+    for b in range(2):
+        for j in range((total[b] + 15) // 16):
+            here = seen[b][16 * j:16 * j + 16]
+            blk = p.table[b, j]
+            for i in np.flatnonzero(~here):
+                k[blk, :, i], v[blk, :, i] = bad, bad
+                if s is not None:
+                    s[blk, :, :, i] = 127 if i % 2 else 254
+            if not here.any():
+                p.table[b, j] = spare
+    p.put(k, v, *((s[:, :, 0], s[:, :, 1]) if s is not None else ()))
+    p.dev_table = torch.from_numpy(p.table).cuda()
+    q = _q(len(seq), p, 96)
+    for form in ((0.0, None), (20.0, None)):
+        out, lse = _prefill(p, before, new, q, _scores(p, *form, begin if kind != "ends" else None, end if kind != "begins" else None))
+        assert out.isfinite().all()
+        check_rows(p, q, out, lse, seq, pos, begin, np.minimum(end, total[seq]), *form, tokens=range(0, len(seq), 1 if len(seq) < 200 else 7))
     p.ctx.close()

@@ -552,7 +552,7 @@ int ecoserve_kv_read(ecoserve_ctx* ctx, const ecoserve_cache* cache, void* k_row
  * others.
  */
 typedef struct {
-  float softcap;             /* 0: none; otherwise from 2^-126 on, and finite */
+  float softcap;             /* 0: none; otherwise from 2^-126 on, and finite.  Caps up to 64 move a score by 2^-16 at most, larger ones by a few units of fp32 */
   const float* slopes;       /* dev, float[Hq], or NULL */
   const int32_t* key_begin;  /* dev, int32[T], or NULL: 0 */
   const int32_t* key_end;    /* dev, int32[T], or NULL: p + 1 */

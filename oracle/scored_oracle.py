@@ -81,7 +81,8 @@ def attend(q: np.ndarray, keys: np.ndarray, values: np.ndarray, at: np.ndarray, 
         off = (D + 8) * 2.0 ** -24 * (np.abs(q) @ np.abs(keys).T).max(1) * scale
         if cap:
             s = cap * np.tanh(s / cap)
-            off = off + cap * 2.0 ** -21
+            # (up to 64 of the cap, beyond that of the score: what is small beside a cap is not to feel it)
+            off = off + np.minimum(cap, np.maximum(np.abs(s).max(1), 64.0)) * 2.0 ** -21
         if slopes is not None:
             bias = slopes[:, None] * (at - position)[None]
             s = s + bias

@@ -30,6 +30,7 @@
 
 #include "quant.h"
 #include "scored.h"
+#include "softcap.h"
 
 namespace eco {
 
@@ -169,7 +170,8 @@ __global__ __launch_bounds__(64 * kWaves, decode_scored_waves(F != kNative, NC))
                                                                  const int32_t* __restrict__ key_begin, const int32_t* __restrict__ key_end,
                                                                  const float* __restrict__ slopes, uint16_t* __restrict__ out, float* __restrict__ lse,
                                                                  float* states, uint32_t* counters, int B, int Hq, int Hkv, int G, int D, int num_cu,
-                                                                 float scale_log2e, float cap_in, float cap_log2e) {
+                                                                 const Cap cap) {
+  const float scale_log2e = cap.scale_log2e;
   constexpr int kThreads = 64 * kWaves;
   typedef Cached<F> C;
   typedef Step<F, NC> Frag;
@@ -385,10 +387,12 @@ __global__ __launch_bounds__(64 * kWaves, decode_scored_waves(F != kNative, NC))
       };
       if constexpr (F == kInt8) scaled(f.sk);
       if constexpr (kForm) {
-        if (cap_in > 0.f) {
-          // cap tanh(y) = cap - 2 cap / (1 + exp(2 y)), off by an ulp of the cap
+        if (cap.kind == kNear) {
 #pragma unroll
-          for (int j = 0; j < kTokens; ++j) x[j] = cap_log2e - 2.f * cap_log2e * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(x[j] * cap_in));
+          for (int j = 0; j < kTokens; ++j) x[j] = __builtin_fmaf(2.f * cap.log2e, near_cap(x[j], cap), cap.log2e);
+        } else if (cap.kind == kFar) {
+#pragma unroll
+          for (int j = 0; j < kTokens; ++j) x[j] = far_cap(x[j], cap);
         } else {
 #pragma unroll
           for (int j = 0; j < kTokens; ++j) x[j] *= scale_log2e;
@@ -535,12 +539,11 @@ void launch_waves(const ScoredArgs& a, hipStream_t s) {
   // states of the wavefronts, or the weights of the pieces when they are added up
   const size_t words = std::max((size_t)kWaves * G * (kPassChannels<NC> + 4), (size_t)G * kScoredMostPieces);
   const size_t lds = (head_words(a.B) + words) * sizeof(uint32_t);
-  const float cap_in = form && a.softcap > 0.f ? 2.f * a.scale_log2e / a.softcap : 0.f;
   const int grid = (kWaves == 8 ? 1 : decode_scored_waves(F != kNative, NC)) * a.num_cu;
   auto go = [&](auto kernel) {
     hipLaunchKernelGGL(kernel, dim3(grid), dim3(64 * kWaves), lds, s, (const uint16_t*)a.q, a.q_row_stride, (const char*)a.k_cache, (const char*)a.v_cache, a.scales,
                        a.block_table, a.bt_stride, a.ctx_before, a.key_begin, a.key_end, a.slopes, (uint16_t*)a.out, a.lse, a.states, a.counters, a.B, a.Hq, a.Hkv, G,
-                       a.D, a.num_cu, a.scale_log2e, cap_in, a.softcap * kLog2e);
+                       a.D, a.num_cu, make_cap(a.softcap, a.scale_log2e));
   };
   const bool full = a.D == 32 * NC;
   if (form) full ? go(&decode_scored_kernel<F, NC, true, kWaves, true>) : go(&decode_scored_kernel<F, NC, true, kWaves, false>);

@@ -32,6 +32,7 @@
 
 #include "quant.h"
 #include "scored.h"
+#include "softcap.h"
 
 namespace eco {
 
@@ -111,11 +112,12 @@ __device__ __forceinline__ TileOf heaviest_tile(const int32_t* __restrict__ cu_q
   return r;
 }
 
-enum { kPlain, kCapped, kBiased };  // scores: scaled, capped, or with a bias
+enum { kPlain, kCapped, kBiased, kFarCapped };  // scores: scaled, capped (near: softcap.h), with a bias (capped or not), or capped far above them, with a bias or without
 
 // What a row of scores needs of the score's form.
 struct Form {
-  float scale_log2e, cap_in, cap_log2e;  // cap_in: 2 log2(e) scale / cap, or 0
+  Cap cap;
+  float by, start;  // without a bias: scores are by s + start, s the products or what their caps make of them
   const float* slopes;
 };
 
@@ -172,9 +174,9 @@ __device__ __attribute__((noinline)) void row_again(const uint16_t* __restrict__
       v[i] = bf16_bits_to_float(vp[d * 16 + (j & 15)]);
     }
     s = wave_sum(s);
-    if (kForm != kPlain && form.cap_in > 0.f) s = form.cap_log2e - 2.f * form.cap_log2e * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(s * form.cap_in));
-    else s *= form.scale_log2e;
-    if (kForm == kBiased) s = __builtin_fmaf(slope, (float)(j - pos), s);
+    if (kForm == kFarCapped) s = far_cap(s, form.cap);
+    else s = __builtin_fmaf(kForm != kPlain && form.cap.kind == kNear ? near_cap(s, form.cap) : s, form.by, form.start);
+    if (kForm == kBiased || kForm == kFarCapped) s = __builtin_fmaf(slope, (float)(j - pos), s);
     const float m_new = fmaxf(m, s), alpha = __builtin_amdgcn_exp2f(m - m_new), p = __builtin_amdgcn_exp2f(s - m_new);
     l = l * alpha + p;
 #pragma unroll
@@ -188,7 +190,6 @@ __device__ __attribute__((noinline)) void row_again(const uint16_t* __restrict__
 
 // Workgroup (x, y): K/V head x % Hkv of tile x / Hkv, counted from the last one; y: which part of its steps.
 // kFull: the head vector fills the instance's channels.
-// kForm: kPlain, kCapped or kBiased (capped or not).
 template <int F, int NC, int kForm, bool kFull, int kWaves>
 __global__ __launch_bounds__(64 * kWaves, NC == 8 ? 1 : 2) void prefill_scored_kernel(
     const uint16_t* __restrict__ q, int q_row_stride, const char* __restrict__ k_cache, const char* __restrict__ v_cache, const uint8_t* __restrict__ scales,
@@ -257,7 +258,7 @@ __global__ __launch_bounds__(64 * kWaves, NC == 8 ? 1 : 2) void prefill_scored_k
     const bf16x8 zero = {0, 0, 0, 0, 0, 0, 0, 0};
     qf[t] = valid && 16 * t + 8 * half < D ? *reinterpret_cast<const bf16x8*>(q_row + 16 * t + 8 * half) : zero;
   }
-  const float slope = kForm == kBiased && form.slopes ? form.slopes[head] * kLog2e : 0.f;
+  const float slope = (kForm == kBiased || kForm == kFarCapped) && form.slopes ? form.slopes[head] * kLog2e : 0.f;
 
   // ---- staging: a step's 16-byte pieces to registers, and from there to LDS as bf16
   const int blk_bytes = kBlockSize * D * C::kBytes;
@@ -426,22 +427,26 @@ __global__ __launch_bounds__(64 * kWaves, NC == 8 ? 1 : 2) void prefill_scored_k
     const int k0 = j * kKeys;
     // register i of half-tile sub is key k0 + 32 sub + 16 (i / 8) + 8 half + i % 8
     if constexpr (kForm == kCapped) {
-      // cap tanh(x / cap) = cap - 2 cap / (1 + e^(2 x / cap)): kept as -1 / (1 + e), the factor and the summand go with the maximum's into the weights' exponent
+      // (the factor and the summand go with the maximum's into the weights' exponent)
 #pragma unroll
       for (int sub = 0; sub < 2; ++sub)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) s[sub][i] = __builtin_amdgcn_rcpf(-1.f - __builtin_amdgcn_exp2f(s[sub][i] * form.cap_in));
+        for (int i = 0; i < 16; ++i) s[sub][i] = near_cap(s[sub][i], form.cap);
     }
-    if constexpr (kForm == kBiased) {
+    if constexpr (kForm == kFarCapped) {
+#pragma unroll
+      for (int sub = 0; sub < 2; ++sub)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[sub][i] = far_cap(s[sub][i], form.cap);
+    }
+    if constexpr (kForm == kBiased || kForm == kFarCapped) {
       const float at_first = slope * (float)(k0 + 8 * half - pos);  // (the further keys' bias is slope times a literal)
-      float by = form.scale_log2e, start = at_first;
-      if (form.cap_in > 0.f) {  // (one branch: as a choice per score it took as long as the products)
-        by = 2.f * form.cap_log2e;
-        start += form.cap_log2e;
+      const float by = form.by, start = at_first + form.start;
+      if (kForm == kBiased && form.cap.kind == kNear) {  // (one branch: as a choice per score it took as long as the products)
 #pragma unroll
         for (int sub = 0; sub < 2; ++sub)
 #pragma unroll
-          for (int i = 0; i < 16; ++i) s[sub][i] = __builtin_amdgcn_rcpf(-1.f - __builtin_amdgcn_exp2f(s[sub][i] * form.cap_in));
+          for (int i = 0; i < 16; ++i) s[sub][i] = near_cap(s[sub][i], form.cap);
       }
 #pragma unroll
       for (int sub = 0; sub < 2; ++sub)
@@ -460,7 +465,7 @@ __global__ __launch_bounds__(64 * kWaves, NC == 8 ? 1 : 2) void prefill_scored_k
         }
     }
     // the exponents of the weights: c s + shift
-    const float c = kForm == kBiased ? 1.f : kForm == kCapped ? 2.f * form.cap_log2e : form.scale_log2e, at_zero = kForm == kCapped ? form.cap_log2e : 0.f;
+    const float c = kForm == kBiased || kForm == kFarCapped ? 1.f : form.by, at_zero = kForm == kCapped ? form.start : 0.f;
     float top = max3(s[0][0], s[0][1], s[0][2]);
 #pragma unroll
     for (int i = 3; i < 15; i += 2) top = max3(top, s[0][i], s[0][i + 1]);
@@ -655,7 +660,8 @@ __global__ __launch_bounds__(64 * kWaves, NC == 8 ? 1 : 2) void prefill_scored_k
 template <int F, int NC, int kWaves>
 void launch_waves(const ScoredArgs& a, int32_t splits, hipStream_t s) {
   const int G = a.Hq / a.Hkv, units = (int)prefill_scored_tiles(32 * kWaves, a.B, a.T, G);
-  const Form form = {a.scale_log2e, a.softcap > 0.f ? 2.f * a.scale_log2e / a.softcap : 0.f, a.softcap * kLog2e, a.slopes};
+  const Cap cap = make_cap(a.softcap, a.scale_log2e);
+  const Form form = {cap, cap.kind == kNear ? 2.f * cap.log2e : cap.kind == kFar ? 1.f : a.scale_log2e, cap.kind == kNear ? cap.log2e : 0.f, a.slopes};
   auto go = [&](auto kernel) {
     hipLaunchKernelGGL(kernel, dim3((unsigned)units * a.Hkv, (unsigned)splits), dim3(64 * kWaves), 0, s, (const uint16_t*)a.q, a.q_row_stride, (const char*)a.k_cache,
                        (const char*)a.v_cache, a.scales, a.cu_q, a.ctx_before, a.block_table, a.bt_stride, a.key_begin, a.key_end, (uint16_t*)a.out, a.lse, a.states,
@@ -666,8 +672,9 @@ void launch_waves(const ScoredArgs& a, int32_t splits, hipStream_t s) {
     constexpr int kForm = decltype(kind)::value;
     full ? go(&prefill_scored_kernel<F, NC, kForm, true, kWaves>) : go(&prefill_scored_kernel<F, NC, kForm, false, kWaves>);
   };
-  if (a.slopes) with_form(std::integral_constant<int, kBiased>());
-  else if (a.softcap > 0.f) with_form(std::integral_constant<int, kCapped>());
+  if (cap.kind == kFar) with_form(std::integral_constant<int, kFarCapped>());
+  else if (a.slopes) with_form(std::integral_constant<int, kBiased>());
+  else if (cap.kind == kNear) with_form(std::integral_constant<int, kCapped>());
   else with_form(std::integral_constant<int, kPlain>());
 }
 

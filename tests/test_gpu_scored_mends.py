@@ -1,10 +1,10 @@
-"""Attention with formed scores where it answered wrongly once: batches of fewer tokens than sequences, ranges that leave keys between them."""
+"""Attention with formed scores where it answered wrongly once: batches of fewer tokens than sequences, ranges that leave keys between them, caps far above the scores."""
 import numpy as np
 import pytest
 import torch
 
 from tests.scored_util import Pools, check_rows, packed
-from tests.test_gpu_scored import FORMATS, _prefill, _q, _scores
+from tests.test_gpu_scored import FORMATS, _decode, _prefill, _q, _scores
 
 pytestmark = pytest.mark.gpu
 
@@ -78,4 +78,46 @@ def test_keys_that_no_row_sees(fmt, D, Hq, Hkv, kind):
         out, lse = _prefill(p, before, new, q, _scores(p, *form, begin if kind != "ends" else None, end if kind != "begins" else None))
         assert out.isfinite().all()
         check_rows(p, q, out, lse, seq, pos, begin, np.minimum(end, total[seq]), *form, tokens=range(0, len(seq), 1 if len(seq) < 200 else 7))
+    p.ctx.close()
+
+
+CAPS = [2.0 ** -126, 1.0, 64.0, 64.5, 100.0, 1e3, 1e4, 1e6, 1e30, 3.4e38]
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("D,Hq,Hkv,size", [(64, 4, 2, 1.5), (128, 8, 1, 40.0), (80, 6, 6, 1.5), (256, 4, 1, 12.0)], ids=str)
+@pytest.mark.parametrize("biased", [False, True])
+def test_caps_of_all_sizes(fmt, D, Hq, Hkv, size, biased):
+    """What is small beside a cap stays as it is; scores on both sides of half a cap; caps that fp32 cannot multiply."""
+    before, new = np.array([200, 0, 9]), np.array([20, 70, 1])
+    total = before + new
+    p = Pools(fmt, D, Hq, Hkv, total, seed=97)
+    p.fill(total, 98)
+    held = p.held()
+    seq, pos = packed(before, new)
+    q = _q(len(seq), p, 99, size)
+    q[5] = 0
+    slopes = (2.0 ** (-8.0 * np.arange(1, Hq + 1) / Hq)).astype(np.float32) if biased else None
+    last = np.cumsum(new) - 1
+    ql = q[torch.from_numpy(last).cuda()].contiguous()
+    for cap in CAPS:
+        out, lse = _prefill(p, before, new, q, _scores(p, cap, slopes))
+        check_rows(p, q, out, lse, seq, pos, np.zeros(len(seq)), pos + 1, cap, slopes, held=held, tokens=range(0, len(seq), 3), label=f"cap {cap:g}, prompts:")
+        out, lse = _decode(p, total, ql, _scores(p, cap, slopes))
+        check_rows(p, ql, out, lse, np.arange(3), total - 1, np.zeros(3), total, cap, slopes, held=held, label=f"cap {cap:g}, a step:")
+    p.ctx.close()
+
+
+def test_a_small_cap_of_large_scales():
+    """Twice the scale by the cap is beyond fp32: scores of zero stay zero, others saturate."""
+    total = np.array([50])
+    p = Pools("bf16", 64, 4, 2, total, seed=100, scale=1000.0)
+    p.fill(total, 101)
+    q = _q(50, p, 102)
+    q[::3] = 0
+    for cap in (2.0 ** -126, 2.0 ** -120, 5.0):
+        out, lse = _prefill(p, np.array([0]), total, q, _scores(p, cap, None))
+        check_rows(p, q, out, lse, np.zeros(50, dtype=int), np.arange(50), np.zeros(50), np.arange(50) + 1, cap)
+        out, lse = _decode(p, total, q[48:49], _scores(p, cap, None))
+        check_rows(p, q[48:49], out, lse, [0], [49], [0], [50], cap)
     p.ctx.close()

@@ -41,6 +41,8 @@ constexpr float kTau = 8.f;        // the maximum in the exponent is raised when
 constexpr int kRsrc = 0x00020000;
 constexpr int kAgent = 16;         // past the caches that XCDs do not share
 
+__device__ const u32x4 kZeros[kBlockSize] = {};  // a unit of K of a block
+
 template <int F, int NC>
 struct Step {
   static constexpr bool kNarrow = F != kNative;
@@ -308,8 +310,10 @@ __global__ __launch_bounds__(64 * kWaves, decode_scored_waves(F != kNative, NC))
       const char* const at = k_head + at_block(id, blk_stride);
 #pragma unroll
       for (int j = 0; j < Frag::NK; ++j) {
-        const int unit = 4 * j + quad;  // (behind the head vector: its first unit, which meets zeros of Q)
-        const char* const unit_at = at + (kFull || unit * C::kUnit < D ? unit : 0) * 256;
+        // (behind the head vector, where Q is zero: codes of its first unit, which are finite, and zeros in the place of elements, which may not be)
+        const int unit = 4 * j + quad;
+        const bool there = kFull || unit * C::kUnit < D;
+        const char* const unit_at = Frag::kNarrow || there ? at + (there ? unit : 0) * 256 : reinterpret_cast<const char*>(kZeros);
 #pragma unroll
         for (int t = 0; t < kBlocks; ++t) f.k[t][j] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(unit_at + 64 * t));
       }

@@ -1,4 +1,5 @@
-"""Attention with formed scores where it answered wrongly once: batches of fewer tokens than sequences, ranges that leave keys between them, caps far above the scores."""
+"""Attention with formed scores where it answered wrongly once: batches of fewer tokens than sequences, ranges that leave keys between them, caps far above the scores, keys that are
+not finite in a step."""
 import numpy as np
 import pytest
 import torch
@@ -120,4 +121,39 @@ def test_a_small_cap_of_large_scales():
         check_rows(p, q, out, lse, np.zeros(50, dtype=int), np.arange(50), np.zeros(50), np.arange(50) + 1, cap)
         out, lse = _decode(p, total, q[48:49], _scores(p, cap, None))
         check_rows(p, q[48:49], out, lse, [0], [49], [0], [50], cap)
+    p.ctx.close()
+
+
+@pytest.mark.parametrize("D,Hq,Hkv", [(16, 4, 2), (48, 6, 2), (80, 8, 8), (112, 4, 1), (144, 2, 1), (208, 4, 4), (64, 8, 1), (128, 8, 1), (256, 4, 1)], ids=str)
+def test_keys_that_are_not_finite_in_a_step(D, Hq, Hkv):
+    """A key with an infinite channel scores plus or minus infinity: minus has no weight, whatever the head's size; NaN, and plus infinity, make the row NaN; and all of that where prompts have it too."""
+    total = np.array([70, 70, 300, 33, 40, 20])
+    p = Pools("bf16", D, Hq, Hkv, total, seed=103)
+    p.fill(total, 104)
+    k, v = p.logical()
+    q = _q(len(total), p, 105)
+    q[:, :, 3] = 1.0                                  # (the sign of the infinite products)
+    inf = float("inf")
+
+    def put(b, j, channel, x, pool=k):
+        pool[p.table[b, j // 16], :, j % 16, channel] = x
+
+    put(0, 20, 3, -inf)
+    put(1, 69, 3, -inf)
+    put(1, 0, 3, -inf)
+    put(2, 130, 3, inf)
+    put(3, 5, 3, float("nan"))
+    for j in range(40):
+        put(4, j, 3, -inf)                            # (all of them)
+    put(5, 7, D - 1, inf, v)
+    p.put(k, v)
+    pos = total - 1
+    for form in ((0.0, None), (20.0, None), (200.0, None)):
+        out, lse = _decode(p, total, q, _scores(p, *form))
+        if form[0] == 0:
+            assert out[:2].isfinite().all() and out[2:5].isnan().all() and (lse[4] == -inf).all()
+        check_rows(p, q, out, lse, np.arange(6), pos, np.zeros(6), total, *form, tokens=[0, 1, 3, 4, 5], label=f"a step, {form[0]}:")
+        prompt, prompt_lse = _prefill(p, pos, np.ones(6, dtype=int), q, _scores(p, *form))
+        assert torch.equal(prompt.isnan(), out.isnan())
+        check_rows(p, q, prompt, prompt_lse, np.arange(6), pos, np.zeros(6), total, *form, tokens=[0, 1, 3, 4, 5], label=f"prompts, {form[0]}:")
     p.ctx.close()

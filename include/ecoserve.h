@@ -564,13 +564,15 @@ typedef struct {
  * The tokens themselves must already be in the cache.  Tokens at negative positions have no keys.  out and lse are packed; lse may be NULL.
  *
  *   scores    : host, or NULL: Eq. 2 as it is
- *   workspace : dev, 16-byte aligned, of at least the bytes that the function of the same call says (0: NULL is fine); nothing in it is kept from call to call
+ *   workspace : dev, 16-byte aligned, of at least the bytes that the function of the same call says (0: NULL is fine); nothing in it is kept from call to call.
+ *               Prompts: few tokens may take some where many take none; no call of the context takes more than ecoserve_prefill_scored_workspace_most(ctx)
  * Limits: T Hq / Hkv, the rows of a K/V head, below 2^31 - 256; B (max_ctx_len / 32 + 6) below 2^31; others: ECOSERVE_EINVAL.
  * Weights are rounded to bf16 before the product with the values; maxima, sums and lse are fp32.
  * Calls that share a context are ordered (rules at the top): work that is split is counted in the context's merge counters.  Calls that may
  * run at the same time, recorded into graphs or not, need a context and a workspace each.  The options do not concern these calls.
  */
 size_t ecoserve_prefill_scored_workspace_bytes(const ecoserve_ctx* ctx, int32_t B, int32_t T);
+size_t ecoserve_prefill_scored_workspace_most(const ecoserve_ctx* ctx);
 int ecoserve_attn_prefill_scored(ecoserve_ctx* ctx, const ecoserve_cache* cache, const ecoserve_scores* scores, const void* q, int64_t q_row_stride,
                                  const int32_t* cu_q, const int32_t* ctx_before, const int32_t* block_table, int32_t bt_stride, void* out, float* lse,
                                  int32_t B, int32_t T, void* workspace, size_t workspace_bytes, void* stream);

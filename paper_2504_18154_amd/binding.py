@@ -33,7 +33,7 @@ EXPORTS = [
     "ecoserve_debug_prefill_queue_shares",
     "ecoserve_kv_append_rope", "ecoserve_summary_bytes", "ecoserve_kv_summary", "ecoserve_select_workspace_bytes",
     "ecoserve_block_select", "ecoserve_sparse_workspace_bytes", "ecoserve_sparse_workspace_most", "ecoserve_attn_sparse",
-    "ecoserve_cache_scale_bytes", "ecoserve_kv_append_norm", "ecoserve_kv_read", "ecoserve_prefill_scored_workspace_bytes",
+    "ecoserve_cache_scale_bytes", "ecoserve_kv_append_norm", "ecoserve_kv_read", "ecoserve_prefill_scored_workspace_bytes", "ecoserve_prefill_scored_workspace_most",
     "ecoserve_attn_prefill_scored", "ecoserve_decode_scored_workspace_bytes", "ecoserve_attn_decode_scored",
 ]
 ROPE_HALVES, ROPE_ADJACENT = 0, 1
@@ -114,10 +114,11 @@ def _load(path: str = LIB_PATH) -> ctypes.CDLL:
                                             i32, i32, i32, vp]
     lib.ecoserve_kv_read.argtypes = [vp, cache, vp, vp, i64, i32p, i32p, i32p, i32, i32, i32, vp]
     lib.ecoserve_prefill_scored_workspace_bytes.argtypes = [vp, i32, i32]
+    lib.ecoserve_prefill_scored_workspace_most.argtypes = [vp]
     lib.ecoserve_attn_prefill_scored.argtypes = [vp, cache, scores, vp, i64, i32p, i32p, i32p, i32, vp, vp, i32, i32, vp, sz, vp]
     lib.ecoserve_decode_scored_workspace_bytes.argtypes = [vp]
     lib.ecoserve_attn_decode_scored.argtypes = [vp, cache, scores, vp, i64, i32p, i32, i32p, vp, vp, i32, i32, vp, sz, vp]
-    for f in (lib.ecoserve_cache_scale_bytes, lib.ecoserve_prefill_scored_workspace_bytes, lib.ecoserve_decode_scored_workspace_bytes):
+    for f in (lib.ecoserve_cache_scale_bytes, lib.ecoserve_prefill_scored_workspace_bytes, lib.ecoserve_prefill_scored_workspace_most, lib.ecoserve_decode_scored_workspace_bytes):
         f.restype = sz
     lib.ecoserve_debug_validate.argtypes = [vp, i32p, i32p, i32p, i32, i32]
     lib.ecoserve_debug_prefill_queue_shares.argtypes = [vp, ctypes.POINTER(ctypes.c_float)]
@@ -676,6 +677,10 @@ class Context:
 
     def prefill_scored_workspace_bytes(self, B: int, T: int) -> int:
         return int(_lib.ecoserve_prefill_scored_workspace_bytes(self._h, int(B), int(T)))
+
+    def prefill_scored_workspace_most(self) -> int:
+        """Bytes that no attn_prefill_scored of this context exceeds."""
+        return int(_lib.ecoserve_prefill_scored_workspace_most(self._h))
 
     def decode_scored_workspace_bytes(self) -> int:
         return int(_lib.ecoserve_decode_scored_workspace_bytes(self._h))

@@ -617,6 +617,7 @@ size_t ecoserve_prefill_scored_workspace_bytes(const ecoserve_ctx* c, int32_t B,
   if (!c || B <= 0 || T <= 0 || !scored_rows_ok(c, B, T)) return 0;
   return prefill_scored_workspace(c->lay, B, T, c->num_cu);
 }
+size_t ecoserve_prefill_scored_workspace_most(const ecoserve_ctx* c) { return c ? prefill_scored_workspace_most(c->lay, c->num_cu) : 0; }
 
 int ecoserve_attn_prefill_scored(ecoserve_ctx* c, const ecoserve_cache* cache, const ecoserve_scores* scores, const void* q, int64_t q_row_stride, const int32_t* cu_q,
                                  const int32_t* ctx_before, const int32_t* block_table, int32_t bt_stride, void* out, float* lse, int32_t B, int32_t T, void* workspace,

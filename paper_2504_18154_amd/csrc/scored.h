@@ -71,6 +71,8 @@ inline size_t prefill_scored_workspace(const ecoserve_layout& L, int32_t B, int3
   if (splits == 1) return 0;
   return (size_t)splits * prefill_scored_tiles(rows, B, T, L.num_q_heads / L.num_kv_heads) * L.num_kv_heads * prefill_scored_state_floats(rows, L.head_dim) * 4;
 }
+// The largest that is: parts are two workgroups per CU at most, and tiles of 256 rows are never cut.
+inline size_t prefill_scored_workspace_most(const ecoserve_layout& L, int32_t num_cu) { return 2 * (size_t)num_cu * prefill_scored_state_floats(kTileRows, L.head_dim) * 4; }
 
 // decode of a few tokens and prompts (attn_scored_decode.hip, attn_scored_prefill.hip)
 hipError_t launch_decode_scored(const ScoredArgs& a, hipStream_t s);

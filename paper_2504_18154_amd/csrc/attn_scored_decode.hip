@@ -37,7 +37,9 @@ namespace eco {
 namespace {
 
 constexpr float kLowest = -3.0e38f;  // maximum before the first key: below every finite score, and no infinity to be subtracted from one
-constexpr float kTau = 8.f;        // the maximum in the exponent is raised when a score passes it by 2^8: weights reach that, and lose nothing by it
+// The offset in the exponent is put this far above the largest score (log2 units), and again when one passes it: no weight is above 1, so that no sum leaves fp32 for the offset,
+// and weights lose nothing by being small.
+constexpr float kRoom = 8.f;
 constexpr int kRsrc = 0x00020000;
 constexpr int kAgent = 16;         // past the caches that XCDs do not share
 
@@ -164,8 +166,10 @@ __device__ __forceinline__ void add_up(int tid, const float* first_state, int n_
   if (lse_rows && tid < G) lse_rows[tid] = (s_M[tid] + log2f(s_L[tid])) * kLn2;
 }
 
+enum { kPlain, kFormed, kFarCapped };  // scores: scaled, capped (near: softcap.h) or with a bias or both, or capped far above them, with a bias or without
+
 // kFull: the head vector fills the instance's channels.
-template <int F, int NC, bool kForm, int kWaves, bool kFull>
+template <int F, int NC, int kForm, int kWaves, bool kFull>
 __global__ __launch_bounds__(64 * kWaves, decode_scored_waves(F != kNative, NC)) void decode_scored_kernel(const uint16_t* __restrict__ q, int q_row_stride, const char* __restrict__ k_cache,
                                                                  const char* __restrict__ v_cache, const uint8_t* __restrict__ scales,
                                                                  const int32_t* __restrict__ block_table, int bt_stride, const int32_t* __restrict__ ctx_len,
@@ -289,7 +293,7 @@ __global__ __launch_bounds__(64 * kWaves, decode_scored_waves(F != kNative, NC))
     }
     float slope = 0.f;
     int position = 0;
-    if (kForm && slopes) {
+    if (kForm != kPlain && slopes) {
       position = ctx_len[b] - 1;
       if (col < G) slope = slopes[g * G + col] * kLog2e;
     }
@@ -390,13 +394,13 @@ __global__ __launch_bounds__(64 * kWaves, decode_scored_waves(F != kNative, NC))
         for (int w = 0; w < kTokens / 4; ++w) x[4 * w] *= scale_of<0>(by[w]), x[4 * w + 1] *= scale_of<1>(by[w]), x[4 * w + 2] *= scale_of<2>(by[w]), x[4 * w + 3] *= scale_of<3>(by[w]);
       };
       if constexpr (F == kInt8) scaled(f.sk);
-      if constexpr (kForm) {
-        if (cap.kind == kNear) {
-#pragma unroll
-          for (int j = 0; j < kTokens; ++j) x[j] = __builtin_fmaf(2.f * cap.log2e, near_cap(x[j], cap), cap.log2e);
-        } else if (cap.kind == kFar) {
+      if constexpr (kForm != kPlain) {
+        if constexpr (kForm == kFarCapped) {
 #pragma unroll
           for (int j = 0; j < kTokens; ++j) x[j] = far_cap(x[j], cap);
+        } else if (cap.kind == kNear) {
+#pragma unroll
+          for (int j = 0; j < kTokens; ++j) x[j] = __builtin_fmaf(2.f * cap.log2e, near_cap(x[j], cap), cap.log2e);
         } else {
 #pragma unroll
           for (int j = 0; j < kTokens; ++j) x[j] *= scale_log2e;
@@ -412,13 +416,13 @@ __global__ __launch_bounds__(64 * kWaves, decode_scored_waves(F != kNative, NC))
         for (int j = 0; j < kTokens; ++j)
           if (j < first || j >= last) x[j] = -INFINITY;
       }
-      const float c = kForm ? 1.f : scale_log2e;  // (formed scores are in the exp2 domain already)
+      const float c = kForm != kPlain ? 1.f : scale_log2e;  // (formed scores are in the exp2 domain already)
       float top = max3(x[0], x[1], x[2]);
 #pragma unroll
       for (int j = 3; j < kTokens - 1; j += 2) top = max3(top, x[j], x[j + 1]);
       top = across_quads_max(fmaxf(top, x[kTokens - 1])) * c;
-      if (__any(top - m > kTau)) {
-        const float m_new = fmaxf(m, top), alpha = __builtin_amdgcn_exp2f(m - m_new);
+      if (__any(top > m)) {
+        const float m_new = top > m ? top + kRoom : m, alpha = __builtin_amdgcn_exp2f(m - m_new);
         l *= alpha;
 #pragma unroll
         for (int dt = 0; dt < 2 * NC; ++dt) acc[dt] *= alpha;
@@ -539,7 +543,7 @@ __global__ __launch_bounds__(64 * kWaves, decode_scored_waves(F != kNative, NC))
 template <int F, int NC, int kWaves>
 void launch_waves(const ScoredArgs& a, hipStream_t s) {
   const int G = a.Hq / a.Hkv;
-  const bool form = a.softcap > 0.f || a.slopes;
+  const Cap cap = make_cap(a.softcap, a.scale_log2e);
   // states of the wavefronts, or the weights of the pieces when they are added up
   const size_t words = std::max((size_t)kWaves * G * (kPassChannels<NC> + 4), (size_t)G * kScoredMostPieces);
   const size_t lds = (head_words(a.B) + words) * sizeof(uint32_t);
@@ -547,11 +551,16 @@ void launch_waves(const ScoredArgs& a, hipStream_t s) {
   auto go = [&](auto kernel) {
     hipLaunchKernelGGL(kernel, dim3(grid), dim3(64 * kWaves), lds, s, (const uint16_t*)a.q, a.q_row_stride, (const char*)a.k_cache, (const char*)a.v_cache, a.scales,
                        a.block_table, a.bt_stride, a.ctx_before, a.key_begin, a.key_end, a.slopes, (uint16_t*)a.out, a.lse, a.states, a.counters, a.B, a.Hq, a.Hkv, G,
-                       a.D, a.num_cu, make_cap(a.softcap, a.scale_log2e));
+                       a.D, a.num_cu, cap);
   };
   const bool full = a.D == 32 * NC;
-  if (form) full ? go(&decode_scored_kernel<F, NC, true, kWaves, true>) : go(&decode_scored_kernel<F, NC, true, kWaves, false>);
-  else full ? go(&decode_scored_kernel<F, NC, false, kWaves, true>) : go(&decode_scored_kernel<F, NC, false, kWaves, false>);
+  auto with_form = [&](auto kind) {
+    constexpr int kForm = decltype(kind)::value;
+    full ? go(&decode_scored_kernel<F, NC, kForm, kWaves, true>) : go(&decode_scored_kernel<F, NC, kForm, kWaves, false>);
+  };
+  if (cap.kind == kFar) with_form(std::integral_constant<int, kFarCapped>());
+  else if (cap.kind == kNear || a.slopes) with_form(std::integral_constant<int, kFormed>());
+  else with_form(std::integral_constant<int, kPlain>());
 }
 template <int F, int NC>
 void launch_formed(const ScoredArgs& a, hipStream_t s) {

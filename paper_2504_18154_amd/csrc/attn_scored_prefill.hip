@@ -40,7 +40,9 @@ namespace {
 
 constexpr int kKeys = 64;
 constexpr float kLowest = -3.0e38f;  // maximum before the first key: below every finite score, and no infinity to be subtracted from one
-constexpr float kTau = 8.f;          // the maximum in the exponent is raised when a score passes it by 2^8: weights reach that, and lose nothing by it
+// The offset in the exponent is put this far above the largest score (log2 units), and again when one passes it: no weight is above 1, so that no sum leaves fp32 for the offset,
+// and weights lose nothing by being small.
+constexpr float kRoom = 8.f;
 constexpr int kRsrc = 0x00020000;
 constexpr int kAgent = 16;           // past the caches that XCDs do not share
 
@@ -473,8 +475,8 @@ __global__ __launch_bounds__(64 * kWaves, NC == 8 ? 1 : 2) void prefill_scored_k
 #pragma unroll
     for (int i = 1; i < 15; i += 2) top = max3(top, s[1][i], s[1][i + 1]);
     top = __builtin_fmaf(across_halves_max(fmaxf(top, s[1][15])), c, at_zero);
-    if (__any(top - m > kTau)) {
-      const float m_new = fmaxf(m, top), alpha = __builtin_amdgcn_exp2f(m - m_new);
+    if (__any(top > m)) {
+      const float m_new = top > m ? top + kRoom : m, alpha = __builtin_amdgcn_exp2f(m - m_new);
       l *= alpha;
 #pragma unroll
       for (int dt = 0; dt < NC; ++dt) o[dt] *= alpha;

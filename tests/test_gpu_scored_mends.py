@@ -1,5 +1,5 @@
 """Attention with formed scores where it answered wrongly once: batches of fewer tokens than sequences, ranges that leave keys between them, caps far above the scores, keys that are
-not finite in a step."""
+not finite in a step, values near the top of fp32's range."""
 import numpy as np
 import pytest
 import torch
@@ -156,4 +156,34 @@ def test_keys_that_are_not_finite_in_a_step(D, Hq, Hkv):
         prompt, prompt_lse = _prefill(p, pos, np.ones(6, dtype=int), q, _scores(p, *form))
         assert torch.equal(prompt.isnan(), out.isnan())
         check_rows(p, q, prompt, prompt_lse, np.arange(6), pos, np.zeros(6), total, *form, tokens=[0, 1, 3, 4, 5], label=f"prompts, {form[0]}:")
+    p.ctx.close()
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("D,Hq,Hkv", [(64, 8, 4), (128, 8, 4), (80, 8, 8), (256, 4, 4)], ids=str)
+def test_values_near_the_top_of_the_range(fmt, D, Hq, Hkv):
+    """Values of 2^126 at keys whose scores rise, by less than a factor of 2^8 of their weights, from step to step: the weighted means are inside fp32, and so are the sums.
+    (So many sequences that no wavefront has a single step of one, and no prompt's steps are cut.)"""
+    total = 1500 + np.arange(70)
+    p = Pools(fmt, D, Hq, Hkv, total, seed=106, scale=1.0)
+    (k, v), s = p.logical(), p.scales()
+    k, v = torch.zeros_like(k), torch.zeros_like(v)
+    one, big, up = {"bf16": (1.0, 2.0 ** 126, 0), "int8": (64, 64, 120), "e4m3": (0x38, 0x78, 118)}[fmt]   # (the code of 1 or 64, of 64 or 256, and the exponent of the large values' scale)
+    if s is not None:
+        s = np.full_like(s, 127)
+        s[:, :, 0] = 127 - (6 if fmt == "int8" else 0)
+    for b in range(len(total)):
+        for j in (0, 600, total[b] - 1):              # the first key's score is 0, as all others' but the last one's, which is q[0]
+            blk, at = p.table[b, j // 16], j % 16
+            v[blk, :, at, ::2] = big
+            if s is not None:
+                s[blk, :, 1, at] = 127 + up
+        k[blk, :, at, 0] = one
+    p.put(k, v, *((s[:, :, 0], s[:, :, 1]) if s is not None else ()))
+    q = _q(len(total), p, 108)
+    q[:, :, 0] = 5.0                                  # 7.2 in the exponent
+    held = p.held()
+    for what, (out, lse) in (("a step:", _decode(p, total, q)), ("prompts:", _prefill(p, total - 1, np.ones(len(total), dtype=int), q))):
+        assert out.isfinite().all(), what
+        check_rows(p, q, out, lse, np.arange(len(total)), total - 1, np.zeros(len(total)), total, held=held, tokens=range(0, len(total), 9), label=what)
     p.ctx.close()

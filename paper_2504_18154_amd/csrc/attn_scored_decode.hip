@@ -17,8 +17,9 @@
 // beginning of another; a piece's steps are dealt in turn to the workgroup's wavefronts.  A piece that is a whole (sequence, head) writes the result; otherwise
 // its state goes to the workspace, and the last workgroup of the (sequence, head) to arrive adds them up in the order of the keys.
 //
-// Weights are rounded to bf16 for the second product (2^-9 of each, unbiased: the result's own rounding is as large); maxima, sums and the
-// log-sum-exp are fp32, from the weights before that rounding.
+// Weights are two bf16 numbers each, 16 bits, as in the other calls for a token over this cache; maxima, sums and the log-sum-exp are fp32, from the weights as they were.  The second parts
+// ride in the eight columns that groups of up to eight heads leave (their columns repeat the heads, so a lane has both parts in hand and takes one), and cost a few vector instructions;
+// larger groups take a product for each part (64 heads on 4 of 128, 32 x 16 k ... 131 k tokens over e4m3: 430 us, with weights of 8 bits 408; one of 20 000: 24.7 and 22.0).
 //
 // Measured: 32 contexts of 16 k ... 131 k tokens, 64 heads on 8 of 128, e4m3: 786 us (5.03 GB, 6.4 TB/s; reads reach 7.0).  64 of 100 ... 4000 tokens, 40 heads on 8: 57 us
 // (4.7 TB/s: four of five heads are cut, a piece costs 5 us of latency, and its workgroup's neighbour on the CU covers half of it).  One of 20 000 tokens, int8: 20.1 us, of
@@ -168,9 +169,13 @@ __device__ __forceinline__ void add_up(int tid, const float* first_state, int n_
 
 enum { kPlain, kFormed, kFarCapped };  // scores: scaled, capped (near: softcap.h) or with a bias or both, or capped far above them, with a bias or without
 
+// Groups of up to kHalf heads: columns kHalf .. 2 kHalf - 1 of the products repeat the heads, and have the weights' second parts where the first columns have the first ones.
+constexpr int kHalf = 8;
+
 // kFull: the head vector fills the instance's channels.
-template <int F, int NC, int kForm, int kWaves, bool kFull>
-__global__ __launch_bounds__(64 * kWaves, decode_scored_waves(F != kNative, NC)) void decode_scored_kernel(const uint16_t* __restrict__ q, int q_row_stride, const char* __restrict__ k_cache,
+// kWide: groups of more than kHalf heads, whose weights' parts are products of their own.
+template <int F, int NC, int kForm, int kWaves, bool kFull, bool kWide>
+__global__ __launch_bounds__(64 * kWaves, kWaves == 8 ? 2 : decode_scored_waves(F != kNative, NC, kWide)) void decode_scored_kernel(const uint16_t* __restrict__ q, int q_row_stride, const char* __restrict__ k_cache,
                                                                  const char* __restrict__ v_cache, const uint8_t* __restrict__ scales,
                                                                  const int32_t* __restrict__ block_table, int bt_stride, const int32_t* __restrict__ ctx_len,
                                                                  const int32_t* __restrict__ key_begin, const int32_t* __restrict__ key_end,
@@ -282,7 +287,7 @@ __global__ __launch_bounds__(64 * kWaves, decode_scored_waves(F != kNative, NC))
     // ---- query rows: B operand, channels in the order of the keys' units
     bf16x8 qf[NC];
     {
-      const int l_ = here_lane(lane), col_ = l_ & 15, quad_ = l_ >> 4, D_ = here(D);
+      const int l_ = here_lane(lane), col_ = l_ & (kWide ? 15 : kHalf - 1), quad_ = l_ >> 4, D_ = here(D);
       const uint16_t* const q_row = q + (size_t)b * q_row_stride + ((size_t)g * G + col_) * D_;
 #pragma unroll
       for (int c = 0; c < NC; ++c) {
@@ -295,7 +300,7 @@ __global__ __launch_bounds__(64 * kWaves, decode_scored_waves(F != kNative, NC))
     int position = 0;
     if (kForm != kPlain && slopes) {
       position = ctx_len[b] - 1;
-      if (col < G) slope = slopes[g * G + col] * kLog2e;
+      if (const int h = kWide ? col : col & (kHalf - 1); h < G) slope = slopes[g * G + h] * kLog2e;
     }
 
     // ---- loads
@@ -347,6 +352,7 @@ __global__ __launch_bounds__(64 * kWaves, decode_scored_waves(F != kNative, NC))
     auto process = [&](Frag& f, int i, auto more, auto edges) {
       constexpr bool kEdge = decltype(edges)::value;
       constexpr int kTokens = Frag::kTokens;
+      constexpr bool kOpen = !Frag::kNarrow;
       const int k0 = (s_first + wave + kWaves * i) << Frag::kShift;
       f32x4 s[kBlocks];
 #pragma unroll
@@ -436,21 +442,36 @@ __global__ __launch_bounds__(64 * kWaves, decode_scored_waves(F != kNative, NC))
       }
       l += sum[0] + sum[1];
       if constexpr (Frag::kNarrow) scaled(f.sv);
-      bf16x8 p[kBlocks / 2];
 #pragma unroll
-      for (int h = 0; h < kBlocks / 2; ++h)
-        p[h] = __builtin_bit_cast(bf16x8, u32x4{pack_bf16x2(x[8 * h], x[8 * h + 1]), pack_bf16x2(x[8 * h + 2], x[8 * h + 3]), pack_bf16x2(x[8 * h + 4], x[8 * h + 5]),
-                                                pack_bf16x2(x[8 * h + 6], x[8 * h + 7])});
+      for (int h = 0; h < kBlocks / 2; ++h) {
+        u32x4 high, low;
 #pragma unroll
-      for (int h = 0; h < kBlocks / 2; ++h)
+        for (int i = 0; i < 4; ++i) {
+          float &a = x[8 * h + 2 * i], &b = x[8 * h + 2 * i + 1];
+          high[i] = first_parts<kOpen>(a, b);
+          if constexpr (kWide) {
+            low[i] = second_parts<kOpen>(a, b, high[i]);
+          } else {
+            // (the columns' mask is made here: held through the loop, or with both parts made before one is taken, registers spilled: 64 x 100 ... 4000 tokens 74 us for 57)
+            const uint32_t second = (uint32_t)((here_lane(lane) << 28) >> 31);
+            if constexpr (kOpen) {
+              high[i] = second ? second_parts<kOpen>(a, b, high[i]) : high[i];
+            } else {
+              a -= __uint_as_float(high[i] << 16 & second), b -= __uint_as_float(high[i] & 0xffff0000u & second);
+              high[i] = pack_bf16x2(a, b);
+            }
+          }
+        }
 #pragma unroll
         for (int dt = 0; dt < 2 * NC; ++dt) {
           if (Frag::kNarrow && dt % 2 == 0) __builtin_amdgcn_sched_barrier(0);
           bf16x8 a;
           if constexpr (Frag::kNarrow) a = codes_to_bf16x8<F>(f.v[dt][0][2 * h], f.v[dt][0][2 * h + 1], 1.f);
           else a = __builtin_bit_cast(bf16x8, f.v[dt][h % Frag::NV]);
-          acc[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, p[h], acc[dt], 0, 0, 0);
+          acc[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, __builtin_bit_cast(bf16x8, high), acc[dt], 0, 0, 0);
+          if constexpr (kWide) acc[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, __builtin_bit_cast(bf16x8, low), acc[dt], 0, 0, 0);
         }
+      }
       __builtin_amdgcn_sched_barrier(0);
       if constexpr (decltype(more)::value) {
         load_v(f, next_v);
@@ -497,6 +518,14 @@ __global__ __launch_bounds__(64 * kWaves, decode_scored_waves(F != kNative, NC))
         s_L[col_] = sum;
       }
     }
+    if constexpr (!kWide) {
+      // the weights' second parts
+      auto turned = [](float x) { return __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(x), 0x128, 0xf, 0xf, true)); };  // row_ror:8
+#pragma unroll
+      for (int dt = 0; dt < 2 * NC; ++dt)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc[dt][i] += turned(acc[dt][i]);
+    }
     // (a workgroup has two states at most: of the piece that it ends, and of the one that it begins and does not end)
     float* const state = states + (size_t)(2 * wg + (p0 == 0 ? 1 : 0)) * G_ * words_;
     const __amdgpu_buffer_rsrc_t to_state = __builtin_amdgcn_make_buffer_rsrc(state, 0, G_ * words_ * 4, kRsrc);
@@ -540,14 +569,14 @@ __global__ __launch_bounds__(64 * kWaves, decode_scored_waves(F != kNative, NC))
   }
 }
 
-template <int F, int NC, int kWaves>
+template <int F, int NC, int kWaves, bool kWide>
 void launch_waves(const ScoredArgs& a, hipStream_t s) {
   const int G = a.Hq / a.Hkv;
   const Cap cap = make_cap(a.softcap, a.scale_log2e);
   // states of the wavefronts, or the weights of the pieces when they are added up
   const size_t words = std::max((size_t)kWaves * G * (kPassChannels<NC> + 4), (size_t)G * kScoredMostPieces);
   const size_t lds = (head_words(a.B) + words) * sizeof(uint32_t);
-  const int grid = (kWaves == 8 ? 1 : decode_scored_waves(F != kNative, NC)) * a.num_cu;
+  const int grid = (kWaves == 8 ? 1 : decode_scored_waves(F != kNative, NC, kWide)) * a.num_cu;
   auto go = [&](auto kernel) {
     hipLaunchKernelGGL(kernel, dim3(grid), dim3(64 * kWaves), lds, s, (const uint16_t*)a.q, a.q_row_stride, (const char*)a.k_cache, (const char*)a.v_cache, a.scales,
                        a.block_table, a.bt_stride, a.ctx_before, a.key_begin, a.key_end, a.slopes, (uint16_t*)a.out, a.lse, a.states, a.counters, a.B, a.Hq, a.Hkv, G,
@@ -556,7 +585,7 @@ void launch_waves(const ScoredArgs& a, hipStream_t s) {
   const bool full = a.D == 32 * NC;
   auto with_form = [&](auto kind) {
     constexpr int kForm = decltype(kind)::value;
-    full ? go(&decode_scored_kernel<F, NC, kForm, kWaves, true>) : go(&decode_scored_kernel<F, NC, kForm, kWaves, false>);
+    full && !kWide ? go(&decode_scored_kernel<F, NC, kForm, kWaves, !kWide, kWide>) : go(&decode_scored_kernel<F, NC, kForm, kWaves, false, kWide>);
   };
   if (cap.kind == kFar) with_form(std::integral_constant<int, kFarCapped>());
   else if (cap.kind == kNear || a.slopes) with_form(std::integral_constant<int, kFormed>());
@@ -564,10 +593,11 @@ void launch_waves(const ScoredArgs& a, hipStream_t s) {
 }
 template <int F, int NC>
 void launch_formed(const ScoredArgs& a, hipStream_t s) {
+  const bool wide = a.Hq / a.Hkv > kHalf;
   if constexpr (F != kNative && NC <= 4) {
-    if (decode_scored_short((int64_t)a.B * a.Hkv * ((a.max_ctx_len + 63) / 64 + kPieceCost), true, NC, a.num_cu)) return launch_waves<F, NC, 8>(a, s);
+    if (decode_scored_short((int64_t)a.B * a.Hkv * ((a.max_ctx_len + 63) / 64 + kPieceCost), true, NC, a.num_cu)) return wide ? launch_waves<F, NC, 8, true>(a, s) : launch_waves<F, NC, 8, false>(a, s);
   }
-  launch_waves<F, NC, 4>(a, s);
+  wide ? launch_waves<F, NC, 4, true>(a, s) : launch_waves<F, NC, 4, false>(a, s);
 }
 
 template <int F>

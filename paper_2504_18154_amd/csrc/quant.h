@@ -62,6 +62,18 @@ __device__ __forceinline__ bf16x8 codes_to_bf16x8(uint32_t a, uint32_t b, float 
   return __builtin_bit_cast(bf16x8, u32x4{x[0], x[1], y[0], y[1]});
 }
 
+// A pair of weights as two bf16 numbers each, 16 bits in all: the first ones, and what they leave.  kOpen: values may be infinite, and the product of an infinity with a part of 0, or a
+// sum of infinities of either sign, would be NaN: no part is negative then, and the second one is not 0 (of weights from 2^-66 on).
+template <bool kOpen>
+__device__ __forceinline__ uint32_t first_parts(float a, float b) {
+  return kOpen ? __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u) : pack_bf16x2(a, b);
+}
+template <bool kOpen>
+__device__ __forceinline__ uint32_t second_parts(float a, float b, uint32_t first) {
+  const float s = a - __uint_as_float(first << 16), t = b - __uint_as_float(first & 0xffff0000u);
+  return kOpen ? pack_bf16x2(__builtin_fmaf(a, 0x1p-60f, s), __builtin_fmaf(b, 0x1p-60f, t)) : pack_bf16x2(s, t);
+}
+
 // The scale byte of a row with largest magnitude `most` (NaN and infinity: 255), and the factor 2^-e of its codes.
 template <int F>
 __device__ __forceinline__ uint32_t scale_byte(float most) {

@@ -41,13 +41,14 @@ constexpr int32_t kScoredMostPieces = 256;  // of a (sequence, K/V head)
 constexpr int32_t kLeastSteps = 8;          // of a share
 constexpr int32_t kShortShare = 16;         // (see the kernel)
 constexpr int32_t kPieceCost = 4;           // units in front of a (sequence, K/V head)'s steps
-// Workgroups of four wavefronts that a CU holds, by the registers of the kernel's instances (chunks: of 32 channels).
-constexpr int32_t decode_scored_waves(bool narrow, int32_t chunks) { return chunks == 8 || (chunks == 4 && !narrow) ? 1 : 2; }
+// Workgroups of four wavefronts that a CU holds, by the registers of the kernel's instances (chunks: of 32 channels; wide: groups of more than eight heads.  Those over codes,
+// 64 x 100 ... 4000 tokens, 64 heads on 4 of 128: 48 us with one, whose registers hold all; spilled, two were behind it).
+constexpr int32_t decode_scored_waves(bool narrow, int32_t chunks, bool wide) { return chunks == 8 || (chunks == 4 && (!narrow || wide)) ? 1 : 2; }
 // Short batches over coded caches, a CU's share of which one workgroup takes: it has eight wavefronts, and twice as many bytes on their way.  One sequence of
 // 20 000 tokens: 22.3 us with four, 20.7 with eight.  (Long ones leave no difference between two workgroups of four and one of eight but their barriers.)
 inline bool decode_scored_short(int64_t steps, bool narrow, int32_t chunks, int32_t num_cu) { return narrow && chunks <= 4 && steps <= (int64_t)kShortShare * num_cu; }
 // A workgroup cuts two (sequence, K/V head)s at most.
-constexpr int64_t decode_scored_states(int32_t chunks, int32_t num_cu) { return 2 * (int64_t)decode_scored_waves(true, chunks) * num_cu; }
+constexpr int64_t decode_scored_states(int32_t chunks, int32_t num_cu) { return 2 * (int64_t)decode_scored_waves(true, chunks, false) * num_cu; }
 inline size_t decode_scored_workspace(const ecoserve_layout& L, int32_t num_cu) {
   return (size_t)decode_scored_states(scored_chunks(L.head_dim), num_cu) * (L.num_q_heads / L.num_kv_heads) * scored_state_words(L.head_dim) * 4;
 }

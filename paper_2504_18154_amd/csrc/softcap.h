@@ -38,7 +38,7 @@ __device__ __forceinline__ float near_cap(float qk, const Cap& cap) { return __b
 // Far caps: the score of a product q.k.  (One behind the other: all of a step's side by side would take the registers of others.)
 __device__ __forceinline__ float far_cap(float qk, const Cap& cap) {
   const float x = qk * cap.scale_log2e, u = x * cap.in, u2 = u * u;
-  float p = -929569.f / 638512875;
+  float p = -929569.f / 638512875.f;
   p = __builtin_fmaf(p, u2, 21844.f / 6081075);
   p = __builtin_fmaf(p, u2, -1382.f / 155925);
   p = __builtin_fmaf(p, u2, 62.f / 2835);

@@ -1,10 +1,12 @@
 """Attention with formed scores where it answered wrongly once: batches of fewer tokens than sequences, ranges that leave keys between them, caps far above the scores, keys that are
-not finite in a step, values near the top of fp32's range."""
+not finite in a step, values near the top of fp32's range, weights of fewer bits than those of
+the calls without forms."""
 import numpy as np
 import pytest
 import torch
 
-from tests.scored_util import Pools, check_rows, packed
+from oracle import scored_oracle as so
+from tests.scored_util import HALF, Pools, check_rows, packed
 from tests.test_gpu_scored import FORMATS, _decode, _prefill, _q, _scores
 
 pytestmark = pytest.mark.gpu
@@ -153,6 +155,7 @@ def test_keys_that_are_not_finite_in_a_step(D, Hq, Hkv):
         if form[0] == 0:
             assert out[:2].isfinite().all() and out[2:5].isnan().all() and (lse[4] == -inf).all()
         check_rows(p, q, out, lse, np.arange(6), pos, np.zeros(6), total, *form, tokens=[0, 1, 3, 4, 5], label=f"a step, {form[0]}:")
+        assert (out[5, :, D - 1] == inf).all() and out[5, :, :D - 1].isfinite().all()
         prompt, prompt_lse = _prefill(p, pos, np.ones(6, dtype=int), q, _scores(p, *form))
         assert torch.equal(prompt.isnan(), out.isnan())
         check_rows(p, q, prompt, prompt_lse, np.arange(6), pos, np.zeros(6), total, *form, tokens=[0, 1, 3, 4, 5], label=f"prompts, {form[0]}:")
@@ -186,4 +189,33 @@ def test_values_near_the_top_of_the_range(fmt, D, Hq, Hkv):
     for what, (out, lse) in (("a step:", _decode(p, total, q)), ("prompts:", _prefill(p, total - 1, np.ones(len(total), dtype=int), q))):
         assert out.isfinite().all(), what
         check_rows(p, q, out, lse, np.arange(len(total)), total - 1, np.zeros(len(total)), total, held=held, tokens=range(0, len(total), 9), label=what)
+    p.ctx.close()
+
+
+def _check_bits(p, q, out, seq, pos, cap, slopes, tokens, label):
+    """Within weights of 16 bits (a part that is cut or rounded leaves less than 2^-7 of a weight, half a step of which is 2^-9), the result's rounding, and what fp32 leaves."""
+    keys, vals = p.held()
+    got, qh = out.double().cpu().numpy(), q.double().cpu().numpy()
+    for t in tokens:
+        for g in range(p.Hkv):
+            heads, n = slice(g * p.G, g * p.G + p.G), int(pos[t]) + 1
+            want, _, size, off = so.attend(qh[t, heads], p.rows(keys, seq[t], g, n), p.rows(vals, seq[t], g, n), np.arange(n), int(pos[t]), p.scale, cap, None if slopes is None else slopes[heads])
+            tol = size * (2.0 ** -16 + 2 * off[:, None] + (n + 64) * 2.0 ** -24) + np.abs(want) * HALF
+            err = np.abs(got[t, heads] - want)
+            assert (err <= tol).all(), f"{label}: token {t}, K/V head {g}: {np.max(err / tol):.2f} of the bound"
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("D,Hq,Hkv", [(64, 8, 2), (128, 5, 1), (128, 16, 2), (80, 3, 3), (48, 16, 1), (112, 9, 1), (128, 12, 1), (256, 4, 2), (256, 16, 1), (144, 7, 1)], ids=str)
+def test_weights_keep_sixteen_bits_in_a_step(fmt, D, Hq, Hkv):
+    """Groups of one head to sixteen, contexts of a few tokens to ones that are cut."""
+    total = np.array([3, 10, 40, 64, 200, 1000, 3000])
+    p = Pools(fmt, D, Hq, Hkv, total, seed=109)
+    p.fill(total, 110)
+    q = _q(len(total), p, 111, 0.4)
+    slopes = (0.1 * 2.0 ** (-8.0 * np.arange(1, Hq + 1) / Hq)).astype(np.float32)
+    for cap, sl in ((0.0, None), (5.0, None), (0.0, slopes), (200.0, slopes)):
+        out, lse = _decode(p, total, q, _scores(p, cap, sl))
+        check_rows(p, q, out, lse, np.arange(len(total)), total - 1, np.zeros(len(total)), total, cap, sl)
+        _check_bits(p, q, out, np.arange(len(total)), total - 1, cap, sl, range(len(total)), f"cap {cap}, slopes {sl is not None}")
     p.ctx.close()

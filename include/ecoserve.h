@@ -567,7 +567,8 @@ typedef struct {
  *   workspace : dev, 16-byte aligned, of at least the bytes that the function of the same call says (0: NULL is fine); nothing in it is kept from call to call.
  *               Prompts: few tokens may take some where many take none; no call of the context takes more than ecoserve_prefill_scored_workspace_most(ctx)
  * Limits: T Hq / Hkv, the rows of a K/V head, below 2^31 - 256; B (max_ctx_len / 32 + 6) below 2^31; others: ECOSERVE_EINVAL.
- * Weights keep 16 bits in the product with the values in steps and are rounded to bf16, 8 bits, in prompts; none is above 1.  Maxima, sums and lse are fp32.
+ * Weights keep 16 bits in the product with the values in steps, and in prompts over ECOSERVE_CACHE_LAYOUT with head_dim other than 128; in other prompts they are rounded to bf16, 8 bits.
+ * None is above 1.  Maxima, sums and lse are fp32.
  * Calls that share a context are ordered (rules at the top): work that is split is counted in the context's merge counters.  Calls that may
  * run at the same time, recorded into graphs or not, need a context and a workspace each.  The options do not concern these calls.
  */

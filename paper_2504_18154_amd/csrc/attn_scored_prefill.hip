@@ -19,7 +19,10 @@
 // Values that are not finite must not reach rows that do not see them (0 times NaN).  Codes: such a row is coded as zeros, its scale byte says 255, and rows that
 // see it are given NaN at the end.  bf16: where a result is not finite and a key that the row does not see may be why, it is taken again over those that it sees.
 //
-// Weights are rounded to bf16 for the second product (2^-9 of each, unbiased); maxima, sums and the log-sum-exp are fp32, from the weights before that.
+// Weights are rounded to bf16 for the second product (2^-9 of each, unbiased) where the cache's codes, of 4 and 7 bits, are coarser, and in heads of 128, as in the other call for prompts of
+// those; over bf16 caches of other heads, where that call holds more, they are two bf16 numbers, 16 bits, and products of their own (us with one part and with two: 4 x 4096 tokens, 8 heads on 1 of
+// 256 over bf16 389 and 505, 8 on 8 of 80 163 and 208;  what was not taken: over e4m3 446 and 557, two of 8192, 64 heads on 8 of 128 2190 and 2990).  Maxima, sums and the log-sum-exp are
+// fp32, from the weights as they were.
 //
 // Measured, 64 heads on 8 of 128: two prompts of 8192 tokens over e4m3 2140 us (1028 TFLOP/s; a library product of 8192^3 reaches 1220), over bf16 2065; a step of
 // 64 keys is 200 vector instructions beside 32 matrix ones of a wavefront, the units are busy 46 and 45% of the time, LDS has no bank conflicts, and the clock gives
@@ -60,10 +63,11 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   return r;
 }
 
-template <int F, int NC, int kWaves>
+template <int F, int NC, bool kFull, int kWaves>
 struct Tile {
   static constexpr int kThreads = 64 * kWaves, kRows = 32 * kWaves;  // of a workgroup
   static constexpr bool kNarrow = F != kNative;
+  static constexpr bool kTwo = !kNarrow && !(NC == 4 && kFull);     // weights in two parts
   static constexpr int kD = 32 * NC;                                // channels that the instance holds
   static constexpr int kUnits = kD / 8;                             // of 8 channels
   static constexpr int kKBytes = kUnits * kKeys * 16;
@@ -199,7 +203,7 @@ __global__ __launch_bounds__(64 * kWaves, NC == 8 ? 1 : 2) void prefill_scored_k
     const int32_t* __restrict__ key_begin, const int32_t* __restrict__ key_end, uint16_t* __restrict__ out, float* __restrict__ lse, float* states,
     uint32_t* counters, int B, int Hq, int Hkv, int G, Divisor div_g, Divisor div_hkv, int D, int units, Form form) {
   typedef Cached<F> C;
-  typedef Tile<F, NC, kWaves> W;
+  typedef Tile<F, NC, kFull, kWaves> W;
   __shared__ __attribute__((aligned(16))) char s_k[W::kBuffers][W::kKBytes], s_v[W::kBuffers][W::kVBytes];
   __shared__ int s_lo[kWaves], s_hi[kWaves], s_order, s_bad[2], s_row_lo[W::kRows], s_row_hi[W::kRows];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 31, half = lane >> 5;
@@ -483,20 +487,20 @@ __global__ __launch_bounds__(64 * kWaves, NC == 8 ? 1 : 2) void prefill_scored_k
       m = m_new;
     }
     const float shift = at_zero - m;
-    bf16x8 p[4];
+    u32x4 p[4];
+    [[maybe_unused]] u32x4 second[4];
     float sums[2] = {0.f, 0.f};
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
-      u32x4 w;
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const int i = 8 * (u & 1) + 2 * e;
         const float a = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u >> 1][i], c, shift)), b = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u >> 1][i + 1], c, shift));
         sums[0] += a;
         sums[1] += b;
-        w[e] = pack_bf16x2(a, b);
+        p[u][e] = first_parts<W::kTwo>(a, b);
+        if constexpr (W::kTwo) second[u][e] = second_parts<true>(a, b, p[u][e]);
       }
-      p[u] = __builtin_bit_cast(bf16x8, w);
     }
     l += sums[0] + sums[1];
 #pragma unroll
@@ -504,7 +508,8 @@ __global__ __launch_bounds__(64 * kWaves, NC == 8 ? 1 : 2) void prefill_scored_k
 #pragma unroll
       for (int dt = 0; dt < NC; ++dt) {
         const bf16x8 a = *reinterpret_cast<const bf16x8*>(vb + 2 * u * W::kOctet + 32 * dt * 16);
-        o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, p[u], o[dt], 0, 0, 0);
+        o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, __builtin_bit_cast(bf16x8, p[u]), o[dt], 0, 0, 0);
+        if constexpr (W::kTwo) o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, __builtin_bit_cast(bf16x8, second[u]), o[dt], 0, 0, 0);
       }
     if (W::kNarrow && s_bad[j & 1] == j + 1) {
       // a value's scale says NaN: rows that see it are NaN

@@ -219,3 +219,29 @@ def test_weights_keep_sixteen_bits_in_a_step(fmt, D, Hq, Hkv):
         check_rows(p, q, out, lse, np.arange(len(total)), total - 1, np.zeros(len(total)), total, cap, sl)
         _check_bits(p, q, out, np.arange(len(total)), total - 1, cap, sl, range(len(total)), f"cap {cap}, slopes {sl is not None}")
     p.ctx.close()
+
+
+@pytest.mark.parametrize("D,Hq,Hkv", [(64, 8, 2), (16, 3, 1), (80, 3, 3), (48, 16, 1), (112, 9, 1), (256, 4, 2), (144, 7, 1)], ids=str)
+@pytest.mark.parametrize("few", [False, True])
+def test_weights_keep_sixteen_bits_in_prompts(D, Hq, Hkv, few):
+    """Over bf16 caches of heads other than 128; behind contexts that are cut too; an infinite value is one in the rows that see it."""
+    before, new = (np.array([1000, 0]), np.array([7, 3])) if few else (np.array([30, 0, 100]), np.array([60, 90, 1]))
+    total = before + new
+    p = Pools("bf16", D, Hq, Hkv, total, seed=112)
+    p.fill(total, 113)
+    seq, pos = packed(before, new)
+    q = _q(len(seq), p, 114, 0.4)
+    slopes = (0.1 * 2.0 ** (-8.0 * np.arange(1, Hq + 1) / Hq)).astype(np.float32)
+    for cap, sl in ((0.0, None), (5.0, None), (0.0, slopes), (200.0, slopes)):
+        out, lse = _prefill(p, before, new, q, _scores(p, cap, sl))
+        check_rows(p, q, out, lse, seq, pos, np.zeros(len(seq)), pos + 1, cap, sl)
+        _check_bits(p, q, out, seq, pos, cap, sl, range(0, len(seq), 3), f"cap {cap}, slopes {sl is not None}")
+    k, v = p.logical()
+    v[p.table[0, 0], :, 9, 5] = float("inf")
+    p.put(k, v)
+    out, lse = _prefill(p, before, new, q)
+    row = torch.from_numpy((seq == 0) & (pos >= 9)).cuda()
+    assert (out[row][..., 5] == float("inf")).all() and out[~row].isfinite().all() and lse.isfinite().all()
+    out[..., 5] = 0
+    assert out.isfinite().all()
+    p.ctx.close()

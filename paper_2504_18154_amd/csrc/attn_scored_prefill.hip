@@ -21,7 +21,7 @@
 //
 // Weights are rounded to bf16 for the second product (2^-9 of each, unbiased) where the cache's codes, of 4 and 7 bits, are coarser, and in heads of 128, as in the other call for prompts of
 // those; over bf16 caches of other heads, where that call holds more, they are two bf16 numbers, 16 bits, and products of their own (us with one part and with two: 4 x 4096 tokens, 8 heads on 1 of
-// 256 over bf16 389 and 505, 8 on 8 of 80 163 and 208;  what was not taken: over e4m3 446 and 557, two of 8192, 64 heads on 8 of 128 2190 and 2990).  Maxima, sums and the log-sum-exp are
+// 256 over bf16 389 and 475, 8 on 8 of 80 163 and 208;  what was not taken: over e4m3 446 and 557, two of 8192, 64 heads on 8 of 128 2190 and 2990).  Maxima, sums and the log-sum-exp are
 // fp32, from the weights as they were.
 //
 // Measured, 64 heads on 8 of 128: two prompts of 8192 tokens over e4m3 2140 us (1028 TFLOP/s; a library product of 8192^3 reaches 1220), over bf16 2065; a step of
@@ -415,7 +415,7 @@ __global__ __launch_bounds__(64 * kWaves, NC == 8 ? 1 : 2) void prefill_scored_k
   const int krow = (col & 0x13) | ((col & 4) << 1) | ((col & 8) >> 1);
   const int a_k_off = (half * kKeys + krow) * 16, a_v_off = half * W::kOctet + col * 16;
 
-  auto step = [&](int j) __attribute__((always_inline)) {
+  auto step = [&](int j, auto) {
     const char* const kb = s_k[W::kBuffers == 2 ? j & 1 : 0] + a_k_off;
     const char* const vb = s_v[W::kBuffers == 2 ? j & 1 : 0] + a_v_off;
     f32x16 s[2];
@@ -520,6 +520,8 @@ __global__ __launch_bounds__(64 * kWaves, NC == 8 ? 1 : 2) void prefill_scored_k
     }
   };
 
+  // (a step is taken in where it is called, by word where there are two such places; where there is one the compiler does so by itself, after it has seen to the step alone: 4 x 4096 tokens, 8 heads on 1
+  // of 256 over e4m3, 480 us by word and 445)
   auto walk = [&](auto gapped) __attribute__((always_inline)) {
     load_ids(j0, gapped);
     load();
@@ -535,7 +537,7 @@ __global__ __launch_bounds__(64 * kWaves, NC == 8 ? 1 : 2) void prefill_scored_k
         // (of eight wavefronts that turn codes into operands, four do so first and four last, so that a SIMD's two are not at the same thing: 2170 and 2140 us of
         // two prompts of 8192 tokens; bf16 is only copied, and better all at once)
         const bool first = kWaves == 4 || !W::kNarrow || wave < 4;
-        if (!first && j >= wj0 && j < wj1) step(j);
+        if (!first && j >= wj0 && j < wj1) [[clang::always_inline]] step(j, gapped);
         if (j + 1 < j1) {
           store(j + 1, gapped);
           if (j + 2 < j1) {
@@ -543,10 +545,10 @@ __global__ __launch_bounds__(64 * kWaves, NC == 8 ? 1 : 2) void prefill_scored_k
             if (j + 3 < j1) load_ids(j + 3, gapped);
           }
         }
-        if (first && j >= wj0 && j < wj1) step(j);
+        if (first && j >= wj0 && j < wj1) [[clang::always_inline]] step(j, gapped);
         __syncthreads();
       } else {
-        if (j >= wj0 && j < wj1) step(j);
+        if (j >= wj0 && j < wj1) step(j, gapped);
         __syncthreads();
         if (j + 1 < j1) {
           store(j + 1, gapped);

@@ -524,7 +524,7 @@ typedef struct {
  *
  *   cache : host struct;  norm : host, or NULL: no norm;  rope : host, or NULL: no rotation (inv_freq and positions are not read)
  *   everything else, tokens at negative positions among it, as in ecoserve_kv_append_rope.
- * K and V alone, neither normed nor rotated, is allowed: the append of a quantised cache.
+ * K and V alone, neither normed nor rotated, is allowed: the append of a quantised cache.  T + 32 B below 2^28; others: ECOSERVE_EINVAL.
  */
 int ecoserve_kv_append_norm(ecoserve_ctx* ctx, const ecoserve_cache* cache, const ecoserve_norm* norm, const ecoserve_rope* rope, const double* inv_freq,
                             const int32_t* positions, const void* q, int64_t q_row_stride, void* q_out, int64_t q_out_row_stride, const void* k_new,
@@ -537,6 +537,7 @@ int ecoserve_kv_append_norm(ecoserve_ctx* ctx, const ecoserve_cache* cache, cons
  *   cu          : dev, int32[B+1], prefix sums of the counts, cu[B] = T
  *   first       : dev, int32[B]; tokens at negative positions are not read, their rows left alone
  *   k_rows, v_rows : dev, E[T][Hkv][D], rows row_stride elements apart (rules of the strided calls), 16-byte aligned; one of them may be NULL
+ * T + 32 B below 2^28; others: ECOSERVE_EINVAL.
  */
 int ecoserve_kv_read(ecoserve_ctx* ctx, const ecoserve_cache* cache, void* k_rows, void* v_rows, int64_t row_stride, const int32_t* cu,
                      const int32_t* first, const int32_t* block_table, int32_t bt_stride, int32_t B, int32_t T, void* stream);
@@ -566,7 +567,7 @@ typedef struct {
  *   scores    : host, or NULL: Eq. 2 as it is
  *   workspace : dev, 16-byte aligned, of at least the bytes that the function of the same call says (0: NULL is fine); nothing in it is kept from call to call.
  *               Prompts: few tokens may take some where many take none; no call of the context takes more than ecoserve_prefill_scored_workspace_most(ctx)
- * Limits: T Hq / Hkv, the rows of a K/V head, below 2^31 - 256; B (max_ctx_len / 32 + 6) below 2^31; others: ECOSERVE_EINVAL.
+ * Limits: T Hq / Hkv, the rows of a K/V head, below 2^31 - 256, and T Hq + 256 B Hkv below 2^31; B (max_ctx_len / 32 + 6) below 2^31; others: ECOSERVE_EINVAL.
  * Weights keep 16 bits in the product with the values in steps, and in prompts over ECOSERVE_CACHE_LAYOUT with head_dim other than 128; in other prompts they are rounded to bf16, 8 bits.
  * None is above 1.  Maxima, sums and lse are fp32.
  * Calls that share a context are ordered (rules at the top): work that is split is counted in the context's merge counters.  Calls that may

@@ -542,6 +542,8 @@ size_t ecoserve_cache_scale_bytes(const ecoserve_layout* L) {
   return layout_ok(L, &st) ? (size_t)L->num_blocks * L->num_kv_heads * kScaleBytes : 0;
 }
 
+// (a workgroup of 256 threads to 16 tokens and two to a sequence; a launch takes fewer than 2^32 threads)
+static bool cached_tokens_ok(int32_t B, int32_t T) { return (int64_t)T + 32 * (int64_t)B < (int64_t)1 << 28; }
 // What the calls on an ecoserve_cache ask of it.  (Its addresses are looked at where there is something to do.)
 static int cache_status(const ecoserve_ctx* c, const ecoserve_cache* cache) {
   if (!cache || !quant_format_ok(cache->format)) return ECOSERVE_EINVAL;
@@ -565,7 +567,7 @@ int ecoserve_kv_append_norm(ecoserve_ctx* c, const ecoserve_cache* cache, const 
   if (q && (!stride_ok(c, q_row_stride, L.num_q_heads) || !stride_ok(c, q_out_row_stride, L.num_q_heads))) return ECOSERVE_EINVAL;
   if (B == 0 || T == 0) return ECOSERVE_OK;
   if (!cache_there(cache) || !k_new || !v_new || !cu_q || !ctx_before || !block_table || (rope && !inv_freq)) return ECOSERVE_EINVAL;
-  if (B > c->max_batch || bt_stride <= 0 || max_new_len > T || max_new_len == 0) return ECOSERVE_EINVAL;
+  if (B > c->max_batch || bt_stride <= 0 || max_new_len > T || max_new_len == 0 || !cached_tokens_ok(B, T)) return ECOSERVE_EINVAL;
   if (!aligned16(k_new) || !aligned16(v_new) || !aligned16(q) || !aligned16(q_out)) return ECOSERVE_EINVAL;
   if (rope && ((reinterpret_cast<uintptr_t>(inv_freq) & 7u) || (reinterpret_cast<uintptr_t>(positions) & 3u))) return ECOSERVE_EINVAL;
   DeviceGuard guard(c->device);
@@ -586,7 +588,7 @@ int ecoserve_kv_read(ecoserve_ctx* c, const ecoserve_cache* cache, void* k_rows,
   if (!stride_ok(c, row_stride, L.num_kv_heads)) return ECOSERVE_EINVAL;
   if (B == 0 || T == 0) return ECOSERVE_OK;
   if (!cache_there(cache) || (!k_rows && !v_rows) || !cu || !first || !block_table) return ECOSERVE_EINVAL;
-  if (B > c->max_batch || bt_stride <= 0 || !aligned16(k_rows) || !aligned16(v_rows)) return ECOSERVE_EINVAL;
+  if (B > c->max_batch || bt_stride <= 0 || !aligned16(k_rows) || !aligned16(v_rows) || !cached_tokens_ok(B, T)) return ECOSERVE_EINVAL;
   DeviceGuard guard(c->device);
   if (!guard.ok) return ECOSERVE_EHIP;
   const ReadBack a = {cache->k, cache->v, cache->scales, k_rows, v_rows, (int32_t)row_stride, cu, first, block_table, bt_stride, B, T, L.num_kv_heads, L.head_dim,
@@ -599,10 +601,10 @@ static bool scores_ok(const ecoserve_scores* scores) {
   auto aligned4 = [](const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; };
   return (scores->softcap == 0.f || (scores->softcap >= 0x1p-126f && !isinf(scores->softcap))) && aligned4(scores->slopes) && aligned4(scores->key_begin) && aligned4(scores->key_end);
 }
-// (prompts of more rows than 32 bits count are refused)
+// (prompts of more rows than 32 bits count, or of more threads than a launch takes, are refused)
 static bool scored_rows_ok(const ecoserve_ctx* c, int32_t B, int32_t T) {
   const int64_t G = c->lay.num_q_heads / c->lay.num_kv_heads;
-  return T * G <= 0x7fffffffLL - kMostTileRows && prefill_scored_tiles(kTileRows, B, T, (int32_t)G) * c->lay.num_kv_heads <= 0x7fffffffLL;
+  return T * G <= 0x7fffffffLL - kMostTileRows && (int64_t)T * c->lay.num_q_heads + (int64_t)kMostTileRows * B * c->lay.num_kv_heads <= 0x7fffffffLL;
 }
 static ScoredArgs scored_args(const ecoserve_ctx* c, const ecoserve_cache* cache, const ecoserve_scores* scores, const void* q, int64_t q_row_stride,
                               const int32_t* cu_q, const int32_t* ctx, const int32_t* block_table, int32_t bt_stride, void* out, float* lse, int32_t B, int32_t T,

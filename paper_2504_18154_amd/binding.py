@@ -613,7 +613,7 @@ class Context:
         L, s = self.layout, cache.struct
         n, dtype = L.num_blocks * L.num_kv_heads * L.block_size * L.head_dim, self.torch_dtype if s.format == CACHE_LAYOUT else torch.uint8
         if self._same(cache.k, "k", dtype, n) != s.k or self._same(cache.v, "v", dtype, n) != s.v or (
-                cache.scales is not None and self._same(cache.scales, "scales", torch.uint8, 32 * L.num_blocks * L.num_kv_heads) != s.scales):
+                (None if cache.scales is None else self._same(cache.scales, "scales", torch.uint8, 32 * L.num_blocks * L.num_kv_heads)) != s.scales):
             raise ValueError("the cache's tensors have moved since it was made")
         return ctypes.byref(s)
 
@@ -623,7 +623,7 @@ class Context:
         s = scores.struct
         for t, what, dtype, least, at in ((scores.slopes, "slopes", torch.float32, self.layout.num_q_heads, s.slopes), (scores.key_begin, "key_begin", torch.int32, T, s.key_begin),
                                           (scores.key_end, "key_end", torch.int32, T, s.key_end)):
-            if t is not None and self._same(t, what, dtype, least) != (at or 0):
+            if (None if t is None else self._same(t, what, dtype, least) or None) != at:
                 raise ValueError(f"{what} has moved since the scores' form was made")
         return ctypes.byref(s)
 
@@ -642,7 +642,7 @@ class Context:
             raise ValueError("k_new and v_new must have the same row stride")
         if norm is not None:
             for w, what, heads, at in ((norm.q_weight, "q_weight", L.num_q_heads, norm.struct.q_weight), (norm.k_weight, "k_weight", L.num_kv_heads, norm.struct.k_weight)):
-                if w is not None and (tuple(w.shape) != ((heads, L.head_dim) if norm.struct.per_head else (L.head_dim,)) or self._same(w, what, torch.float32) != at):
+                if (at is not None) if w is None else tuple(w.shape) != ((heads, L.head_dim) if norm.struct.per_head else (L.head_dim,)) or self._same(w, what, torch.float32) != at:
                     raise ValueError(f"{what} must be [D] or [heads, D], where it was when the norm was made")
         freq = None
         if rope is not None:

@@ -352,9 +352,9 @@ const ecoserve_cache* paged_cache(LayerArguments& in, int i) {
 const ecoserve_scores* score_form(LayerArguments& in, int i, int64_t tokens) {
   const auto* const scores = static_cast<const ecoserve_scores*>(in.handle(i));
   if (!in.taken || !scores) return nullptr;
-  if (in.a[i + 1] != Py_None && in.whole(i + 1, at::kFloat, in.l->num_q_heads) != scores->slopes) in.taken = false;
-  if (in.a[i + 2] != Py_None && in.ints(i + 2, tokens) != scores->key_begin) in.taken = false;
-  if (in.a[i + 3] != Py_None && in.ints(i + 3, tokens) != scores->key_end) in.taken = false;
+  if ((in.a[i + 1] == Py_None ? nullptr : in.whole(i + 1, at::kFloat, in.l->num_q_heads)) != scores->slopes) in.taken = false;
+  if ((in.a[i + 2] == Py_None ? nullptr : in.ints(i + 2, tokens)) != scores->key_begin) in.taken = false;
+  if ((in.a[i + 3] == Py_None ? nullptr : in.ints(i + 3, tokens)) != scores->key_end) in.taken = false;
   return scores;
 }
 
@@ -369,8 +369,8 @@ PyObject* kv_append_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const int32_t T = in.size(13, 0), B = in.numel(16), width = in.size(17, 1), most = in.or_all(20, T);
     if (norm) {
       const int64_t D = in.l->head_dim, q_heads = norm->per_head ? in.l->num_q_heads : 1, k_heads = norm->per_head ? in.l->num_kv_heads : 1;
-      if (in.a[8] != Py_None && (in.whole(8, at::kFloat, q_heads * D) != norm->q_weight || in.numel(8) != q_heads * D)) in.taken = false;
-      if (in.a[9] != Py_None && (in.whole(9, at::kFloat, k_heads * D) != norm->k_weight || in.numel(9) != k_heads * D)) in.taken = false;
+      if (in.a[8] == Py_None ? norm->q_weight != nullptr : in.whole(8, at::kFloat, q_heads * D) != norm->q_weight || in.numel(8) != q_heads * D) in.taken = false;
+      if (in.a[9] == Py_None ? norm->k_weight != nullptr : in.whole(9, at::kFloat, k_heads * D) != norm->k_weight || in.numel(9) != k_heads * D) in.taken = false;
     }
     const double* freq = nullptr;
     const int32_t* positions = nullptr;

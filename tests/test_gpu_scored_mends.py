@@ -6,6 +6,7 @@ import pytest
 import torch
 
 from oracle import scored_oracle as so
+from tests.parity_util import dev_i32
 from tests.scored_util import HALF, Pools, check_rows, packed
 from tests.test_gpu_scored import FORMATS, _decode, _prefill, _q, _scores
 
@@ -244,4 +245,40 @@ def test_weights_keep_sixteen_bits_in_prompts(D, Hq, Hkv, few):
     assert (out[row][..., 5] == float("inf")).all() and out[~row].isfinite().all() and lse.isfinite().all()
     out[..., 5] = 0
     assert out.isfinite().all()
+    p.ctx.close()
+
+
+def test_structs_whose_tensors_are_gone():
+    """What a struct names and its holder no longer holds is refused, and not read."""
+    total = np.array([20])
+    p = Pools("e4m3", 64, 4, 2, total, seed=115)
+    p.fill(total, 116)
+    b = p.binding
+    q = _q(1, p, 117)
+    seen = torch.zeros(1, dtype=torch.int32, device="cuda")
+    make = lambda: b.Scores(slopes=torch.zeros(4, device="cuda"), key_begin=seen, key_end=seen + 20)
+    assert _decode(p, total, q, make())[0].isfinite().all() and _prefill(p, total - 1, np.ones(1, dtype=int), q, make())[0].isfinite().all()
+    for name in ("slopes", "key_begin", "key_end"):
+        scores = make()
+        setattr(scores, name, None)
+        with pytest.raises(ValueError):
+            _decode(p, total, q, scores)
+        with pytest.raises(ValueError):
+            _prefill(p, total - 1, np.ones(1, dtype=int), q, scores)
+    none = torch.zeros(0, dtype=torch.int32, device="cuda")
+    p.ctx.attn_prefill_scored(q[:0], p.cache, dev_i32([0, 0]), dev_i32([3]), p.dev_table, q[:0].clone(), scores=b.Scores(key_begin=none))   # (no tokens, no ranges)
+    rows = torch.randn(1, 2, 64, device="cuda").to(torch.bfloat16)
+    w = torch.ones(64, device="cuda")
+    cu, at = dev_i32([0, 1]), dev_i32([3])
+    for name in ("q_weight", "k_weight"):
+        norm = b.HeadNorm(1e-6, w, w)
+        p.ctx.kv_append_norm(p.cache, rows, rows, cu, at, p.dev_table, norm=norm)
+        setattr(norm, name, None)
+        with pytest.raises(ValueError):
+            p.ctx.kv_append_norm(p.cache, rows, rows, cu, at, p.dev_table, norm=norm)
+    p.ctx.kv_append_norm(p.cache, rows, rows, cu, at, p.dev_table, norm=b.HeadNorm(1e-6, None, w))
+    bare = b.PagedCache(p.cache.k, p.cache.v, p.cache.scales, format="e4m3")
+    bare.scales = None
+    with pytest.raises(ValueError):
+        p.ctx.kv_append_norm(bare, rows, rows, cu, at, p.dev_table)
     p.ctx.close()

@@ -28,6 +28,7 @@ constexpr int kVHeads = 4;  // heads of V to a workgroup
 // Heads of K and Q to a workgroup from which its lanes work on two rows at a time.  72 heads of 65 536 tokens into codes: 573 us with one, 506 with two; into bf16 600 and
 // 704.  7 heads of 2400 tokens: 38 with one, 47 with two, whose registers (118 for 85) leave fewer workgroups to a CU.
 constexpr int kManyHeads = 16;
+constexpr float kLeastEps = 0x1p-100f;  // of a norm, beside which squares below 2^-126 do not count
 
 // Sum and maximum over the LP lanes that hold a row; every lane has the result, in the same order of sums everywhere.
 template <int LP, typename Op>
@@ -163,10 +164,20 @@ __device__ __forceinline__ void formed(float (&y)[8], Raw<kAdjacent>& raw, const
   values_of(x, raw.own);
   values_of(other, raw.partner);
   if (per_D > 0.f) {
-    float sum = 0.f;
+    auto squares = [&]() {
+      float sum = 0.f;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) sum = __builtin_fmaf(x[i], x[i], sum);
-    sum = over_row<LP>(sum, [](float a, float b) { return a + b; });
+      for (int i = 0; i < 8; ++i) sum = __builtin_fmaf(x[i], x[i], sum);
+      return over_row<LP>(sum, [](float a, float b) { return a + b; });
+    };
+    float sum = squares();
+    if (eps < kLeastEps) {  // (squares that fp32 has no bits for are the whole of the mean: they are taken of the row times 2^80)
+      const bool tiny = sum < 0x1p-60f;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i] = tiny ? x[i] * 0x1p80f : x[i], other[i] = tiny ? other[i] * 0x1p80f : other[i];
+      sum = squares();
+      eps = tiny ? eps * 0x1p80f * 0x1p80f : eps;
+    }
     const float f = rsqrtf(__builtin_fmaf(sum, per_D, eps));
     // (before the weights and the rotation: what is large stays inside fp32)
 #pragma unroll

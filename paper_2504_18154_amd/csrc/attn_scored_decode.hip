@@ -21,10 +21,11 @@
 // ride in the eight columns that groups of up to eight heads leave (their columns repeat the heads, so a lane has both parts in hand and takes one), and cost a few vector instructions;
 // larger groups take a product for each part (64 heads on 4 of 128, 32 x 16 k ... 131 k tokens over e4m3: 430 us, with weights of 8 bits 408; one of 20 000: 24.7 and 22.0).
 //
-// Measured: 32 contexts of 16 k ... 131 k tokens, 64 heads on 8 of 128, e4m3: 786 us (5.03 GB, 6.4 TB/s; reads reach 7.0).  64 of 100 ... 4000 tokens, 40 heads on 8: 57 us
-// (4.7 TB/s: four of five heads are cut, a piece costs 5 us of latency, and its workgroup's neighbour on the CU covers half of it).  One of 20 000 tokens, int8: 20.1 us, of
+// Measured: 32 contexts of 16 k ... 131 k tokens, 64 heads on 8 of 128, e4m3: 787 us (5.03 GB, 6.4 TB/s; reads reach 7.0).  64 of 100 ... 4000 tokens, 40 heads on 8: 58 us
+// (4.2 TB/s: four of five heads are cut, a piece costs 5 us of latency, and its workgroup's neighbour on the CU covers half of it).  One of 20 000 tokens, int8: 20.9 us, of
 // which 6 are the reads: the numbering, ids and first keys 6, the wavefronts' states 2, writing and counting 1.5, adding up 5.  96 windows of 1024 tokens, 8 heads on 1
-// of 256, bf16: 30 us (3.3 TB/s), a workgroup to a CU.
+// of 256, bf16: 31 us (3.2 TB/s), a workgroup to a CU.  Over codes, heads that do not fill an instance and capped or biased ones of 256 spill some 20 registers around the loop
+// (32 x 9 k ... 60 k tokens, 8 heads of 80, int8: 4.5 TB/s).
 //
 // Lane layouts relied upon (lane = 16 quad + col), 16x16x32:  A[row = col][k = 8 quad .. + 7],  B[k = 8 quad .. + 7][col],  C[row = 4 quad + i][col].
 #include <type_traits>

@@ -24,10 +24,10 @@
 // 256 over bf16 389 and 475, 8 on 8 of 80 163 and 208;  what was not taken: over e4m3 446 and 557, two of 8192, 64 heads on 8 of 128 2190 and 2990).  Maxima, sums and the log-sum-exp are
 // fp32, from the weights as they were.
 //
-// Measured, 64 heads on 8 of 128: two prompts of 8192 tokens over e4m3 2140 us (1028 TFLOP/s; a library product of 8192^3 reaches 1220), over bf16 2065; a step of
-// 64 keys is 200 vector instructions beside 32 matrix ones of a wavefront, the units are busy 46 and 45% of the time, LDS has no bank conflicts, and the clock gives
+// Measured, 64 heads on 8 of 128: two prompts of 8192 tokens over e4m3 2100 ... 2190 us from card to card (1045 ... 1005 TFLOP/s; a library product of 8192^3 reaches 1220), over bf16
+// 2040 ... 2145; a step of 64 keys is 201 vector instructions beside 32 matrix ones of a wavefront, the units are busy 47 and 45% of the time, LDS has no bank conflicts, and the clock gives
 // way: fewer instructions raise it more than they save cycles.  Capped scores cost four vector instructions each, two of them at half rate (2048 tokens of three
-// prompts 127 us).  24 prompts of 5 ... 300 tokens, 32 heads on 8 of 64, biased: 23.6 us, of which 5 are a workgroup's way to its first keys.
+// prompts 129 us).  24 prompts of 5 ... 300 tokens, 32 heads on 8 of 64, biased: 23.4 us, of which 5 are a workgroup's way to its first keys.
 //
 // Lane layouts relied upon (lane = 32 half + col), 32x32x16:  A[row = col][k = 8 half .. + 7],  B[k = 8 half .. + 7][col],
 // C[row = 8 (i / 4) + 4 half + i % 4][col].

@@ -26,7 +26,7 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kVHeads = 4;  // heads of V to a workgroup
 // Heads of K and Q to a workgroup from which its lanes work on two rows at a time.  72 heads of 65 536 tokens into codes: 573 us with one, 506 with two; into bf16 600 and
-// 704.  7 heads of 2400 tokens: 38 with one, 47 with two, whose registers (118 for 85) leave fewer workgroups to a CU.
+// 704.  7 heads of 2400 tokens: 38 with one, 47 with two, whose registers (116 for 86) leave fewer workgroups to a CU.
 constexpr int kManyHeads = 16;
 constexpr float kLeastEps = 0x1p-100f;  // of a norm, beside which squares below 2^-126 do not count
 

@@ -41,8 +41,8 @@ constexpr int32_t kScoredMostPieces = 256;  // of a (sequence, K/V head)
 constexpr int32_t kLeastSteps = 8;          // of a share
 constexpr int32_t kShortShare = 16;         // (see the kernel)
 constexpr int32_t kPieceCost = 4;           // units in front of a (sequence, K/V head)'s steps
-// Workgroups of four wavefronts that a CU holds, by the registers of the kernel's instances (chunks: of 32 channels; wide: groups of more than eight heads.  Those over codes,
-// 64 x 100 ... 4000 tokens, 64 heads on 4 of 128: 48 us with one, whose registers hold all; spilled, two were behind it).
+// Workgroups of four wavefronts that a CU holds, by the registers of the kernel's instances (chunks: of 32 channels; wide: groups of more than eight heads, whose weights' second parts are products of their
+// own.  Over codes of 128 channels these spill with two: 64 x 100 ... 4000 tokens, 40 heads on 8, as wide ones, 74 us for 57 with weights in one part; with one, 64 heads on 4, 48 for 44).
 constexpr int32_t decode_scored_waves(bool narrow, int32_t chunks, bool wide) { return chunks == 8 || (chunks == 4 && (!narrow || wide)) ? 1 : 2; }
 // Short batches over coded caches, a CU's share of which one workgroup takes: it has eight wavefronts, and twice as many bytes on their way.  One sequence of
 // 20 000 tokens: 22.3 us with four, 20.7 with eight.  (Long ones leave no difference between two workgroups of four and one of eight but their barriers.)

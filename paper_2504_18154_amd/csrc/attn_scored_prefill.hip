@@ -232,7 +232,12 @@ __global__ __launch_bounds__(64 * kWaves, NC == 8 ? 1 : 2) void prefill_scored_k
   const int w_lo = -lanes_max(0x7fffffff - lo) + 0x7fffffff, w_hi = lanes_max(hi), w_lo_last = lanes_max(none ? 0 : lo), w_hi_first = 0x7fffffff - lanes_max(none ? 0 : 0x7fffffff - hi);
   const bool given = key_begin || key_end;
   if (lane == 0) s_lo[wave] = w_lo, s_hi[wave] = w_hi;
-  if (given && half == 0) s_row_lo[wave * 32 + col] = lo, s_row_hi[wave * 32 + col] = hi;
+  if (given) {
+    // (a row without keys stands in for the nearest one of its wavefront that has some: those around it are neighbours then)
+    const uint32_t some = (uint32_t)__ballot(!none), before = some & (0xffffffffu >> (31 - col));
+    const int as = some ? before ? 31 - __builtin_clz(before) : __builtin_ctz(some) : col, as_lo = __shfl(lo, as), as_hi = __shfl(hi, as);
+    if (half == 0) s_row_lo[wave * 32 + col] = as_lo, s_row_hi[wave * 32 + col] = as_hi;
+  }
   if (tid < 2) s_bad[tid] = 0;
   __syncthreads();
   int t_lo = s_lo[0], t_hi = s_hi[0];
@@ -278,13 +283,13 @@ __global__ __launch_bounds__(64 * kWaves, NC == 8 ? 1 : 2) void prefill_scored_k
   uint32_t k_scale = 127, v_scale[4] = {0x7f7f7f7fu, 0x7f7f7f7fu, 0x7f7f7f7fu, 0x7f7f7f7fu};
   int id_k = 0, id_v = 0;
   const int v_block = wave & 3, v_part = wave >> 2;  // the block of V that the wavefront stages, and which of its runs of 64 places first
+  uint64_t seen_asked = 0, seen_stored = 0;  // tiles with gaps: the keys that are seen, of the step whose blocks were named last and of the next one to be stored
   // (blocks without keys of the tile are not named: another of its blocks stands in, and is masked)
   auto load_ids = [&](int j, auto gapped) __attribute__((always_inline)) {
     constexpr bool kGaps = decltype(gapped)::value;
-    uint64_t seen = 0;
-    if constexpr (kGaps) seen = seen_in(j);
-    id_k = table[entry_of_block(4 * j + (lane >> 4), blk_lo, blk_hi, kGaps, seen)];
-    id_v = table[entry_of_block(4 * j + v_block, blk_lo, blk_hi, kGaps, seen)];
+    if constexpr (kGaps) seen_asked = seen_in(j);
+    id_k = table[entry_of_block(4 * j + (lane >> 4), blk_lo, blk_hi, kGaps, seen_asked)];
+    id_v = table[entry_of_block(4 * j + v_block, blk_lo, blk_hi, kGaps, seen_asked)];
   };
   auto at_block = [](int id, uint32_t stride) { return (size_t)(uint32_t)id * stride; };
   auto load = [&]() __attribute__((always_inline)) {
@@ -328,7 +333,7 @@ __global__ __launch_bounds__(64 * kWaves, NC == 8 ? 1 : 2) void prefill_scored_k
     // V: slots behind the tile's last key (nobody sees them) may hold anything: zeros.  So are those in front of the first, and between others that none of its rows sees.
     const int key0 = j * kKeys + 16 * v_block;
     uint32_t slots = 0xffffu;
-    if constexpr (decltype(gapped)::value) slots &= (uint32_t)(seen_in(j) >> (16 * v_block));
+    if constexpr (decltype(gapped)::value) slots &= (uint32_t)(seen_stored >> (16 * v_block));
     else if (key0 < t_lo || key0 + 16 > t_hi) slots &= (uint32_t)keys_seen(t_lo, t_hi, key0);
     const bool edge = slots != 0xffffu;
     if constexpr (W::kNarrow) {
@@ -525,8 +530,10 @@ __global__ __launch_bounds__(64 * kWaves, NC == 8 ? 1 : 2) void prefill_scored_k
   auto walk = [&](auto gapped) __attribute__((always_inline)) {
     load_ids(j0, gapped);
     load();
+    seen_stored = seen_asked;
     if (j0 + 1 < j1) load_ids(j0 + 1, gapped);
     store(j0, gapped);
+    seen_stored = seen_asked;
     if (j0 + 1 < j1) {
       load();
       if (j0 + 2 < j1) load_ids(j0 + 2, gapped);
@@ -540,6 +547,7 @@ __global__ __launch_bounds__(64 * kWaves, NC == 8 ? 1 : 2) void prefill_scored_k
         if (!first && j >= wj0 && j < wj1) [[clang::always_inline]] step(j, gapped);
         if (j + 1 < j1) {
           store(j + 1, gapped);
+          seen_stored = seen_asked;
           if (j + 2 < j1) {
             load();
             if (j + 3 < j1) load_ids(j + 3, gapped);
@@ -552,6 +560,7 @@ __global__ __launch_bounds__(64 * kWaves, NC == 8 ? 1 : 2) void prefill_scored_k
         __syncthreads();
         if (j + 1 < j1) {
           store(j + 1, gapped);
+          seen_stored = seen_asked;
           if (j + 2 < j1) {
             load();
             if (j + 3 < j1) load_ids(j + 3, gapped);

@@ -68,7 +68,16 @@ BLOCKS = r"""
 using namespace eco;
 typedef std::vector<std::pair<int, int>> Ranges;
 // What the kernel reads and keeps of a tile whose rows have these ranges (no keys: 2^31 - 1, 0).
-static bool right(const Ranges& rows) {
+static bool right(const Ranges& given) {
+  // (a row without keys stands in for the one in front of it, among its wavefront's 32, that has some, or the first one behind it)
+  Ranges rows = given;
+  for (size_t w = 0; w < rows.size(); w += 32) {
+    const size_t end = std::min(w + 32, rows.size());
+    for (size_t i = w + 1; i < end; ++i)
+      if (rows[i].second == 0) rows[i] = rows[i - 1];
+    for (size_t i = end - 1; i > w; --i)
+      if (rows[i - 1].second == 0) rows[i - 1] = rows[i];
+  }
   bool gaps = false;
   int lo = 0x7fffffff, hi = 0;
   for (size_t i = 0; i < rows.size(); ++i) {
@@ -77,7 +86,7 @@ static bool right(const Ranges& rows) {
   }
   if (hi == 0) return true;
   std::vector<char> sees(hi + 64, 0);
-  for (const auto& r : rows)
+  for (const auto& r : given)
     for (int k = r.first; k < r.second; ++k) sees[k] = 1;
   for (int j = lo / 64; j <= (hi - 1) / 64; ++j) {
     uint64_t seen = 0;

@@ -21,7 +21,7 @@
 //
 // Weights are rounded to bf16 for the second product (2^-9 of each, unbiased) where the cache's codes, of 4 and 7 bits, are coarser, and in heads of 128, as in the other call for prompts of
 // those; over bf16 caches of other heads, where that call holds more, they are two bf16 numbers, 16 bits, and products of their own (us with one part and with two: 4 x 4096 tokens, 8 heads on 1 of
-// 256 over bf16 389 and 475, 8 on 8 of 80 163 and 208;  what was not taken: over e4m3 446 and 557, two of 8192, 64 heads on 8 of 128 2190 and 2990).  Maxima, sums and the log-sum-exp are
+// 256 over bf16 389 and 475, 8 on 8 of 80 163 and 204;  what was not taken: over e4m3 446 and 557, two of 8192, 64 heads on 8 of 128 2190 and 2990).  Maxima, sums and the log-sum-exp are
 // fp32, from the weights as they were.
 //
 // Measured, 64 heads on 8 of 128: two prompts of 8192 tokens over e4m3 2100 ... 2190 us from card to card (1045 ... 1005 TFLOP/s; a library product of 8192^3 reaches 1220), over bf16

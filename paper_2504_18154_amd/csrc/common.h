@@ -303,7 +303,7 @@ __device__ __forceinline__ size_t v_index(int64_t blk, int g, int slot, int d, i
 }
 
 // The sequence that work unit `unit` belongs to, for units numbered so that sequence b's begin at
-// first(cu_q[b], b), increasing in b, first(0, 0) = 0: a search with 64 candidates at a time, no prefix sum over the batch
+// first(cu_q[b], b), never falling in b (of equal ones the last is found), first(0, 0) = 0: a search with 64 candidates at a time, no prefix sum over the batch
 // and no barrier; what the caller needs of the batch description comes along with the last round.  Whole wavefronts.
 struct SeqOf {
   int b, tok0, S, cb;  // sequence, its first packed token, new tokens, cached tokens
